@@ -424,6 +424,130 @@ int32_t cqa_dense_attention(const void* q_fp16_dev, const void* k_fp16_dev,
                             void* workspace_dev, void* stream);
 int64_t cqa_dense_workspace_bytes(int32_t batch, int32_t n_q_heads, int64_t n_tokens);
 
+/* ---- several drafted tokens at once: rotary positions, a tree (or a chunk) over the cache,
+ *      reading the cache back ------------------------------------------------------------- */
+
+/* Number types of the calls below that take a choice. */
+enum { CQA_TYPE_FP16 = 0, CQA_TYPE_BF16 = 1, CQA_TYPE_FP32 = 2 };
+
+/* Where a row of 128 contiguous channels lies: element strides of its sequence, head and token.
+ * Any values, in any order; rows that are written must not overlap. */
+typedef struct cqa_strides {
+  int64_t batch;
+  int64_t head;
+  int64_t token;
+} cqa_strides;
+
+/* Channels that turn together: i and i + rot_dim / 2, or 2 i and 2 i + 1. */
+enum { CQA_ROTARY_HALF = 0, CQA_ROTARY_INTERLEAVED = 1 };
+/* Frequencies f_i = base^(-2 i / rot_dim), i < rot_dim / 2:
+ *   PLAIN   as they are;
+ *   LINEAR  f_i / factor (positions are compressed);
+ *   PARTS   f_i (g + (1 - g) / factor) with g = clamp((r_i - low_rotations) / (high_rotations -
+ *           low_rotations), 0, 1), r_i = trained_tokens f_i / 2 pi: pairs that turn often within the
+ *           trained length keep their frequency, those that do not complete a turn are stretched. */
+enum { CQA_ROTARY_PLAIN = 0, CQA_ROTARY_LINEAR = 1, CQA_ROTARY_PARTS = 2 };
+
+typedef struct cqa_rotary_desc {
+  int32_t rot_dim;        /* even, 2 .. 128: the first rot_dim channels turn, the others are copied      */
+  int32_t layout;         /* CQA_ROTARY_HALF or CQA_ROTARY_INTERLEAVED                                   */
+  int32_t scaling;        /* CQA_ROTARY_PLAIN, _LINEAR or _PARTS                                         */
+  float magnitude;        /* the turned channels are multiplied by it (1: none), finite, not 0           */
+  double base;            /* finite, >= 1                                                                */
+  double factor;          /* LINEAR, PARTS: finite, >= 1                                                 */
+  double low_rotations;   /* PARTS: 0 <= low_rotations < high_rotations, finite                          */
+  double high_rotations;
+  int64_t trained_tokens; /* PARTS: >= 1                                                                 */
+} cqa_rotary_desc;
+
+/* One kind of rotary positions: a table of frequencies on the host, no device memory; used from any
+ * number of threads, streams and devices at a time. */
+typedef struct cqa_rotary cqa_rotary;
+int32_t cqa_rotary_create(const cqa_rotary_desc* desc, cqa_rotary** out);
+int32_t cqa_rotary_destroy(cqa_rotary* r);
+
+/* Rows to turn: in_dev and out_dev, [batch][n_heads][n_tokens] rows at the given strides. */
+typedef struct cqa_rotary_rows {
+  const void* in_dev;
+  void* out_dev;
+  int32_t n_heads;        /* 1 .. 65535 */
+  int32_t reserved;       /* 0 */
+  cqa_strides in_strides;
+  cqa_strides out_strides;
+} cqa_rotary_rows;
+
+/* Turns the rows of n_rows (1 or 2) tensors, the queries and the keys of a projection, in one launch:
+ * a pair (a, b) of the row of token t of sequence s becomes
+ *   magnitude (a cos w - b sin w),  magnitude (a sin w + b cos w),  w = p f_i,
+ * p = positions_dev[s * position_stride + t] (device int64, any value; position_stride 0: the sequences
+ * share their positions), computed in FP32 (the angle exactly modulo a turn, however far the position)
+ * and rounded once.  Negative positions turn back: with -p the call is the gradient of the call with p, and
+ * with -d it moves rows d positions towards the front.
+ * in_type, out_type: CQA_TYPE_*; pointers aligned to their type.  A tensor may be turned in place (same address,
+ * same strides, types of the same size); no other overlap is allowed.
+ * batch 1 .. 65535; n_tokens = 0 does nothing.  Asynchronous on `stream`, on the current device.
+ * Errors: INVALID_ARG; UNSUPPORTED (more tokens or heads than a launch takes); HIP. */
+int32_t cqa_rotary_apply(const cqa_rotary* r, const int64_t* positions_dev, int64_t position_stride,
+                         int32_t batch, int64_t n_tokens, const cqa_rotary_rows* rows, int32_t n_rows,
+                         int32_t in_type, int32_t out_type, void* stream);
+
+/* The cache's own reconstruction of tokens first .. first + n_tokens - 1 of every sequence of `layer`, e.g.
+ * for a program that goes on in FP16, or that moves a sequence elsewhere: sealed tokens
+ *   k = code * sigma + z (one fused FP32 operation),  v = code * scale + offset,
+ * rounded once to `type` (CQA_TYPE_*; beyond FP16's range: its largest number), trailing tokens their FP16 originals.
+ * k_dev, v_dev: [batch][n_kv_heads][n_tokens] rows of 128 at `strides` (host pointer, copied; NULL: contiguous in
+ * that order); either may be NULL.  Needs no originals.  n_tokens = 0 does nothing.  The current device must be
+ * the cache's.  Asynchronous on `stream`, ordered with the cache's appends by it.
+ * Errors: INVALID_ARG (range not within the cache's length, both outputs NULL, ...), HIP. */
+int32_t cqa_cache_read(const cqa_cache* c, int32_t layer, int64_t first, int64_t n_tokens, int32_t type,
+                       void* k_dev, void* v_dev, const cqa_strides* strides, void* stream);
+
+/* Certificate of one (node, query head) of cqa_tree_decode; the fields of cqa_head_cert.  32 bytes. */
+typedef struct cqa_node_cert {
+  float E_key;
+  float E_val;
+  float delta_h;
+  float v_max;
+  float alpha_tail_hat;
+  float lse;               /* -inf: the node attends nothing */
+  float max_block_contrib;
+  float reserved;          /* 0 */
+} cqa_node_cert;
+
+#define CQA_MAX_DRAFT 256
+
+/* Attention of n_draft drafted tokens (nodes) per sequence, none of them appended, in one pass over the cache:
+ * node i attends every token of the cache (if any) and the drafted tokens j of its mask -- itself and its ancestors, for a
+ * tree of drafted tokens -- or, without a mask, tokens 0 .. i: a chunk of a prompt over its cached beginning.
+ *   q_fp16_dev               [batch][n_draft][n_q_heads][128]
+ *   k_draft_dev, v_draft_dev [batch][n_kv_heads][n_draft][128], FP16, as cqa_cache_append takes them
+ *   mask_dev                 uint64 [batch][n_draft][ceil(n_draft / 64)], 8-byte aligned: node i attends draft j where bit
+ *                            j % 64 of its word j / 64 is set (bits from n_draft on are ignored); NULL: j <= i
+ *   O_dev                    FP16 [batch][n_draft][n_q_heads][128]
+ *   cert_dev, flags_dev      [batch][n_draft][n_q_heads]
+ *   workspace_dev            cqa_tree_workspace_bytes(c, n_draft) bytes; calls that share one must be ordered
+ * Sealed tokens are attended as cqa_cache_read gives them in FP16, trailing and drafted ones exactly; FP32 accumulation, the softmax's weights enter the value product in FP16.  The certificate is
+ * that of cqa_certified_decode with what the rounding to FP16 adds: sigma_c becomes the next FP16 number from
+ *   sigma_c + 2 min(sigma_c / 2, 2^-11 max(|z_c - 128 sigma_c|, |z_c + 127 sigma_c|) + 2^-25)
+ * upwards, eta_b becomes eta_b + min(eta_b, 2^-11 (nu_b + eta_b) + 2^-21); v_max ranges over the tokens the node attends.
+ * flags: KEY, VAL, TOTAL, PRECOND by tol's thresholds, force_flags; they only REQUEST precision, there is no ladder for
+ * nodes: a program accepts a path up to its first flagged node and has the token from there on served by a step of the
+ * single-token calls.  A node that attends nothing (an empty cache and mask) returns O = 0, lse = -inf, zeros, and no
+ * flag of its own.  One that attends a drafted key or value that is no finite number returns NaN and PRECOND; other
+ * nodes are not touched by it.
+ * The mask is read on the device: calls can be recorded into a HIP graph (the length of the cache is that at the recording).
+ * The current device must be the cache's.  Asynchronous on `stream`; uses none of the handle's workspaces, so that calls with
+ * workspaces of their own may overlap with each other and with decode calls.
+ * Errors: INVALID_ARG (n_draft < 1, tolerances out of range, null pointers, O, cert, flags, workspace not 16-byte
+ * aligned), UNSUPPORTED (n_draft > CQA_MAX_DRAFT; tol->rank_depth or tol->int8_query not 0: the ranking test and INT8
+ * scoring are the single-token calls'), HIP. */
+int32_t cqa_tree_decode(const cqa_cache* c, int32_t layer, const void* q_fp16_dev, const void* k_draft_dev,
+                        const void* v_draft_dev, int32_t n_draft, const uint64_t* mask_dev,
+                        const cqa_tolerances* tol, void* O_dev, cqa_node_cert* cert_dev, uint32_t* flags_dev,
+                        void* workspace_dev, void* stream);
+/* Holds for every length the cache can have.  Errors: INVALID_ARG, UNSUPPORTED (n_draft). */
+int32_t cqa_tree_workspace_bytes(const cqa_cache* c, int32_t n_draft, int64_t* bytes);
+
 /* ---- misc ------------------------------------------------------------------ */
 
 /* Split count the decode pass uses for the current length of `layer`

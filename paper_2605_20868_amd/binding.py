@@ -39,6 +39,17 @@ FLAG_ANY = 0x1F
 RUNG_SHIFT = 8
 
 
+FP16 = 0
+BF16 = 1
+FP32 = 2
+ROTARY_HALF = 0
+ROTARY_INTERLEAVED = 1
+ROTARY_PLAIN = 0
+ROTARY_LINEAR = 1
+ROTARY_PARTS = 2
+MAX_DRAFT = 256
+
+
 class CacheDesc(C.Structure):
     _fields_ = [("n_layers", C.c_int32), ("batch", C.c_int32), ("n_q_heads", C.c_int32),
                 ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("block_tokens", C.c_int32),
@@ -87,6 +98,32 @@ CERT_BYTES = C.sizeof(HeadCert)
 CERT_FIELDS = [("E_key", "<f4"), ("E_val", "<f4"), ("delta_h", "<f4"), ("v_max", "<f4"),
                ("alpha_tail_hat", "<f4"), ("lse", "<f4"), ("max_block_contrib", "<f4"),
                ("rank_margin", "<f4"), ("top_block", "<i4"), ("served_rung", "<i4")]
+
+
+class Strides(C.Structure):
+    """Element strides of a row's sequence, head and token (cqa_strides)."""
+    _fields_ = [("batch", C.c_int64), ("head", C.c_int64), ("token", C.c_int64)]
+
+
+class RotaryDesc(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("magnitude", C.c_float),
+                ("base", C.c_double), ("factor", C.c_double), ("low_rotations", C.c_double),
+                ("high_rotations", C.c_double), ("trained_tokens", C.c_int64)]
+
+
+class RotaryRows(C.Structure):
+    """A tensor of rows to turn (cqa_rotary_rows); strides are (batch, head, token) in elements."""
+    _fields_ = [("in_dev", C.c_void_p), ("out_dev", C.c_void_p), ("n_heads", C.c_int32), ("reserved", C.c_int32),
+                ("in_strides", Strides), ("out_strides", Strides)]
+
+    def __init__(self, in_dev, out_dev, n_heads, in_strides, out_strides):
+        super().__init__(_ptr(in_dev), _ptr(out_dev), n_heads, 0, Strides(*in_strides), Strides(*out_strides))
+
+
+class NodeCert(C.Structure):
+    _fields_ = [("E_key", C.c_float), ("E_val", C.c_float), ("delta_h", C.c_float), ("v_max", C.c_float),
+                ("alpha_tail_hat", C.c_float), ("lse", C.c_float), ("max_block_contrib", C.c_float),
+                ("reserved", C.c_float)]
 
 
 class CqaError(RuntimeError):
@@ -138,6 +175,12 @@ def _load():
         "cqa_adaptive_state": (i32, [vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
         "cqa_dense_attention": (i32, [vp, vp, vp, i32, i32, i32, i64, vp, vp, vp]),
         "cqa_dense_workspace_bytes": (i64, [i32, i32, i64]),
+        "cqa_rotary_create": (i32, [C.POINTER(RotaryDesc), C.POINTER(vp)]),
+        "cqa_rotary_destroy": (i32, [vp]),
+        "cqa_rotary_apply": (i32, [vp, vp, i64, i32, i64, C.POINTER(RotaryRows), i32, i32, i32, vp]),
+        "cqa_cache_read": (i32, [vp, i32, i64, i64, i32, vp, vp, C.POINTER(Strides), vp]),
+        "cqa_tree_decode": (i32, [vp, i32, vp, vp, vp, i32, vp, C.POINTER(Tolerances), vp, vp, vp, vp, vp]),
+        "cqa_tree_workspace_bytes": (i32, [vp, i32, C.POINTER(i64)]),
         "cqa_time_certified_decode": (i32, [vp, i32, vp, C.POINTER(Tolerances), vp, vp, vp, vp,
                                             i32, C.POINTER(C.c_float), vp]),
         "cqa_time_stream_read": (i32, [vp, i32, i32, C.POINTER(C.c_float), C.POINTER(i64), vp]),
@@ -379,6 +422,46 @@ def cqa_dense_attention(q_dev, k_dev, v_dev, batch, n_q_heads, n_kv_heads, n_tok
     _check(_lib.cqa_dense_attention(_ptr(q_dev), _ptr(k_dev), _ptr(v_dev), batch, n_q_heads,
                                     n_kv_heads, n_tokens, _ptr(O_dev), _ptr(workspace_dev),
                                     _ptr(stream)), "cqa_dense_attention")
+
+
+def cqa_rotary_create(rot_dim=128, layout=ROTARY_HALF, base=10000.0, scaling=ROTARY_PLAIN, factor=1.0, low_rotations=0.0,
+                      high_rotations=0.0, trained_tokens=0, magnitude=1.0):
+    desc = RotaryDesc(rot_dim, layout, scaling, magnitude, base, factor, low_rotations, high_rotations, trained_tokens)
+    h = C.c_void_p(None)
+    _check(_lib.cqa_rotary_create(C.byref(desc), C.byref(h)), "cqa_rotary_create")
+    return h
+
+
+def cqa_rotary_destroy(r) -> None:
+    _check(_lib.cqa_rotary_destroy(r), "cqa_rotary_destroy")
+
+
+def cqa_rotary_apply(r, positions_dev, position_stride, batch, n_tokens, rows, in_type=FP16, out_type=FP16,
+                     stream=None) -> None:
+    """rows: one or two RotaryRows, e.g. the queries' and the keys'."""
+    arr = (RotaryRows * len(rows))(*rows)
+    _check(_lib.cqa_rotary_apply(r, _ptr(positions_dev), position_stride, batch, n_tokens, arr, len(rows), in_type,
+                                 out_type, _ptr(stream)), "cqa_rotary_apply")
+
+
+def cqa_cache_read(h, layer, first, n_tokens, out_type, k_dev, v_dev, strides=None, stream=None) -> None:
+    """strides: (batch, head, token) in elements, or None for contiguous [batch][n_kv_heads][n_tokens][128]."""
+    st = None if strides is None else C.byref(Strides(*strides))
+    _check(_lib.cqa_cache_read(h, layer, first, n_tokens, out_type, _ptr(k_dev), _ptr(v_dev), st, _ptr(stream)),
+           "cqa_cache_read")
+
+
+def cqa_tree_workspace_bytes(h, n_draft) -> int:
+    n = C.c_int64(0)
+    _check(_lib.cqa_tree_workspace_bytes(h, n_draft, C.byref(n)), "cqa_tree_workspace_bytes")
+    return n.value
+
+
+def cqa_tree_decode(h, layer, q_dev, k_draft_dev, v_draft_dev, n_draft, mask_dev, tol: Tolerances, O_dev, cert_dev,
+                    flags_dev, workspace_dev, stream=None) -> None:
+    _check(_lib.cqa_tree_decode(h, layer, _ptr(q_dev), _ptr(k_draft_dev), _ptr(v_draft_dev), n_draft, _ptr(mask_dev),
+                                C.byref(tol), _ptr(O_dev), _ptr(cert_dev), _ptr(flags_dev), _ptr(workspace_dev),
+                                _ptr(stream)), "cqa_tree_decode")
 
 
 def cqa_time_certified_decode(h, layer, q_dev, tol: Tolerances, O_dev, cert_dev, flags_dev,

@@ -13,6 +13,9 @@
 struct cqa_cache {
   cqa::Cache impl;
 };
+struct cqa_rotary {
+  cqa::Rotary impl;
+};
 
 namespace cqa {
 thread_local int g_last_hip_error = 0;
@@ -1136,6 +1139,119 @@ int32_t cqa_dense_attention(const void* q_fp16_dev, const void* k_fp16_dev,
   const int64_t groups = (int64_t)batch * n_kv_heads;
   return launch_dense((const __half*)q_fp16_dev, (const __half*)k_fp16_dev, (const __half*)v_fp16_dev, g, groups,
                       groups, n_tokens, O_dev, nullptr, nullptr, nullptr, 0, (float*)workspace_dev, (hipStream_t)stream);
+}
+
+// ---- several drafted tokens at once
+
+int32_t cqa_rotary_create(const cqa_rotary_desc* desc, cqa_rotary** out) {
+  if (desc == nullptr || out == nullptr) return CQA_ERR_INVALID_ARG;
+  const cqa_rotary_desc& d = *desc;
+  if (d.rot_dim < 2 || d.rot_dim > D || d.rot_dim % 2 != 0 || (d.layout != CQA_ROTARY_HALF && d.layout != CQA_ROTARY_INTERLEAVED) ||
+      d.scaling < CQA_ROTARY_PLAIN || d.scaling > CQA_ROTARY_PARTS || !isfinite(d.magnitude) || d.magnitude == 0.0f ||
+      !isfinite(d.base) || !(d.base >= 1.0))
+    return CQA_ERR_INVALID_ARG;
+  if (d.scaling != CQA_ROTARY_PLAIN && (!isfinite(d.factor) || !(d.factor >= 1.0))) return CQA_ERR_INVALID_ARG;
+  if (d.scaling == CQA_ROTARY_PARTS && (!(d.low_rotations >= 0.0) || !(d.high_rotations > d.low_rotations) ||
+                                        !isfinite(d.high_rotations) || d.trained_tokens < 1))
+    return CQA_ERR_INVALID_ARG;
+  cqa_rotary* r = new (std::nothrow) cqa_rotary;
+  if (r == nullptr) return CQA_ERR_INVALID_ARG;
+  r->impl.rot_dim = d.rot_dim;
+  r->impl.layout = d.layout;
+  r->impl.magnitude = d.magnitude;
+  for (int i = 0; i < D / 2; ++i) {
+    r->impl.turn[i] = 0u;
+    if (i >= d.rot_dim / 2) continue;
+    // turns per position, in the x87 format's 64 bits
+    const long double f = powl((long double)d.base, -2.0L * i / d.rot_dim);
+    long double turn = f / (2.0L * 3.14159265358979323846264338327950288L);
+    if (d.scaling == CQA_ROTARY_LINEAR) turn /= d.factor;
+    if (d.scaling == CQA_ROTARY_PARTS) {
+      const long double g = ((long double)d.trained_tokens * turn - d.low_rotations) / ((long double)d.high_rotations - d.low_rotations);
+      const long double keep = std::min(1.0L, std::max(0.0L, g));
+      turn *= keep + (1.0L - keep) / d.factor;
+    }
+    r->impl.turn[i] = (uint64_t)roundl(ldexpl(turn, 64));   // at most 2^64 / 2 pi
+  }
+  *out = r;
+  return CQA_OK;
+}
+
+int32_t cqa_rotary_destroy(cqa_rotary* r) {
+  if (r == nullptr) return CQA_ERR_INVALID_ARG;
+  delete r;
+  return CQA_OK;
+}
+
+static bool is_type(int32_t t) { return t == CQA_TYPE_FP16 || t == CQA_TYPE_BF16 || t == CQA_TYPE_FP32; }
+static bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+static uintptr_t type_bytes(int32_t t) { return t == CQA_TYPE_FP32 ? 4 : 2; }
+
+int32_t cqa_rotary_apply(const cqa_rotary* r, const int64_t* positions_dev, int64_t position_stride,
+                         int32_t batch, int64_t n_tokens, const cqa_rotary_rows* rows, int32_t n_rows,
+                         int32_t in_type, int32_t out_type, void* stream) {
+  if (r == nullptr || rows == nullptr || n_rows < 1 || n_rows > 2 || batch < 1 || batch > 65535 || n_tokens < 0 ||
+      !is_type(in_type) || !is_type(out_type))
+    return CQA_ERR_INVALID_ARG;
+  if (n_tokens == 0) return CQA_OK;
+  if (positions_dev == nullptr || !aligned(positions_dev, 8)) return CQA_ERR_INVALID_ARG;
+  for (int i = 0; i < n_rows; ++i)
+    if (rows[i].in_dev == nullptr || rows[i].out_dev == nullptr || rows[i].n_heads < 1 || rows[i].n_heads > 65535 ||
+        rows[i].reserved != 0 || !aligned(rows[i].in_dev, type_bytes(in_type)) || !aligned(rows[i].out_dev, type_bytes(out_type)))
+      return CQA_ERR_INVALID_ARG;
+  return launch_rotary(r->impl, positions_dev, position_stride, batch, n_tokens, rows, n_rows, in_type, out_type, (hipStream_t)stream);
+}
+
+// Calls that launch on the handle's arrays directly: the current device has to be the one that holds them.
+static int32_t check_device(const Cache* c) {
+  int cur = -1;
+  CQA_HIP(hipGetDevice(&cur));
+  return cur == c->device ? CQA_OK : CQA_ERR_INVALID_ARG;
+}
+
+int32_t cqa_cache_read(const cqa_cache* h, int32_t layer, int64_t first, int64_t n_tokens, int32_t type,
+                       void* k_dev, void* v_dev, const cqa_strides* strides, void* stream) {
+  if (h == nullptr || layer < 0 || layer >= h->impl.desc.n_layers || first < 0 || n_tokens < 0 || !is_type(type) ||
+      (k_dev == nullptr && v_dev == nullptr) || !aligned(k_dev, type_bytes(type)) || !aligned(v_dev, type_bytes(type)))
+    return CQA_ERR_INVALID_ARG;
+  const Cache* c = &h->impl;
+  if (first > c->length[layer] || n_tokens > c->length[layer] - first) return CQA_ERR_INVALID_ARG;
+  if (n_tokens == 0) return CQA_OK;
+  if (const int32_t rc = check_device(c)) return rc;
+  const cqa_strides st = strides != nullptr ? *strides : cqa_strides{c->desc.n_kv_heads * n_tokens * D, n_tokens * D, D};
+  return launch_read(c, layer, first, n_tokens, type, k_dev, v_dev, st, (hipStream_t)stream);
+}
+
+static int32_t check_draft(const cqa_cache* h, int32_t n_draft) {
+  if (h == nullptr || n_draft < 1) return CQA_ERR_INVALID_ARG;
+  // a workgroup column per KV group of the batch
+  if (n_draft > CQA_MAX_DRAFT || (int64_t)h->impl.desc.batch * h->impl.desc.n_kv_heads > 0xffffff) return CQA_ERR_UNSUPPORTED;
+  return CQA_OK;
+}
+
+int32_t cqa_tree_workspace_bytes(const cqa_cache* h, int32_t n_draft, int64_t* bytes) {
+  if (bytes == nullptr) return CQA_ERR_INVALID_ARG;
+  if (const int32_t rc = check_draft(h, n_draft)) return rc;
+  *bytes = tree_ws_bytes(&h->impl, n_draft);
+  return CQA_OK;
+}
+
+int32_t cqa_tree_decode(const cqa_cache* h, int32_t layer, const void* q_fp16_dev, const void* k_draft_dev,
+                        const void* v_draft_dev, int32_t n_draft, const uint64_t* mask_dev,
+                        const cqa_tolerances* tol, void* O_dev, cqa_node_cert* cert_dev, uint32_t* flags_dev,
+                        void* workspace_dev, void* stream) {
+  if (h == nullptr || layer < 0 || layer >= h->impl.desc.n_layers || q_fp16_dev == nullptr || k_draft_dev == nullptr ||
+      v_draft_dev == nullptr || tol == nullptr || O_dev == nullptr || cert_dev == nullptr || flags_dev == nullptr ||
+      workspace_dev == nullptr || !aligned(q_fp16_dev, 2) || !aligned(k_draft_dev, 2) || !aligned(v_draft_dev, 2) ||
+      !aligned(mask_dev, 8) || !aligned(O_dev, 16) || !aligned(cert_dev, 16) || !aligned(flags_dev, 16) || !aligned(workspace_dev, 16))
+    return CQA_ERR_INVALID_ARG;
+  if (const int32_t rc = check_draft(h, n_draft)) return rc;
+  if (const int32_t rc = check_tolerances(tol, 0)) return rc;
+  if (tol->int8_query != 0) return CQA_ERR_UNSUPPORTED;
+  const Cache* c = &h->impl;
+  if (const int32_t rc = check_device(c)) return rc;
+  return launch_tree(c, layer, (const __half*)q_fp16_dev, (const __half*)k_draft_dev, (const __half*)v_draft_dev, n_draft, mask_dev, *tol,
+                     (__half*)O_dev, cert_dev, flags_dev, (float*)workspace_dev, (hipStream_t)stream);
 }
 
 }  // extern "C"

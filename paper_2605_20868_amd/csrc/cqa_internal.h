@@ -440,6 +440,20 @@ int32_t launch_dense_ladder(Cache* c, int layer, const __half* q, int rung4_min_
 // *launched (may be null) tells whether the split launch, which stores that token, was reached
 int32_t launch_step(Cache* c, int layer, const __half* q, const cqa_tolerances& tol, float* O, cqa_head_cert* cert,
                     uint32_t* flags, hipStream_t st, const __half* k_new, const __half* v_new, bool* launched);
+// Rotary positions (rotary.hip), reading back (read.hip), drafted tokens over the cache (tree.hip)
+struct Rotary {
+  uint64_t turn[D / 2];   // per pair: turns per position, 64 bits behind the point
+  float magnitude;
+  int rot_dim, layout;
+};
+int32_t launch_rotary(const Rotary& r, const int64_t* positions, int64_t pos_batch, int batch, int64_t n_tokens,
+                      const cqa_rotary_rows* rows, int n_rows, int in_type, int out_type, hipStream_t st);
+int32_t launch_read(const Cache* c, int layer, int64_t first, int64_t n, int type, void* k, void* v, const cqa_strides& strides,
+                    hipStream_t st);
+int32_t launch_tree(const Cache* c, int layer, const __half* q, const __half* kd, const __half* vd, int n_draft, const uint64_t* mask,
+                    const cqa_tolerances& tol, __half* O, cqa_node_cert* cert, uint32_t* flags, float* ws, hipStream_t st);
+int64_t tree_ws_bytes(const Cache* c, int n_draft);
+
 inline uint32_t* ladder_raised(Cache* c) { return c->ladder_counts + 2; }
 inline uint32_t next_ladder_tag(Cache* c) {
   c->ladder_seq = c->ladder_seq == 0xFFFFFFFFu ? 1u : c->ladder_seq + 1u;
