@@ -22,6 +22,7 @@
 #include <algorithm>
 
 #include "cqa_internal.h"
+#include "reduce_inl.h"
 
 namespace cqa {
 
@@ -31,11 +32,12 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float SCORE = 0.08838834764831845f * 1.4426950408889634f;   // 1 / sqrt(d), in the exponent's base 2
+constexpr float HALF_SCORE = 0.5f * 0.08838834764831845f;
 constexpr float F16_MAX = 65504.0f;
 constexpr float LN2 = 0.6931471805599453f;
 
 // ---- partial set of a split and 32 rows: the accumulators by (four channels, row), then one float per row for each quantity
-enum { T_M = 0, T_L, T_EV, T_EVMAX, T_DMAX, T_VMAX, T_STATS };
+enum { T_M = 0, T_L, T_SEALED, T_EV, T_EVMAX, T_DMAX, T_VMAX };
 constexpr int T_ROWS = 32;
 constexpr int T_OFLOATS = D * T_ROWS;
 constexpr int T_FLOATS = T_OFLOATS + 8 * T_ROWS;
@@ -48,18 +50,24 @@ struct TreeArgs {
   const __half* kd;        // [Bt][Hkv][n][128]
   const __half* vd;
   const uint64_t* mask;    // [Bt][n][words], or null: node i attends nodes 0 .. i
-  float* part;             // [Bt * Hkv][row tiles][nsplit + 1][T_FLOATS]
+  float* part;             // [Bt * Hkv][row tiles][nsplit][T_FLOATS]
   int64_t nq_cap;
   int64_t nb;              // sealed blocks
   int n, words, trail;     // drafted nodes, mask words of one, trailing tokens
   int n_kv, group;
   int row_tiles;           // of 32 rows
-  int nsplit;              // partial sets of the sealed blocks; one more of the other tokens
+  int nsplit;              // partial sets per row
 };
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const f32x2 x = {lo, hi};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, f16x2));
+}
+// two keys of a dword of codes: code sigma + z
+template <int I>
+__device__ __forceinline__ uint32_t key2(uint32_t codes, float s0, float s1, float z0, float z1) {
+  const uint32_t x = codes >> (16 * I);
+  return pack_f16(fmaf((float)(x & 255u) - 128.0f, s0, z0), fmaf((float)(x >> 8 & 255u) - 128.0f, s1, z1));
 }
 // code scale + offset of two tokens, rounded once.  The scale's rounding to FP16 can take the largest code beyond the group's maximum, and
 // beyond FP16's range where that is at its end (keys cannot: z and sigma are FP32, the largest code is the maximum within 2^-23).
@@ -68,421 +76,595 @@ __device__ __forceinline__ uint32_t value2(uint32_t code, uint32_t scale, uint32
   const f16x2 most = {(_Float16)F16_MAX, (_Float16)F16_MAX};
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_minimum(x, most));
 }
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
-
+// codes of tokens (2 I, 2 I + 1) of a dword as FP16 integers: dropped into the mantissa of 1024, which leaves exactly
+template <int I>
+__device__ __forceinline__ uint32_t codes2(uint32_t d) {
+  const uint32_t x = d >> (8 * I);
+  const uint32_t pair = (x & 0xfu) | (x << 12 & 0xf0000u) | 0x64006400u;
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, pair) - __builtin_bit_cast(f16x2, 0x64006400u));
+}
+__device__ __forceinline__ uint4 values8(uint32_t d, uint4 scale, uint4 off) {
+  return make_uint4(value2(codes2<0>(d), scale.x, off.x), value2(codes2<1>(d), scale.y, off.y), value2(codes2<2>(d), scale.z, off.z),
+                    value2(codes2<3>(d), scale.w, off.w));
+}
 // the width of a key channel in the bound, rounded up to FP16
-__device__ __forceinline__ uint16_t key_width(float sigma, float z) {
+__device__ __forceinline__ uint32_t key_width(float sigma, float z) {
   const float most = fmaxf(fabsf(fmaf(-128.0f, sigma, z)), fabsf(fmaf(127.0f, sigma, z)));
   const float w = fmaf(2.0f, fminf(0.5f * sigma, fmaf(most, 0x1p-11f, 0x1p-25f)), sigma);
   const _Float16 h = (_Float16)w;
-  uint16_t u = __builtin_bit_cast(uint16_t, h);
-  if ((float)h < w) ++u;
-  return u;
+  const uint32_t u = __builtin_bit_cast(uint16_t, h);
+  return (float)h < w ? u + 1u : u;
 }
+__device__ __forceinline__ float value_error(float2 an) { return an.x + fminf(an.x, fmaf(an.y + an.x, 0x1p-11f, 0x1p-21f)); }
 
-// NT tiles of 32 rows per wave, WR waves side by side over rows, WT over tokens; four waves.
-template <int NT, int WR, int WT>
-struct TreeShape {
-  static constexpr int MT = WT == 1 ? 2 : 1;                 // tiles of 32 tokens a wave takes of a tile
-  static constexpr int TOK = 32 * MT * WT;                   // tokens of a tile
-  static constexpr int QUADS = TOK / 64;
-  static constexpr int BLKS = TOK / BLK;
-  static constexpr int ROWS = 32 * NT * WR;
-  static constexpr int KV_BYTES = 2 * TOK * D * 2;
-  static constexpr int OUT_BYTES = WT > 1 ? 4 * T_FLOATS * 4 : 0;   // the waves' sets, joined through LDS
-  static constexpr int MAIN_BYTES = KV_BYTES > OUT_BYTES ? KV_BYTES : OUT_BYTES;
+// What a wave holds of its 32 rows: lane l has row l & 31; its two halves have the tokens of different blocks.
+struct TreeRows {
+  f16x8 q[8];     // run of 8 channels (half * 8 + ks)
+  f32x16 o[4];
+  float m, sum, sealed, ev, evmax, dmax, vmax;
+  int node;
 };
 
-template <int NT, int WR, int WT>
-__global__ __launch_bounds__(256, NT * WR > 2 ? 1 : 2) void tree_split_kernel(TreeArgs a) {
-  using S = TreeShape<NT, WR, WT>;
-  constexpr int MT = S::MT, TOK = S::TOK, BLKS = S::BLKS;
-  __shared__ __align__(16) uint8_t s_main[S::MAIN_BYTES];   // keys [16 runs of 8 channels][TOK] x 16 B, values [TOK / 8][128] x 16 B
-  __shared__ __align__(16) uint16_t s_width[D / 8][32][8];  // key widths of the last 32 blocks
-  __shared__ float s_eta[BLKS];
-  __shared__ float s_norm[TOK];
-  __shared__ uint32_t s_bad[BLKS];
-  uint4* const s_k = reinterpret_cast<uint4*>(s_main);
-  uint4* const s_v = s_k + 16 * TOK;
-
-  const int tid = threadIdx.x, l = tid & 63, n32 = l & 31, half = l >> 5;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wr = w % WR, wt = w / WR;
-  const int head = blockIdx.x;   // (batch, KV head)
-  const int split = blockIdx.y;
-  const int b = head / a.n_kv, kvh = head - b * a.n_kv;
-  const int n_rows = a.n * a.group;
-  const int tile0 = blockIdx.z * (NT * WR) + wr * NT;   // first row tile of the wave
-
-  f16x8 qf[NT][8];
-  int node[NT];
+__device__ __forceinline__ void start_rows(TreeRows& s, const TreeArgs& a, int b, int kvh, int tile) {
+  const int l = threadIdx.x & 63;
+  const int r = min(tile * 32 + (l & 31), a.n * a.group - 1);
+  s.node = r / a.group;
+  const __half* row = a.q + (((int64_t)b * a.n + s.node) * a.n_kv * a.group + kvh * a.group + (r - s.node * a.group)) * D + (l >> 5) * 64;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int r = min((tile0 + nt) * 32 + n32, n_rows - 1);
-    node[nt] = r / a.group;
-    const __half* row = a.q + (((int64_t)b * a.n + node[nt]) * a.n_kv * a.group + kvh * a.group + (r - node[nt] * a.group)) * D;
+  for (int ks = 0; ks < 8; ++ks) s.q[ks] = __builtin_bit_cast(f16x8, ld16_any(row + ks * 8));
+  s.m = -INFINITY;
+  s.sum = s.sealed = s.ev = s.evmax = s.dmax = s.vmax = 0.0f;
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks) qf[nt][ks] = __builtin_bit_cast(f16x8, ld16_any(row + ks * 16 + half * 8));
+  for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s.o[ct][r] = 0.0f;
+}
+
+// Scores, softmax and values of 32 tokens.  key(ks), value(oct, ct): the A operands of the two products; bits, where masked: the tokens
+// of the lane's block that its row attends.
+template <typename Key, typename Value>
+__device__ __forceinline__ void attend32(TreeRows& w, bool masked, uint32_t bits, float eta, Key key, Value value) {
+  f32x16 s;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(key(ks), w.q[ks], s, 0, 0, 0);
+  if (masked) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = bits >> r & 1u ? s[r] : -INFINITY;
   }
-  f32x16 o[NT][4];
-  float m[NT], sum[NT], ev[NT], evmax[NT], dmax[NT], vmax[NT];
+  float top = s[0];
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    m[nt] = -INFINITY;
-    sum[nt] = ev[nt] = evmax[nt] = dmax[nt] = vmax[nt] = 0.0f;
+  for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+  top = max_x32(top) * SCORE;
+  if (__any(top > w.m)) {
+    const float mn = fmaxf(w.m, top);
+    const float f = mn == w.m ? 1.0f : __builtin_amdgcn_exp2f(w.m - mn);
+    w.m = mn;
+    w.sum *= f;
+    w.sealed *= f;
+    w.ev *= f;
+    w.evmax *= f;
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[nt][ct][r] = 0.0f;
+      for (int r = 0; r < 16; ++r) w.o[ct][r] *= f;
   }
-  float nu = 0.0f;
+  const float base = w.m == -INFINITY ? 0.0f : w.m;   // nothing attended yet: every weight is exp2(-inf) = 0
+  uint32_t p[8];
+  float bs = 0.0f;
+#pragma unroll
+  for (int r = 0; r < 16; r += 2) {
+    const float x = __builtin_amdgcn_exp2f(fmaf(s[r], SCORE, -base));
+    const float y = __builtin_amdgcn_exp2f(fmaf(s[r + 1], SCORE, -base));
+    bs += x + y;
+    p[r / 2] = pack_f16(x, y);
+  }
+  const float e = bs * eta;
+  w.sum += bs;
+  w.ev += e;
+  w.evmax = fmaxf(w.evmax, e);
+#pragma unroll
+  for (int oct = 0; oct < 2; ++oct)
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+      w.o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+          value(oct, ct), __builtin_bit_cast(f16x8, make_uint4(p[4 * oct], p[4 * oct + 1], p[4 * oct + 2], p[4 * oct + 3])), w.o[ct], 0, 0, 0);
+}
 
-  // Scores, softmax and values of the tile in LDS.  bits, where masked: the tokens of the lane's block that its row attends.
-  const auto attend = [&](bool masked, const uint32_t (&bits)[NT][MT]) {
-    f32x16 s[MT][NT];
+// Delta of 32 blocks (or of fewer, repeated); width(ks): the A operand
+template <typename Width>
+__device__ __forceinline__ void bound_scores(TreeRows& w, Width width) {
+  f32x16 d;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
+  for (int r = 0; r < 16; ++r) d[r] = 0.0f;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+  for (int ks = 0; ks < 8; ++ks) {
+    uint4 y = __builtin_bit_cast(uint4, w.q[ks]);
+    y.x &= 0x7fff7fffu, y.y &= 0x7fff7fffu, y.z &= 0x7fff7fffu, y.w &= 0x7fff7fffu;
+    d = __builtin_amdgcn_mfma_f32_32x32x16_f16(width(ks), __builtin_bit_cast(f16x8, y), d, 0, 0, 0);
+  }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[mt][nt][r] = 0.0f;
+  for (int r = 0; r < 16; ++r) w.dmax = fmaxf(w.dmax, d[r]);
+}
+
+// place of token t of block `blk` among the keys of a tile: the A operand's rows are dealt to two blocks
+__device__ __forceinline__ int key_place(int blk, int t) { return (blk >> 1) * 32 + (t >> 2) * 8 + (blk & 1) * 4 + (t & 3); }
+// run of 8 tokens of channel c among the values of a tile: the A operand's rows are (c >> 6, c & 15), its tiles (c >> 4) & 3
+__device__ __forceinline__ int value_place(int oct, int c) { return oct * D + ((c >> 4) & 3) * 32 + (c >> 6) * 16 + (c & 15); }
+
+// Trailing and drafted tokens t0 .. t0 + TOK - 1 (of trail + n; zeros behind the last) by THREADS threads, thread `tid`.
+//   keys [16 runs of 8 channels][TOK], values [TOK / 8][128] by value_place, norms [TOK], bad: a bit per token, per block (zero before)
+// A number that is not finite must not meet the zero weight of a row that does not attend its token: the token is taken out, and the
+// rows that do attend it get a sum that is no number.
+template <int THREADS, int TOK>
+__device__ __forceinline__ void load_exact(const TreeArgs& a, int64_t head, int t0, int tid, uint4* keys, uint4* values, float* norms, uint32_t* bad) {
+  const int total = a.trail + a.n;
+  const auto finite = [](uint32_t x) { return (x & 0x7c00u) != 0x7c00u && (x & 0x7c000000u) != 0x7c000000u; };
+#pragma unroll
+  for (int k = 0; k < TOK * 16 / THREADS; ++k) {
+    const int i = tid + k * THREADS, t = i >> 4, run = i & 15, pos = t0 + t;
+    uint4 x = make_uint4(0u, 0u, 0u, 0u);
+    if (pos < total)
+      x = ld16_any((pos < a.trail ? a.trail_k + (head * BLK + pos) * D : a.kd + (head * a.n + pos - a.trail) * D) + run * 8);
+    if (!(finite(x.x) && finite(x.y) && finite(x.z) && finite(x.w))) {
+      atomicOr(&bad[t / BLK], 1u << (t % BLK));
+      x = make_uint4(0u, 0u, 0u, 0u);   // (its other runs are numbers)
+    }
+    keys[run * TOK + key_place(t / BLK, t % BLK)] = x;
+  }
+  // four channels of eight tokens
+#pragma unroll
+  for (int k = 0; k < (TOK * 4 + THREADS - 1) / THREADS; ++k) {
+    const int i = tid + k * THREADS, oct = i >> 5, c = (i & 31) * 4;
+    if (THREADS > TOK * 4 && i >= TOK * 4) break;   // (whole waves)
+    uint32_t x[8][2];
+    float sq[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int pos = t0 + oct * 8 + j;
+      x[j][0] = x[j][1] = 0u;
+      if (pos < total) {
+        const __half* p = (pos < a.trail ? a.trail_v + (head * BLK + pos) * D : a.vd + (head * a.n + pos - a.trail) * D) + c;
+        x[j][0] = ld4_any(p);
+        x[j][1] = ld4_any(p + 2);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const f16x2 u = __builtin_bit_cast(f16x2, x[j][0]), v = __builtin_bit_cast(f16x2, x[j][1]);
+      sq[j] = fmaf((float)u[0], (float)u[0], fmaf((float)u[1], (float)u[1], fmaf((float)v[0], (float)v[0], (float)v[1] * (float)v[1])));
+      if (!(finite(x[j][0]) && finite(x[j][1]))) {
+        const int t = oct * 8 + j;
+        atomicOr(&bad[t / BLK], 1u << (t % BLK));
+        x[j][0] = x[j][1] = 0u;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      sq[j] = sum_x16(row_sum(sq[j]));   // the 32 lanes that have the token
+      if ((i & 31) == j) norms[oct * 8 + j] = sqrtf(sq[j]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      uint32_t h[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) h[j] = __builtin_amdgcn_perm(x[2 * j + 1][e >> 1], x[2 * j][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+      values[value_place(oct, c + e)] = make_uint4(h[0], h[1], h[2], h[3]);
+    }
+  }
+}
+
+// The open ones among the 16 trailing and drafted tokens from `first` on, for a node of sequence b.
+__device__ __forceinline__ uint32_t open_tokens(const TreeArgs& a, int b, int node, int first) {
+  const int j = first - a.trail;   // drafted node of the first token; below 0: trailing ones ahead of it
+  if (a.mask == nullptr) {
+    const int seen = node - j + 1;   // tokens up to the node itself
+    return seen >= BLK ? 0xffffu : (seen > 0 ? (1u << seen) - 1u : 0u);
+  }
+  uint32_t x = 0u;
+  const int lo = max(j, 0);
+  if (j + BLK > 0 && lo < a.n) {
+    const uint64_t* const mw = a.mask + ((int64_t)b * a.n + node) * a.words;
+    uint64_t y = mw[lo >> 6] >> (lo & 63);
+    if ((lo & 63) + BLK > 64 && (lo >> 6) + 1 < a.words) y |= mw[(lo >> 6) + 1] << (64 - (lo & 63));
+    x = ((uint32_t)y & ((1u << min(a.n - lo, BLK)) - 1u)) << (lo - j);
+  }
+  if (j < 0) x |= (1u << min(-j, BLK)) - 1u;
+  return x & 0xffffu;
+}
+// ... with what the lane's row takes from them besides: the largest value norm, and no sum where one is not a number
+__device__ __forceinline__ uint32_t open_exact(TreeRows& w, const TreeArgs& a, int b, int first, const float* norms, uint32_t bad) {
+  const uint32_t bits = open_tokens(a, b, w.node, first);
+  for (int r = 0; r < BLK; ++r)
+    if (bits >> r & 1u) w.vmax = fmaxf(w.vmax, norms[r]);
+  if (bits & bad) w.sum = NAN;   // stays
+  return bits;
+}
+
+// Joins the halves of the rows.
+__device__ __forceinline__ void end_rows(TreeRows& w) {
+  w.sum = sum_x32(w.sum);
+  w.sealed = sum_x32(w.sealed);
+  w.ev = sum_x32(w.ev);
+  w.evmax = max_x32(w.evmax);
+  w.dmax = max_x32(w.dmax) * HALF_SCORE;
+  w.vmax = max_x32(w.vmax);
+}
+__device__ __forceinline__ void put_rows(const TreeRows& w, float* to) {
+  const int l = threadIdx.x & 63, row = l & 31, half = l >> 5;
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      // rows 8 r4 + 4 half + 0 .. 3 of the A operand: channels (r4 >> 1) 64 + ct 16 + (r4 & 1) 8 + half 4 + 0 .. 3
+      const int c = (r4 >> 1) * 16 + ct * 4 + (r4 & 1) * 2 + half;
+      reinterpret_cast<float4*>(to)[c * T_ROWS + row] = make_float4(w.o[ct][4 * r4], w.o[ct][4 * r4 + 1], w.o[ct][4 * r4 + 2], w.o[ct][4 * r4 + 3]);
+    }
+  if (half == 0) {
+    float* const st = to + T_OFLOATS + row;
+    st[T_M * T_ROWS] = w.m;
+    st[T_L * T_ROWS] = w.sum;
+    st[T_SEALED * T_ROWS] = w.sealed;
+    st[T_EV * T_ROWS] = w.ev;
+    st[T_EVMAX * T_ROWS] = w.evmax;
+    st[T_DMAX * T_ROWS] = w.dmax;
+    st[T_VMAX * T_ROWS] = w.vmax;
+  }
+}
+// Joins N sets, `stride` floats apart, into one by THREADS threads (whole groups of 32).
+template <int N, int THREADS>
+__device__ __forceinline__ void join_sets(const float* sets, int stride, float* to, int tid) {
+  const int row = tid & 31;
+  float f[N], M = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    f[i] = sets[i * stride + T_OFLOATS + T_M * T_ROWS + row];
+    M = fmaxf(M, f[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) f[i] = f[i] == M ? 1.0f : __builtin_amdgcn_exp2f(f[i] - M);
+  for (int c = tid >> 5; c < 32; c += THREADS / 32) {
+    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float4 y = reinterpret_cast<const float4*>(sets + i * stride)[c * T_ROWS + row];
+      x.x = fmaf(f[i], y.x, x.x), x.y = fmaf(f[i], y.y, x.y), x.z = fmaf(f[i], y.z, x.z), x.w = fmaf(f[i], y.w, x.w);
+    }
+    reinterpret_cast<float4*>(to)[c * T_ROWS + row] = x;
+  }
+  if (tid < 32) {
+    float L = 0.0f, SL = 0.0f, E = 0.0f, EM = 0.0f, DM = 0.0f, VM = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float* const st = sets + i * stride + T_OFLOATS + row;
+      L = fmaf(f[i], st[T_L * T_ROWS], L);
+      SL = fmaf(f[i], st[T_SEALED * T_ROWS], SL);
+      E = fmaf(f[i], st[T_EV * T_ROWS], E);
+      EM = fmaxf(EM, f[i] * st[T_EVMAX * T_ROWS]);
+      DM = fmaxf(DM, st[T_DMAX * T_ROWS]);
+      VM = fmaxf(VM, st[T_VMAX * T_ROWS]);
+    }
+    float* const st = to + T_OFLOATS + row;
+    st[T_M * T_ROWS] = M;
+    st[T_L * T_ROWS] = L;
+    st[T_SEALED * T_ROWS] = SL;
+    st[T_EV * T_ROWS] = E;
+    st[T_EVMAX * T_ROWS] = EM;
+    st[T_DMAX * T_ROWS] = DM;
+    st[T_VMAX * T_ROWS] = VM;
+  }
+}
+__device__ __forceinline__ float* set_of(const TreeArgs& a, int64_t head, int tile, int split) {
+  return a.part + ((head * a.row_tiles + tile) * a.nsplit + split) * T_FLOATS;
+}
+
+// ---- up to 32 rows: bound by the cache's bytes and their reconstruction ------------------------------------------------------------
+//
+// A wave takes pairs of blocks by itself and reconstructs them in registers, in the operands' layout: a 16-byte piece of key codes (16
+// channels of a token) is two operands' part of its lane, a dword of value codes (8 tokens of a channel) one.  Only the metadata, which 16
+// lanes share, goes through LDS, the wave's own part of it, so that no wave waits for another until the waves' sets are joined.
+constexpr int FEW_KM_HALF = 64 + 4, FEW_KM_KIND = 2 * FEW_KM_HALF, FEW_KM_BLK = 2 * FEW_KM_KIND + 8;   // floats; padded: the four
+constexpr int FEW_VM_BLK = VM_BYTES + 32, FEW_W_BLK = 2 * D + 16;                                      // addresses of a read in four sets of banks
+constexpr int FEW_KM = 0, FEW_VM = FEW_KM + 2 * FEW_KM_BLK * 4, FEW_W = FEW_VM + 2 * FEW_VM_BLK, FEW_META_END = FEW_W + 2 * FEW_W_BLK;
+constexpr int FEW_K = 0, FEW_V = FEW_K + 32 * D * 2, FEW_NORM = FEW_V + 32 * D * 2, FEW_BAD = FEW_NORM + 32 * 4, FEW_EXACT_END = FEW_BAD + 8;
+static_assert(FEW_META_END <= T_FLOATS * 4 && FEW_EXACT_END <= T_FLOATS * 4 && FEW_VM % 16 == 0 && FEW_W % 16 == 0, "a wave's part of LDS");
+
+__global__ __launch_bounds__(256, 2) void tree_few_kernel(TreeArgs a) {
+  __shared__ __align__(16) float s_set[4][T_FLOATS];
+  const int tid = threadIdx.x, l = tid & 63, n32 = l & 31, half = l >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t head = blockIdx.x;
+  const int split = blockIdx.y, tile = blockIdx.z;
+  const int b = (int)(head / a.n_kv), kvh = (int)(head - (int64_t)b * a.n_kv);
+  uint8_t* const mine = reinterpret_cast<uint8_t*>(s_set[w]);
+  TreeRows rows;
+
+  const uint8_t* const base = a.t1 + head * a.nq_cap * QUAD_BYTES;
+  const int units = (int)((a.nb + 1) >> 1);                 // pairs of sealed blocks
+  const int all = units + (a.trail + a.n + 31) / 32;        // ... and of 32 other tokens
+  const int step = 4 * a.nsplit;
+  const int bsel = (n32 >> 2) & 1, tok = (n32 >> 3) * 4 + (n32 & 3);   // the lane's token as a row of the keys' operand
+  uint4 kc[4], km[2], vc[2], vm;
+  float2 an;
+  // (behind the last pair: the head's first, which is not used)
+  const auto record = [&](int u) { return base + (int64_t)(u < units ? u >> 1 : 0) * QUAD_BYTES; };
+  const auto load_keys = [&](int u) {
+    const uint8_t* const r = record(u);
+    const int b0 = (u & 1) * 2;
+    const uint8_t* const p = r + Q_KC + (b0 + bsel) * KC_BYTES + half * 1024 + tok * 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) kc[i] = *reinterpret_cast<const uint4*>(p + i * 256);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) km[i] = reinterpret_cast<const uint4*>(r + Q_KM + (b0 + i) * KM_BYTES)[l];
+    an = reinterpret_cast<const float2*>(r + Q_AN)[b0 + half];
+  };
+  const auto load_values = [&](int u) {
+    const uint8_t* const r = record(u);
+    const int b0 = (u & 1) * 2;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) vc[i] = reinterpret_cast<const uint4*>(r + Q_VC + (b0 + half) * VC_BYTES + i * 512)[n32];
+    vm = reinterpret_cast<const uint4*>(r + Q_VM + b0 * VM_BYTES)[l];
+  };
+  int u = split * 4 + w;
+  load_keys(u);
+  load_values(u);
+  start_rows(rows, a, b, kvh, tile);
+
+  for (; u < all; u += step) {
+    const bool sealed = u < units;
+    f16x8 kf[8], vf[2][4];
+    uint32_t bits = 0xffffu;
+    bool masked = false;
+    float eta = 0.0f;
+    if (sealed) {
+      // metadata: sigma and z by (block, kind, half of the channels), scales and offsets by block
+      float* const skm = reinterpret_cast<float*>(mine + FEW_KM);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        *reinterpret_cast<uint4*>(skm + i * FEW_KM_BLK + half * FEW_KM_KIND + ((l >> 4) & 1) * FEW_KM_HALF + (l & 15) * 4) = km[i];
+      *reinterpret_cast<uint4*>(mine + FEW_VM + half * FEW_VM_BLK + n32 * 16) = vm;
+      wave_sync();
+      const float* const sg = skm + bsel * FEW_KM_BLK + half * FEW_KM_HALF;
+      const float* const zz = sg + FEW_KM_KIND;
 #pragma unroll
       for (int ks = 0; ks < 8; ++ks) {
-        const f16x8 k = __builtin_bit_cast(f16x8, s_k[(2 * ks + half) * TOK + (wt * MT + mt) * 32 + n32]);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s[mt][nt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qf[nt][ks], s[mt][nt], 0, 0, 0);
+        const float4 s0 = *reinterpret_cast<const float4*>(sg + ks * 8), s1 = *reinterpret_cast<const float4*>(sg + ks * 8 + 4);
+        const float4 z0 = *reinterpret_cast<const float4*>(zz + ks * 8), z1 = *reinterpret_cast<const float4*>(zz + ks * 8 + 4);
+        const uint32_t c0 = ks & 1 ? kc[ks >> 1].z : kc[ks >> 1].x, c1 = ks & 1 ? kc[ks >> 1].w : kc[ks >> 1].y;
+        kf[ks] = __builtin_bit_cast(f16x8, make_uint4(key2<0>(c0, s0.x, s0.y, z0.x, z0.y), key2<1>(c0, s0.z, s0.w, z0.z, z0.w),
+                                                      key2<0>(c1, s1.x, s1.y, z1.x, z1.y), key2<1>(c1, s1.z, s1.w, z1.z, z1.w)));
       }
+      // widths: four channels a lane
+      {
+        const int c = n32 * 4;
+        const float* const p = skm + half * FEW_KM_BLK + (c >> 6) * FEW_KM_HALF + (c & 63);
+        const float4 s4 = *reinterpret_cast<const float4*>(p), z4 = *reinterpret_cast<const float4*>(p + FEW_KM_KIND);
+        *reinterpret_cast<uint2*>(mine + FEW_W + half * FEW_W_BLK + c * 2) =
+            make_uint2(key_width(s4.x, z4.x) | key_width(s4.y, z4.y) << 16, key_width(s4.z, z4.z) | key_width(s4.w, z4.w) << 16);
+        wave_sync();
+      }
+      eta = value_error(an);
+      rows.vmax = fmaxf(rows.vmax, an.y);
+      masked = (int64_t)u * 2 + 2 > a.nb;
+      bits = (int64_t)u * 2 + half < a.nb ? 0xffffu : 0u;
+      load_keys(u + step);
+      bound_scores(rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(mine + FEW_W + bsel * FEW_W_BLK + half * 128 + ks * 16); });
+    } else {
+      const int t0 = (u - units) * 32;
+      if (u - step < units) rows.sealed = rows.sum;   // the wave's first of these
+      uint32_t* const bad = reinterpret_cast<uint32_t*>(mine + FEW_BAD);
+      if (l < 2) bad[l] = 0u;
+      wave_sync();
+      load_exact<64, 32>(a, head, t0, l, reinterpret_cast<uint4*>(mine + FEW_K), reinterpret_cast<uint4*>(mine + FEW_V),
+                         reinterpret_cast<float*>(mine + FEW_NORM), bad);
+      wave_sync();
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) kf[ks] = __builtin_bit_cast(f16x8, reinterpret_cast<const uint4*>(mine + FEW_K)[(half * 8 + ks) * 32 + n32]);
+      masked = true;
+      bits = open_exact(rows, a, b, t0 + half * BLK, reinterpret_cast<const float*>(mine + FEW_NORM) + half * BLK, bad[half]);
     }
-    uint32_t p[MT][NT][8];
+    if (sealed) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        if (masked) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[mt][nt][r] = bits[nt][mt] >> r & 1u ? s[mt][nt][r] : -INFINITY;
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[mt][nt][r]);
-      }
-      top = fmaxf(top, other_half(top)) * SCORE;
-      if (__any(top > m[nt])) {
-        const float mn = fmaxf(m[nt], top);
-        const float f = mn == m[nt] ? 1.0f : __builtin_amdgcn_exp2f(m[nt] - mn);
-        m[nt] = mn;
-        sum[nt] *= f;
-        ev[nt] *= f;
-        evmax[nt] *= f;
+      for (int oct = 0; oct < 2; ++oct) {
+        const uint8_t* const p = mine + FEW_VM + half * FEW_VM_BLK + oct * 128 + (n32 >> 4) * 64;
+        const uint32_t c[4] = {vc[oct].x, vc[oct].y, vc[oct].z, vc[oct].w};
 #pragma unroll
         for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[nt][ct][r] *= f;
+          vf[oct][ct] = __builtin_bit_cast(f16x8, values8(c[ct], reinterpret_cast<const uint4*>(p)[ct], reinterpret_cast<const uint4*>(p + 256)[ct]));
       }
-      const float base = m[nt] == -INFINITY ? 0.0f : m[nt];   // nothing attended yet: every weight is exp2(-inf) = 0
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        float bs = 0.0f;
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-          const float x = __builtin_amdgcn_exp2f(fmaf(s[mt][nt][r], SCORE, -base));
-          const float y = __builtin_amdgcn_exp2f(fmaf(s[mt][nt][r + 1], SCORE, -base));
-          bs += x + y;
-          p[mt][nt][r / 2] = pack_f16(x, y);
-        }
-        const float e = bs * s_eta[(wt * MT + mt) * 2 + half];
-        sum[nt] += bs;
-        ev[nt] += e;
-        evmax[nt] = fmaxf(evmax[nt], e);
-      }
-    }
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+      load_values(u + step);
+    } else {
 #pragma unroll
       for (int oct = 0; oct < 2; ++oct)
 #pragma unroll
-        for (int ct = 0; ct < 4; ++ct) {
-          const f16x8 v = __builtin_bit_cast(f16x8, s_v[(((wt * MT + mt) * 2 + half) * 2 + oct) * D + ct * 32 + n32]);
+        for (int ct = 0; ct < 4; ++ct)
+          vf[oct][ct] = __builtin_bit_cast(f16x8, reinterpret_cast<const uint4*>(mine + FEW_V)[(half * 2 + oct) * D + ct * 32 + n32]);
+    }
+    attend32(rows, masked, bits, eta, [&](int ks) { return kf[ks]; }, [&](int oct, int ct) { return vf[oct][ct]; });
+    wave_sync();
+  }
+  if (u - step < units) rows.sealed = rows.sum;   // no other tokens
+  end_rows(rows);
+  put_rows(rows, s_set[w]);
+  __syncthreads();
+  join_sets<4, 256>(s_set[0], T_FLOATS, set_of(a, head, tile, split), tid);
+}
+
+// ---- more rows: bound by the products -------------------------------------------------------------------------------------------------
+//
+// Eight waves, WR side by side over rows (32 each) and WT over tokens; four of them reconstruct the tile's keys and four its values
+// into LDS, a block each, for all.  Two tiles in LDS: the next one is written while the slower waves still read the last, one barrier a
+// tile; its codes are requested a tile ahead.
+template <int WR>
+struct ManyShape {
+  static constexpr int WT = 8 / WR;
+  static constexpr int MT = WR == 8 ? 2 : 1;      // times 32 tokens a wave takes of a tile
+  static constexpr int TOK = 32 * MT * WT;
+  static constexpr int QUADS = TOK / 64, BLKS = TOK / BLK;
+  static constexpr int TILE = 2 * TOK * D * 2;    // keys [16 runs][TOK], values [TOK / 8][128], 16 bytes each
+  // LDS: two tiles, the waves' metadata of a block (16 bytes more behind each 64 floats), the widths of 32 blocks while the next 32 come;
+  // at the end the waves' sets, where there are some to be joined
+  static constexpr int META = KM_BYTES + 3 * 16, META_AT = 2 * TILE, WIDTH_AT = META_AT + 8 * META, END = WIDTH_AT + 2 * 32 * D * 2;
+  static constexpr int BYTES = WT > 1 && 8 * T_FLOATS * 4 > END ? 8 * T_FLOATS * 4 : END;
+};
+
+template <int WR>
+__global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
+  using S = ManyShape<WR>;
+  constexpr int MT = S::MT, TOK = S::TOK, QUADS = S::QUADS, BLKS = S::BLKS;
+  __shared__ __align__(16) uint8_t s_main[S::BYTES];
+  __shared__ float s_eta[2][BLKS];
+  __shared__ float s_norm[TOK];
+  __shared__ uint32_t s_bad[BLKS];
+
+  const int tid = threadIdx.x, l = tid & 63, n32 = l & 31, half = l >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wr = w % WR, wt = w / WR, wb = w & 3;
+  const int64_t head = blockIdx.x;
+  const int split = blockIdx.y;
+  const int b = (int)(head / a.n_kv), kvh = (int)(head - (int64_t)b * a.n_kv);
+  const int tile0 = blockIdx.z * WR;
+  uint8_t* const s_meta = s_main + S::META_AT + w * S::META;
+  // [ring][run of 8 channels][block], 16 bytes
+  const auto width_at = [&](int ring, int run, int blk) { return s_main + S::WIDTH_AT + ((ring * (D / 8) + run) * 32 + blk) * 16; };
+  TreeRows rows;
+
+  const uint8_t* const base = a.t1 + head * a.nq_cap * QUAD_BYTES;
+  const int nquads = (int)((a.nb + 3) >> 2);
+  const int units = (nquads + QUADS - 1) / QUADS;
+  const int all = units + (a.trail + a.n + TOK - 1) / TOK;
+  const int step = a.nsplit;
+  // the wave's block of each quad of the tile: keys, lane (run pair c8, token t8) has 16 channels of tokens t8 and t8 + 8; values, lane (octet
+  // oc, n = gh 16 + n16) has four channels of eight tokens
+  const int t8 = l & 7, c8 = l >> 3;
+  uint4 raw[QUADS][3];
+  float2 an[QUADS];
+  float nu = 0.0f;
+  const auto load = [&](int u) {
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            const uint32_t* x = &p[mt][nt][4 * oct];
-            o[nt][ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, __builtin_bit_cast(f16x8, make_uint4(x[0], x[1], x[2], x[3])), o[nt][ct], 0, 0, 0);
-          }
-        }
-  };
-  // Delta of the 32 blocks whose widths are in LDS
-  const auto bound_scores = [&] {
-    if (wt != 0) return;
-    f32x16 d[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) d[nt][r] = 0.0f;
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) {
-      const f16x8 x = *reinterpret_cast<const f16x8*>(s_width[2 * ks + half][n32]);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        uint4 y = __builtin_bit_cast(uint4, qf[nt][ks]);
-        y.x &= 0x7fff7fffu, y.y &= 0x7fff7fffu, y.z &= 0x7fff7fffu, y.w &= 0x7fff7fffu;
-        d[nt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(f16x8, y), d[nt], 0, 0, 0);
+    for (int qd = 0; qd < QUADS; ++qd) {
+      int quad = u * QUADS + qd;
+      if (quad >= nquads) quad = 0;   // behind the last: any record of the head, its scores are masked
+      const uint8_t* const r = base + (int64_t)quad * QUAD_BYTES;
+      if (w < 4) {
+        const uint8_t* const p = r + Q_KC + wb * KC_BYTES + c8 * 256 + t8 * 16;
+        raw[qd][0] = *reinterpret_cast<const uint4*>(p);
+        raw[qd][1] = *reinterpret_cast<const uint4*>(p + 128);
+        raw[qd][2] = reinterpret_cast<const uint4*>(r + Q_KM + wb * KM_BYTES)[l];
+      } else {
+        raw[qd][0] = reinterpret_cast<const uint4*>(r + Q_VC + wb * VC_BYTES)[l];
+        const uint2 x = reinterpret_cast<const uint2*>(r + Q_VM + wb * VM_BYTES)[l];
+        raw[qd][2].x = x.x;
+        raw[qd][2].y = x.y;
+        an[qd] = reinterpret_cast<const float2*>(r + Q_AN)[wb];
       }
     }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) dmax[nt] = fmaxf(dmax[nt], d[nt][r]);
   };
-  // token t of block `blk` of the tile has this place among the keys: the A operand's rows, see attend
-  const auto place = [](int blk, int t) { return (blk >> 1) * 32 + (t >> 2) * 8 + (blk & 1) * 4 + (t & 3); };
+  int u = split;
+  load(u);
+  start_rows(rows, a, b, kvh, tile0 + wr);
+  for (int i = tid; i < 2 * 32 * D * 2 / 4; i += 512) reinterpret_cast<uint32_t*>(s_main + S::WIDTH_AT)[i] = 0u;
+  int fresh = 0, ring = 0;   // blocks whose widths have come into the half `ring`
+  int buf = 0;
+  __syncthreads();
 
-  const bool sealed = split < a.nsplit;
-  const int64_t nquads = (a.nb + 3) >> 2;
-  const int total = a.trail + a.n;   // of the other tokens: trailing ones, then drafted ones
-  // sealed tokens: tiles split, split + nsplit, ..., so that the workgroups of a head move through it side by side
-  const int64_t tiles = sealed ? (nquads + S::QUADS - 1) / S::QUADS : (total + TOK - 1) / TOK;
-  const int64_t step = sealed ? a.nsplit : 1;
-  int fresh = 0;   // blocks whose widths have come since bound_scores
-  if (sealed)
-    for (int i = tid; i < (int)sizeof(s_width) / 4; i += 256) reinterpret_cast<uint32_t*>(s_width)[i] = 0u;
-
-  for (int64_t tile = sealed ? split : 0; tile < tiles; tile += step) {
-    uint32_t bits[NT][MT];
-    bool masked;
-    __syncthreads();   // the last tile is done with
+  for (; u < all; u += step, buf ^= 1) {
+    const bool sealed = u < units;
+    uint4* const s_k = reinterpret_cast<uint4*>(s_main + buf * S::TILE);
+    uint4* const s_v = s_k + 16 * TOK;
     if (sealed) {
-      const uint8_t* const base = a.t1 + (int64_t)head * a.nq_cap * QUAD_BYTES;
 #pragma unroll
-      for (int qd = 0; qd < S::QUADS; ++qd) {
-        int64_t quad = tile * S::QUADS + qd;
-        if (quad >= nquads) quad = 0;   // behind the last: any record of the head, its scores are masked
-        const uint8_t* const rec = base + quad * QUAD_BYTES;
-        const int blk = qd * 4 + (tid >> 6);   // a wave: one block
-        {
-          // keys: lane (run pair c8, token t8) has 16 channels of tokens t8 and t8 + 8
-          const int t8 = tid & 7, c8 = (tid >> 3) & 7;
-          const uint8_t* const kc = rec + Q_KC + (tid >> 6) * KC_BYTES + (c8 >> 2) * 1024 + (c8 & 3) * 256;
-          const float* const km = reinterpret_cast<const float*>(rec + Q_KM + (tid >> 6) * KM_BYTES) + c8 * 16;
-          float sg[16], z[16];
+      for (int qd = 0; qd < QUADS; ++qd) {
+        const int blk = qd * 4 + wb;
+        float* const meta = reinterpret_cast<float*>(s_meta);
+        if (w < 4) {
+          *reinterpret_cast<uint4*>(meta + l * 4 + (l >> 4) * 4) = raw[qd][2];
+          wave_sync();
+          const float* const sg = meta + c8 * 16 + (c8 >> 2) * 4;
+          const float* const zz = sg + D + 8;
+          uint4 h[2][2];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            *reinterpret_cast<float4*>(&sg[4 * e]) = reinterpret_cast<const float4*>(km)[e];
-            *reinterpret_cast<float4*>(&z[4 * e]) = reinterpret_cast<const float4*>(km + D)[e];
-          }
+          for (int e = 0; e < 2; ++e) {
+            const float4 s0 = *reinterpret_cast<const float4*>(sg + e * 8), s1 = *reinterpret_cast<const float4*>(sg + e * 8 + 4);
+            const float4 z0 = *reinterpret_cast<const float4*>(zz + e * 8), z1 = *reinterpret_cast<const float4*>(zz + e * 8 + 4);
 #pragma unroll
-          for (int tt = 0; tt < 2; ++tt) {
-            const uint4 c4 = *reinterpret_cast<const uint4*>(kc + (t8 + 8 * tt) * 16);
-            const uint32_t c[4] = {c4.x, c4.y, c4.z, c4.w};
-            uint32_t h[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const uint32_t x = c[e >> 1] >> (16 * (e & 1));
-              h[e] = pack_f16(fmaf((float)(x & 255u) - 128.0f, sg[2 * e], z[2 * e]),
-                              fmaf((float)(x >> 8 & 255u) - 128.0f, sg[2 * e + 1], z[2 * e + 1]));
+            for (int tt = 0; tt < 2; ++tt) {
+              const uint32_t x0 = e ? raw[qd][tt].z : raw[qd][tt].x, x1 = e ? raw[qd][tt].w : raw[qd][tt].y;
+              h[tt][e] = make_uint4(key2<0>(x0, s0.x, s0.y, z0.x, z0.y), key2<1>(x0, s0.z, s0.w, z0.z, z0.w), key2<0>(x1, s1.x, s1.y, z1.x, z1.y),
+                                    key2<1>(x1, s1.z, s1.w, z1.z, z1.w));
             }
-            const int at = place(blk, t8 + 8 * tt);
-            s_k[(2 * c8) * TOK + at] = make_uint4(h[0], h[1], h[2], h[3]);
-            s_k[(2 * c8 + 1) * TOK + at] = make_uint4(h[4], h[5], h[6], h[7]);
           }
+#pragma unroll
+          for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) s_k[(2 * c8 + e) * TOK + key_place(blk, t8 + 8 * tt)] = h[tt][e];
           // widths: two channels a lane
           const int ch = c8 * 16 + 2 * t8;
-          const float2 s2 = *reinterpret_cast<const float2*>(km + 2 * t8), z2 = *reinterpret_cast<const float2*>(km + D + 2 * t8);
-          const uint32_t w2 = key_width(s2.x, z2.x) | (uint32_t)key_width(s2.y, z2.y) << 16;
-          *reinterpret_cast<uint32_t*>(&s_width[ch >> 3][fresh + blk][ch & 7]) = w2;
-        }
-        {
-          // values: lane (octet oc, group set gh, channel n) has four channels of eight tokens, one dword each
-          const int n16 = tid & 15, gh = (tid >> 4) & 1, oc = (tid >> 5) & 1;
-          const uint4 c4 = reinterpret_cast<const uint4*>(rec + Q_VC)[tid];
-          const uint32_t c[4] = {c4.x, c4.y, c4.z, c4.w};
-          const uint8_t* const vm = rec + Q_VM + (tid >> 6) * VM_BYTES + oc * 128 + gh * 64;
+          const float2 s2 = *reinterpret_cast<const float2*>(sg + 2 * t8), z2 = *reinterpret_cast<const float2*>(zz + 2 * t8);
+          *reinterpret_cast<uint32_t*>(width_at(ring, ch >> 3, fresh + blk) + (ch & 7) * 2) = key_width(s2.x, z2.x) | key_width(s2.y, z2.y) << 16;
+        } else {
+          reinterpret_cast<uint2*>(meta)[l] = make_uint2(raw[qd][2].x, raw[qd][2].y);
+          wave_sync();
+          const int oc = l >> 5, gh = (l >> 4) & 1, n16 = l & 15;
+          const uint8_t* const p = s_meta + oc * 128 + gh * 64;
+          const uint32_t c[4] = {raw[qd][0].x, raw[qd][0].y, raw[qd][0].z, raw[qd][0].w};
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const uint4 sc = reinterpret_cast<const uint4*>(vm)[g], of = reinterpret_cast<const uint4*>(vm + 256)[g];
-            const uint32_t d = c[g];
-            // codes of tokens (2 i, 2 i + 1) as FP16 integers: dropped into the mantissa of 1024, which leaves exactly
-            const auto codes = [&](int i) {
-              const uint32_t x = d >> (8 * i);
-              const uint32_t pair = (x & 0xfu) | (x << 12 & 0xf0000u) | 0x64006400u;
-              return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, pair) - __builtin_bit_cast(f16x2, 0x64006400u));
-            };
-            s_v[((tid >> 6) + qd * 4) * 2 * D + oc * D + (gh * 4 + g) * 16 + n16] =
-                make_uint4(value2(codes(0), sc.x, of.x), value2(codes(1), sc.y, of.y), value2(codes(2), sc.z, of.z), value2(codes(3), sc.w, of.w));
-          }
+          for (int g = 0; g < 4; ++g)
+            s_v[value_place(blk * 2 + oc, (gh * 4 + g) * 16 + n16)] = values8(c[g], reinterpret_cast<const uint4*>(p)[g], reinterpret_cast<const uint4*>(p + 256)[g]);
+          if (l == 0) s_eta[buf][blk] = value_error(an[qd]);
+          nu = fmaxf(nu, an[qd].y);
         }
-        if (tid < 4) {
-          const float2 an = reinterpret_cast<const float2*>(rec + Q_AN)[tid];   // eta, nu; zeros where not sealed
-          s_eta[qd * 4 + tid] = an.x + fminf(an.x, fmaf(an.y + an.x, 0x1p-11f, 0x1p-21f));
-          nu = fmaxf(nu, an.y);
-        }
+        wave_sync();
       }
+      load(u + step < units ? u + step : 0);
       fresh += BLKS;
-      const int64_t left = a.nb - tile * BLKS;   // sealed blocks from the tile's first on
-      masked = left < BLKS;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) bits[nt][mt] = (wt * MT + mt) * 2 + half < left ? 0xffffu : 0u;
-      __syncthreads();
     } else {
-      const int t0 = (int)tile * TOK;
-      masked = true;
+      if (u - step < units) rows.sealed = rows.sum;   // the workgroup's first of these
+      __syncthreads();   // norms and bad tokens of the last tile are done with
       if (tid < BLKS) {
-        s_eta[tid] = 0.0f;   // exact tokens
         s_bad[tid] = 0u;
+        s_eta[buf][tid] = 0.0f;
       }
       __syncthreads();
-      // a wave takes a token at a time: 2 channels a lane; rows behind the last token are zeros
-      for (int t = w; t < TOK; t += 4) {
-        const int i = t0 + t;
-        uint32_t k2 = 0u, v2 = 0u;
-        if (i < total) {
-          const bool old = i < a.trail;
-          k2 = ld4_any((old ? a.trail_k + ((int64_t)head * BLK + i) * D : a.kd + ((int64_t)head * a.n + i - a.trail) * D) + 2 * l);
-          v2 = ld4_any((old ? a.trail_v + ((int64_t)head * BLK + i) * D : a.vd + ((int64_t)head * a.n + i - a.trail) * D) + 2 * l);
-        }
-        const f16x2 k = __builtin_bit_cast(f16x2, k2), v = __builtin_bit_cast(f16x2, v2);
-        const float x = (float)v[0], y = (float)v[1];
-        // A number that is not finite must not meet the zero weight of a row that does not attend its token: the token is
-        // taken out, and the rows that do attend it get a sum that is no number.
-        const bool bad = __any(!(fabsf(x) <= F16_MAX && fabsf(y) <= F16_MAX && fabsf((float)k[0]) <= F16_MAX && fabsf((float)k[1]) <= F16_MAX));
-        float sq = fmaf(x, x, y * y);
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) sq += __shfl_xor(sq, d);
-        if (l == 0) {
-          s_norm[t] = sqrtf(sq);
-          if (bad) atomicOr(&s_bad[t / BLK], 1u << (t % BLK));
-        }
-        if (bad) k2 = v2 = 0u;
-        reinterpret_cast<uint32_t*>(s_k)[((l >> 2) * TOK + place(t / BLK, t % BLK)) * 4 + (l & 3)] = k2;
-        uint16_t* const vh = reinterpret_cast<uint16_t*>(s_v);
-        vh[((t >> 3) * D + 2 * l) * 8 + (t & 7)] = (uint16_t)v2;
-        vh[((t >> 3) * D + 2 * l + 1) * 8 + (t & 7)] = (uint16_t)(v2 >> 16);
-      }
-      __syncthreads();
-      // a row's open tokens among the 16 of the lane's block
-      const auto open = [&](int nt, int mt) -> uint32_t {
-        const int j = t0 + ((wt * MT + mt) * 2 + half) * BLK - a.trail;   // drafted node of the block's first token; below 0: trailing ones
-        uint32_t x = 0u;
-        if (a.mask == nullptr) {
-          const int seen = node[nt] - j + 1;   // tokens up to the node itself
-          return seen >= BLK ? 0xffffu : (seen > 0 ? (1u << seen) - 1u : 0u);
-        }
-        const int lo = max(j, 0);
-        if (j + BLK > 0 && lo < a.n) {
-          const uint64_t* const mw = a.mask + ((int64_t)b * a.n + node[nt]) * a.words;
-          uint64_t y = mw[lo >> 6] >> (lo & 63);
-          if ((lo & 63) + BLK > 64 && (lo >> 6) + 1 < a.words) y |= mw[(lo >> 6) + 1] << (64 - (lo & 63));
-          x = ((uint32_t)y & ((1u << min(a.n - lo, BLK)) - 1u)) << (lo - j);
-        }
-        if (j < 0) x |= (1u << min(-j, BLK)) - 1u;
-        return x & 0xffffu;
-      };
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          const int blk = (wt * MT + mt) * 2 + half;
-          bits[nt][mt] = open(nt, mt);
-          for (int r = 0; r < BLK; ++r)
-            if (bits[nt][mt] >> r & 1u) vmax[nt] = fmaxf(vmax[nt], s_norm[blk * BLK + r]);
-          if (bits[nt][mt] & s_bad[blk]) sum[nt] = NAN;   // stays
-        }
+      load_exact<512, TOK>(a, head, (u - units) * TOK, tid, s_k, s_v, s_norm, s_bad);
     }
-    attend(masked, bits);
-    if (sealed && (fresh == 32 || tile + step >= tiles)) {
-      bound_scores();
-      fresh = 0;
-    }
-  }
-  if (sealed) {
-    if (tid < 4) s_norm[tid] = nu;
     __syncthreads();
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) vmax[nt] = fmaxf(fmaxf(s_norm[0], s_norm[1]), fmaxf(s_norm[2], s_norm[3]));
-  }
-
-  // the halves of a row have the tokens of different blocks
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    sum[nt] += other_half(sum[nt]);
-    ev[nt] += other_half(ev[nt]);
-    evmax[nt] = fmaxf(evmax[nt], other_half(evmax[nt]));
-    dmax[nt] = fmaxf(dmax[nt], other_half(dmax[nt])) * (0.5f * 0.08838834764831845f);
-    vmax[nt] = fmaxf(vmax[nt], other_half(vmax[nt]));
-  }
-  const auto put = [&](float* to, int nt) {
-#pragma unroll
-    for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4)   // channels ct * 32 + r4 * 8 + half * 4 + 0 .. 3
-        reinterpret_cast<float4*>(to)[(ct * 8 + r4 * 2 + half) * T_ROWS + n32] =
-            make_float4(o[nt][ct][4 * r4], o[nt][ct][4 * r4 + 1], o[nt][ct][4 * r4 + 2], o[nt][ct][4 * r4 + 3]);
-    if (half == 0) {
-      float* const st = to + T_OFLOATS + n32;
-      st[T_M * T_ROWS] = m[nt];
-      st[T_L * T_ROWS] = sum[nt];
-      st[T_EV * T_ROWS] = ev[nt];
-      st[T_EVMAX * T_ROWS] = evmax[nt];
-      st[T_DMAX * T_ROWS] = dmax[nt];
-      st[T_VMAX * T_ROWS] = vmax[nt];
+    for (int mt = 0; mt < MT; ++mt) {
+      const int unit = wt * MT + mt, blk = unit * 2 + half;   // 32 tokens; the lane's block
+      uint32_t bits;
+      if (sealed)
+        bits = (int64_t)u * BLKS + blk < a.nb ? 0xffffu : 0u;
+      else
+        bits = open_exact(rows, a, b, (u - units) * TOK + blk * BLK, s_norm + blk * BLK, s_bad[blk]);
+      attend32(
+          rows, !sealed || (int64_t)(u + 1) * BLKS > a.nb, bits, s_eta[buf][blk],
+          [&](int ks) { return __builtin_bit_cast(f16x8, s_k[(half * 8 + ks) * TOK + unit * 32 + n32]); },
+          [&](int oct, int ct) { return __builtin_bit_cast(f16x8, s_v[(blk * 2 + oct) * D + ct * 32 + n32]); });
     }
-  };
-  const auto set_of = [&](int tile) { return a.part + (((int64_t)head * a.row_tiles + tile) * (a.nsplit + 1) + split) * T_FLOATS; };
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    if constexpr (WT == 1) {
-      if (tile0 + nt < a.row_tiles) put(set_of(tile0 + nt), nt);
-    } else {
-      // the token waves' sets are joined through LDS
-      float* const sets = reinterpret_cast<float*>(s_main);
-      __syncthreads();
-      put(sets + w * T_FLOATS, nt);
-      __syncthreads();
-      constexpr int PER = 256 / WR;   // threads a joined set
-      const int mine = tid / PER, lane = tid % PER;
-      const int tile = blockIdx.z * (NT * WR) + mine * NT + nt;
-      if (tile < a.row_tiles) {
-        float* const to = set_of(tile);
-        const int row = lane & 31;
-        float f[WT], M = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < WT; ++i) {
-          f[i] = sets[(i * WR + mine) * T_FLOATS + T_OFLOATS + T_M * T_ROWS + row];
-          M = fmaxf(M, f[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < WT; ++i) f[i] = f[i] == M ? 1.0f : __builtin_amdgcn_exp2f(f[i] - M);
-        for (int c = lane >> 5; c < 32; c += PER / 32) {
-          float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-          for (int i = 0; i < WT; ++i) {
-            const float4 y = reinterpret_cast<const float4*>(sets + (i * WR + mine) * T_FLOATS)[c * T_ROWS + row];
-            x.x = fmaf(f[i], y.x, x.x), x.y = fmaf(f[i], y.y, x.y), x.z = fmaf(f[i], y.z, x.z), x.w = fmaf(f[i], y.w, x.w);
-          }
-          reinterpret_cast<float4*>(to)[c * T_ROWS + row] = x;
-        }
-        if (lane < 32) {
-          float L = 0.0f, E = 0.0f, EM = 0.0f, DM = 0.0f, VM = 0.0f;
-#pragma unroll
-          for (int i = 0; i < WT; ++i) {
-            const float* const st = sets + (i * WR + mine) * T_FLOATS + T_OFLOATS + row;
-            L = fmaf(f[i], st[T_L * T_ROWS], L);
-            E = fmaf(f[i], st[T_EV * T_ROWS], E);
-            EM = fmaxf(EM, f[i] * st[T_EVMAX * T_ROWS]);
-            DM = fmaxf(DM, st[T_DMAX * T_ROWS]);
-            VM = fmaxf(VM, st[T_VMAX * T_ROWS]);
-          }
-          float* const st = to + T_OFLOATS + row;
-          st[T_M * T_ROWS] = M;
-          st[T_L * T_ROWS] = L;
-          st[T_EV * T_ROWS] = E;
-          st[T_EVMAX * T_ROWS] = EM;
-          st[T_DMAX * T_ROWS] = DM;
-          st[T_VMAX * T_ROWS] = VM;
-        }
-      }
+    if (sealed && (fresh == 32 || u + step >= units)) {
+      if (wt == 0) bound_scores(rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(width_at(ring, half * 8 + ks, n32)); });
+      fresh = 0;
+      ring ^= 1;
     }
+  }
+  if (u - step < units) rows.sealed = rows.sum;   // no other tokens
+  __syncthreads();
+  if (w >= 4 && l == 0) s_norm[w - 4] = nu;
+  __syncthreads();
+  rows.vmax = fmaxf(rows.vmax, fmaxf(fmaxf(s_norm[0], s_norm[1]), fmaxf(s_norm[2], s_norm[3])));
+  end_rows(rows);
+  if constexpr (S::WT == 1) {
+    if (tile0 + wr < a.row_tiles) put_rows(rows, set_of(a, head, tile0 + wr, split));
+  } else {
+    // the token waves' sets are joined through LDS
+    float* const sets = reinterpret_cast<float*>(s_main);
+    put_rows(rows, sets + w * T_FLOATS);
+    __syncthreads();
+    constexpr int PER = 512 / WR;   // threads a joined set: set i of row wave r is that of wave i * WR + r
+    const int r = tid / PER;
+    if (tile0 + r < a.row_tiles) join_sets<S::WT, PER>(sets + r * T_FLOATS, WR * T_FLOATS, set_of(a, head, tile0 + r, split), tid % PER);
   }
 }
 
@@ -501,22 +683,22 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeJoinArgs a) {
   const int row = threadIdx.x & 7, c = threadIdx.x >> 3;
   const int head = blockIdx.x, tile = blockIdx.y >> 2, r32 = (blockIdx.y & 3) * 8 + row;
   const int r = tile * 32 + r32;
-  const float* const sets = a.part + ((int64_t)head * a.row_tiles + tile) * (a.nsplit + 1) * T_FLOATS;
+  const float* const sets = a.part + ((int64_t)head * a.row_tiles + tile) * a.nsplit * T_FLOATS;
   __shared__ uint32_t s_bad[8];
   if (threadIdx.x < 8) s_bad[threadIdx.x] = 0u;
   __syncthreads();
   float M = -INFINITY;
-  for (int i = 0; i <= a.nsplit; ++i) M = fmaxf(M, sets[i * T_FLOATS + T_OFLOATS + T_M * T_ROWS + r32]);
+  for (int i = 0; i < a.nsplit; ++i) M = fmaxf(M, sets[i * T_FLOATS + T_OFLOATS + T_M * T_ROWS + r32]);
   float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   float L = 0.0f, sealed = 0.0f, E = 0.0f, EM = 0.0f, DM = 0.0f, VM = 0.0f;
-  for (int i = 0; i <= a.nsplit; ++i) {
+  for (int i = 0; i < a.nsplit; ++i) {
     const float* const st = sets + i * T_FLOATS + T_OFLOATS + r32;
     const float mi = st[T_M * T_ROWS];
     const float f = mi == M ? 1.0f : __builtin_amdgcn_exp2f(mi - M);
     const float4 y = reinterpret_cast<const float4*>(sets + i * T_FLOATS)[c * T_ROWS + r32];
     x.x = fmaf(f, y.x, x.x), x.y = fmaf(f, y.y, x.y), x.z = fmaf(f, y.z, x.z), x.w = fmaf(f, y.w, x.w);
     L = fmaf(f, st[T_L * T_ROWS], L);
-    if (i < a.nsplit) sealed = L;
+    sealed = fmaf(f, st[T_SEALED * T_ROWS], sealed);
     E = fmaf(f, st[T_EV * T_ROWS], E);
     EM = fmaxf(EM, f * st[T_EVMAX * T_ROWS]);
     DM = fmaxf(DM, st[T_DMAX * T_ROWS]);
@@ -562,29 +744,27 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeJoinArgs a) {
 
 // ---- host --------------------------------------------------------------------------------------------------------------------------
 
-// Rows of a KV group a workgroup takes: few rows spare the accumulators, and the waves share the tokens instead.
+// Rows of a KV group a workgroup takes.
 static int tree_rows(int n_rows) { return n_rows <= 32 ? 32 : (n_rows <= 64 ? 64 : (n_rows <= 128 ? 128 : 256)); }
 
-// Partial sets of the sealed blocks: as many workgroups as the device holds at a time.
-static int tree_splits(int n_cu, int64_t heads, int n_rows, int64_t nb) {
+// Partial sets: as many workgroups as the device holds at a time, each with something to do at the cache's full length.
+static int tree_splits(int n_cu, int64_t heads, int n_rows, int n_draft, int64_t tokens) {
   const int rows = tree_rows(n_rows);
   const int64_t z = (n_rows + rows - 1) / rows;
-  const int64_t most = std::max<int64_t>(1, (rows <= 64 ? 2 : 1) * (int64_t)n_cu / (heads * z));
-  const int64_t quads = (nb + 3) / 4;
-  const int64_t tiles = rows == 32 ? (quads + 1) / 2 : quads;
-  return (int)std::min(most, tiles);
+  const int64_t most = std::max<int64_t>(1, (rows == 32 ? 2 : 1) * (int64_t)n_cu / (heads * z));
+  const int64_t tok = rows == 32 || rows == 64 ? 128 : 64;   // of a workgroup's tile, or of its four waves' units
+  return (int)std::min(most, (tokens + n_draft + tok - 1) / tok);
 }
 
 int64_t tree_ws_bytes(const Cache* c, int n_draft) {
   const int64_t heads = (int64_t)c->desc.batch * c->desc.n_kv_heads;
   const int n_rows = n_draft * (c->desc.n_q_heads / c->desc.n_kv_heads);
-  return heads * ((n_rows + 31) / 32) * (tree_splits(c->n_cu, heads, n_rows, c->nb_cap) + 1) * T_FLOATS * 4;
+  return heads * ((n_rows + 31) / 32) * tree_splits(c->n_cu, heads, n_rows, n_draft, c->desc.max_tokens) * T_FLOATS * 4;
 }
 
-template <int NT, int WR, int WT>
-static void launch_tree_shape(const TreeArgs& a, int64_t heads, hipStream_t st) {
-  const uint32_t z = (uint32_t)((a.row_tiles + NT * WR - 1) / (NT * WR));
-  tree_split_kernel<NT, WR, WT><<<dim3((uint32_t)heads, (uint32_t)a.nsplit + 1, z), 256, 0, st>>>(a);
+template <int WR>
+static void launch_many(const TreeArgs& a, int64_t heads, hipStream_t st) {
+  tree_many_kernel<WR><<<dim3((uint32_t)heads, (uint32_t)a.nsplit, (uint32_t)((a.row_tiles + WR - 1) / WR)), 512, 0, st>>>(a);
 }
 
 int32_t launch_tree(const Cache* c, int layer, const __half* q, const __half* kd, const __half* vd, int n_draft, const uint64_t* mask,
@@ -609,12 +789,12 @@ int32_t launch_tree(const Cache* c, int layer, const __half* q, const __half* kd
   a.group = c->desc.n_q_heads / c->desc.n_kv_heads;
   const int n_rows = n_draft * a.group;
   a.row_tiles = (n_rows + 31) / 32;
-  a.nsplit = tree_splits(c->n_cu, heads, n_rows, a.nb);
+  a.nsplit = tree_splits(c->n_cu, heads, n_rows, n_draft, c->length[layer]);
   switch (tree_rows(n_rows)) {
-    case 32: launch_tree_shape<1, 1, 4>(a, heads, st); break;
-    case 64: launch_tree_shape<1, 2, 2>(a, heads, st); break;
-    case 128: launch_tree_shape<2, 2, 2>(a, heads, st); break;
-    default: launch_tree_shape<2, 4, 1>(a, heads, st); break;
+    case 32: tree_few_kernel<<<dim3((uint32_t)heads, (uint32_t)a.nsplit, 1), 256, 0, st>>>(a); break;
+    case 64: launch_many<2>(a, heads, st); break;
+    case 128: launch_many<4>(a, heads, st); break;
+    default: launch_many<8>(a, heads, st); break;
   }
   CQA_HIP(hipGetLastError());
   TreeJoinArgs j;
