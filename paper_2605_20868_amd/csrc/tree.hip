@@ -120,15 +120,16 @@ __device__ __forceinline__ void start_rows(TreeRows& s, const TreeArgs& a, int b
     for (int r = 0; r < 16; ++r) s.o[ct][r] = 0.0f;
 }
 
-// Scores, softmax and values of 32 tokens.  key(ks), value(oct, ct): the A operands of the two products; bits, where masked: the tokens
-// of the lane's block that its row attends.
-template <typename Key, typename Value>
-__device__ __forceinline__ void attend32(TreeRows& w, bool masked, uint32_t bits, float eta, Key key, Value value) {
+// Scores, softmax and values of 32 tokens.  key(ks), value(oct, ct): the A operands of the two products; between(): what is to be done
+// once the keys are; bits, where masked: the tokens of the lane's block that its row attends.
+template <typename Key, typename Between, typename Value>
+__device__ __forceinline__ void attend32(TreeRows& w, bool masked, uint32_t bits, float eta, Key key, Between between, Value value) {
   f32x16 s;
 #pragma unroll
   for (int r = 0; r < 16; ++r) s[r] = 0.0f;
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(key(ks), w.q[ks], s, 0, 0, 0);
+  between();
   if (masked) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = bits >> r & 1u ? s[r] : -INFINITY;
@@ -194,24 +195,35 @@ __device__ __forceinline__ int key_place(int blk, int t) { return (blk >> 1) * 3
 __device__ __forceinline__ int value_place(int oct, int c) { return oct * D + ((c >> 4) & 3) * 32 + (c >> 6) * 16 + (c & 15); }
 
 // Trailing and drafted tokens t0 .. t0 + TOK - 1 (of trail + n; zeros behind the last) by THREADS threads, thread `tid`.
-//   keys [16 runs of 8 channels][TOK], values [TOK / 8][128] by value_place, norms [TOK], bad: a bit per token, per block (zero before)
-// A number that is not finite must not meet the zero weight of a row that does not attend its token: the token is taken out, and the
-// rows that do attend it get a sum that is no number.
+//   keys [16 runs of 8 channels][TOK], values [TOK / 8][128] by value_place, norms [TOK], bad [TOK]: 1 for a token with a number that
+//   is not finite (zeros before)
+// Such a number must not meet the zero weight of a row that does not attend its token: it is taken out, and the rows that do attend
+// the token get a sum that is no number.
 template <int THREADS, int TOK>
-__device__ __forceinline__ void load_exact(const TreeArgs& a, int64_t head, int t0, int tid, uint4* keys, uint4* values, float* norms, uint32_t* bad) {
+__device__ __forceinline__ void load_exact(const TreeArgs& a, int64_t head, int t0, int tid, uint4* keys, uint4* values, float* norms, uint8_t* bad) {
   const int total = a.trail + a.n;
-  const auto finite = [](uint32_t x) { return (x & 0x7c00u) != 0x7c00u && (x & 0x7c000000u) != 0x7c000000u; };
+  const auto finite = [](uint32_t x) { return (uint32_t)((x & 0x7c00u) != 0x7c00u) & (uint32_t)((x & 0x7c000000u) != 0x7c000000u); };
+  // (every address is a token's: the requests stand in no branch)
+  const auto token = [&](const __half* trail, const __half* drafts, int pos) {
+    pos = min(pos, total - 1);
+    return pos < a.trail ? trail + (head * BLK + pos) * D : drafts + (head * a.n + pos - a.trail) * D;
+  };
+  constexpr int NK = TOK * 16 / THREADS;
+  uint4 kx[NK];
 #pragma unroll
-  for (int k = 0; k < TOK * 16 / THREADS; ++k) {
-    const int i = tid + k * THREADS, t = i >> 4, run = i & 15, pos = t0 + t;
-    uint4 x = make_uint4(0u, 0u, 0u, 0u);
-    if (pos < total)
-      x = ld16_any((pos < a.trail ? a.trail_k + (head * BLK + pos) * D : a.kd + (head * a.n + pos - a.trail) * D) + run * 8);
-    if (!(finite(x.x) && finite(x.y) && finite(x.z) && finite(x.w))) {
-      atomicOr(&bad[t / BLK], 1u << (t % BLK));
-      x = make_uint4(0u, 0u, 0u, 0u);   // (its other runs are numbers)
-    }
-    keys[run * TOK + key_place(t / BLK, t % BLK)] = x;
+  for (int k = 0; k < NK; ++k) {
+    const int i = tid + k * THREADS;
+    kx[k] = ld16_any(token(a.trail_k, a.kd, t0 + (i >> 4)) + (i & 15) * 8);
+  }
+#pragma unroll
+  for (int k = 0; k < NK; ++k) {
+    const int i = tid + k * THREADS, t = i >> 4;
+    uint4 x = kx[k];
+    const uint32_t ok = finite(x.x) & finite(x.y) & finite(x.z) & finite(x.w), there = t0 + t < total;
+    if (there & (ok ^ 1u)) bad[t] = 1;
+    const uint32_t keep = 0u - (there & ok);
+    x.x &= keep, x.y &= keep, x.z &= keep, x.w &= keep;
+    keys[(i & 15) * TOK + key_place(t / BLK, t % BLK)] = x;
   }
   // four channels of eight tokens
 #pragma unroll
@@ -219,32 +231,26 @@ __device__ __forceinline__ void load_exact(const TreeArgs& a, int64_t head, int 
     const int i = tid + k * THREADS, oct = i >> 5, c = (i & 31) * 4;
     if (THREADS > TOK * 4 && i >= TOK * 4) break;   // (whole waves)
     uint32_t x[8][2];
-    float sq[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int pos = t0 + oct * 8 + j;
-      x[j][0] = x[j][1] = 0u;
-      if (pos < total) {
-        const __half* p = (pos < a.trail ? a.trail_v + (head * BLK + pos) * D : a.vd + (head * a.n + pos - a.trail) * D) + c;
-        x[j][0] = ld4_any(p);
-        x[j][1] = ld4_any(p + 2);
-      }
+      const __half* const p = token(a.trail_v, a.vd, t0 + oct * 8 + j) + c;
+      x[j][0] = ld4_any(p);
+      x[j][1] = ld4_any(p + 2);
     }
+    float norm2 = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
+      const int t = oct * 8 + j;
       const f16x2 u = __builtin_bit_cast(f16x2, x[j][0]), v = __builtin_bit_cast(f16x2, x[j][1]);
-      sq[j] = fmaf((float)u[0], (float)u[0], fmaf((float)u[1], (float)u[1], fmaf((float)v[0], (float)v[0], (float)v[1] * (float)v[1])));
-      if (!(finite(x[j][0]) && finite(x[j][1]))) {
-        const int t = oct * 8 + j;
-        atomicOr(&bad[t / BLK], 1u << (t % BLK));
-        x[j][0] = x[j][1] = 0u;
-      }
+      float sq = fmaf((float)u[0], (float)u[0], fmaf((float)u[1], (float)u[1], fmaf((float)v[0], (float)v[0], (float)v[1] * (float)v[1])));
+      sq = sum_x16(row_sum(sq));   // the 32 lanes that have the token
+      norm2 = (i & 31) == j ? sq : norm2;
+      const uint32_t ok = finite(x[j][0]) & finite(x[j][1]), there = t0 + t < total;
+      if (there & (ok ^ 1u)) bad[t] = 1;
+      x[j][0] &= 0u - (there & ok);
+      x[j][1] &= 0u - (there & ok);
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      sq[j] = sum_x16(row_sum(sq[j]));   // the 32 lanes that have the token
-      if ((i & 31) == j) norms[oct * 8 + j] = sqrtf(sq[j]);
-    }
+    if ((i & 31) < 8) norms[oct * 8 + (i & 31)] = sqrtf(norm2);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       uint32_t h[4];
@@ -274,11 +280,17 @@ __device__ __forceinline__ uint32_t open_tokens(const TreeArgs& a, int b, int no
   return x & 0xffffu;
 }
 // ... with what the lane's row takes from them besides: the largest value norm, and no sum where one is not a number
-__device__ __forceinline__ uint32_t open_exact(TreeRows& w, const TreeArgs& a, int b, int first, const float* norms, uint32_t bad) {
+__device__ __forceinline__ uint32_t open_exact(TreeRows& w, const TreeArgs& a, int b, int first, const float* norms, const uint8_t* bad) {
   const uint32_t bits = open_tokens(a, b, w.node, first);
-  for (int r = 0; r < BLK; ++r)
-    if (bits >> r & 1u) w.vmax = fmaxf(w.vmax, norms[r]);
-  if (bits & bad) w.sum = NAN;   // stays
+  uint32_t hit = 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    hit |= (reinterpret_cast<const uint32_t*>(bad)[i] * 0x10204080u >> 28) << (4 * i);   // a bit per byte
+    const float4 x = reinterpret_cast<const float4*>(norms)[i];
+    w.vmax = fmaxf(w.vmax, fmaxf(fmaxf(bits >> (4 * i) & 1u ? x.x : 0.0f, bits >> (4 * i + 1) & 1u ? x.y : 0.0f),
+                                 fmaxf(bits >> (4 * i + 2) & 1u ? x.z : 0.0f, bits >> (4 * i + 3) & 1u ? x.w : 0.0f)));
+  }
+  if (bits & hit) w.sum = NAN;   // stays
   return bits;
 }
 
@@ -367,7 +379,7 @@ __device__ __forceinline__ float* set_of(const TreeArgs& a, int64_t head, int ti
 constexpr int FEW_KM_HALF = 64 + 4, FEW_KM_KIND = 2 * FEW_KM_HALF, FEW_KM_BLK = 2 * FEW_KM_KIND + 8;   // floats; padded: the four
 constexpr int FEW_VM_BLK = VM_BYTES + 32, FEW_W_BLK = 2 * D + 16;                                      // addresses of a read in four sets of banks
 constexpr int FEW_KM = 0, FEW_VM = FEW_KM + 2 * FEW_KM_BLK * 4, FEW_W = FEW_VM + 2 * FEW_VM_BLK, FEW_META_END = FEW_W + 2 * FEW_W_BLK;
-constexpr int FEW_K = 0, FEW_V = FEW_K + 32 * D * 2, FEW_NORM = FEW_V + 32 * D * 2, FEW_BAD = FEW_NORM + 32 * 4, FEW_EXACT_END = FEW_BAD + 8;
+constexpr int FEW_K = 0, FEW_V = FEW_K + 32 * D * 2, FEW_NORM = FEW_V + 32 * D * 2, FEW_BAD = FEW_NORM + 32 * 4, FEW_EXACT_END = FEW_BAD + 32;
 static_assert(FEW_META_END <= T_FLOATS * 4 && FEW_EXACT_END <= T_FLOATS * 4 && FEW_VM % 16 == 0 && FEW_W % 16 == 0, "a wave's part of LDS");
 
 __global__ __launch_bounds__(256, 2) void tree_few_kernel(TreeArgs a) {
@@ -411,80 +423,63 @@ __global__ __launch_bounds__(256, 2) void tree_few_kernel(TreeArgs a) {
   load_values(u);
   start_rows(rows, a, b, kvh, tile);
 
-  for (; u < all; u += step) {
-    const bool sealed = u < units;
-    f16x8 kf[8], vf[2][4];
-    uint32_t bits = 0xffffu;
-    bool masked = false;
-    float eta = 0.0f;
-    if (sealed) {
-      // metadata: sigma and z by (block, kind, half of the channels), scales and offsets by block
-      float* const skm = reinterpret_cast<float*>(mine + FEW_KM);
+  for (; u < units; u += step) {
+    // metadata: sigma and z by (block, kind, half of the channels), scales and offsets by block
+    float* const skm = reinterpret_cast<float*>(mine + FEW_KM);
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        *reinterpret_cast<uint4*>(skm + i * FEW_KM_BLK + half * FEW_KM_KIND + ((l >> 4) & 1) * FEW_KM_HALF + (l & 15) * 4) = km[i];
-      *reinterpret_cast<uint4*>(mine + FEW_VM + half * FEW_VM_BLK + n32 * 16) = vm;
-      wave_sync();
-      const float* const sg = skm + bsel * FEW_KM_BLK + half * FEW_KM_HALF;
-      const float* const zz = sg + FEW_KM_KIND;
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
-        const float4 s0 = *reinterpret_cast<const float4*>(sg + ks * 8), s1 = *reinterpret_cast<const float4*>(sg + ks * 8 + 4);
-        const float4 z0 = *reinterpret_cast<const float4*>(zz + ks * 8), z1 = *reinterpret_cast<const float4*>(zz + ks * 8 + 4);
-        const uint32_t c0 = ks & 1 ? kc[ks >> 1].z : kc[ks >> 1].x, c1 = ks & 1 ? kc[ks >> 1].w : kc[ks >> 1].y;
-        kf[ks] = __builtin_bit_cast(f16x8, make_uint4(key2<0>(c0, s0.x, s0.y, z0.x, z0.y), key2<1>(c0, s0.z, s0.w, z0.z, z0.w),
+    for (int i = 0; i < 2; ++i)
+      *reinterpret_cast<uint4*>(skm + i * FEW_KM_BLK + half * FEW_KM_KIND + ((l >> 4) & 1) * FEW_KM_HALF + (l & 15) * 4) = km[i];
+    *reinterpret_cast<uint4*>(mine + FEW_VM + half * FEW_VM_BLK + n32 * 16) = vm;
+    wave_sync();
+    // widths: four channels a lane
+    {
+      const int c = n32 * 4;
+      const float* const p = skm + half * FEW_KM_BLK + (c >> 6) * FEW_KM_HALF + (c & 63);
+      const float4 s4 = *reinterpret_cast<const float4*>(p), z4 = *reinterpret_cast<const float4*>(p + FEW_KM_KIND);
+      *reinterpret_cast<uint2*>(mine + FEW_W + half * FEW_W_BLK + c * 2) =
+          make_uint2(key_width(s4.x, z4.x) | key_width(s4.y, z4.y) << 16, key_width(s4.z, z4.z) | key_width(s4.w, z4.w) << 16);
+    }
+    const float* const sg = skm + bsel * FEW_KM_BLK + half * FEW_KM_HALF;
+    const float* const zz = sg + FEW_KM_KIND;
+    const float eta = value_error(an);
+    rows.vmax = fmaxf(rows.vmax, an.y);
+    attend32(
+        rows, (int64_t)u * 2 + 2 > a.nb, (int64_t)u * 2 + half < a.nb ? 0xffffu : 0u, eta,
+        [&](int ks) {
+          const float4 s0 = *reinterpret_cast<const float4*>(sg + ks * 8), s1 = *reinterpret_cast<const float4*>(sg + ks * 8 + 4);
+          const float4 z0 = *reinterpret_cast<const float4*>(zz + ks * 8), z1 = *reinterpret_cast<const float4*>(zz + ks * 8 + 4);
+          const uint32_t c0 = ks & 1 ? kc[ks >> 1].z : kc[ks >> 1].x, c1 = ks & 1 ? kc[ks >> 1].w : kc[ks >> 1].y;
+          return __builtin_bit_cast(f16x8, make_uint4(key2<0>(c0, s0.x, s0.y, z0.x, z0.y), key2<1>(c0, s0.z, s0.w, z0.z, z0.w),
                                                       key2<0>(c1, s1.x, s1.y, z1.x, z1.y), key2<1>(c1, s1.z, s1.w, z1.z, z1.w)));
-      }
-      // widths: four channels a lane
-      {
-        const int c = n32 * 4;
-        const float* const p = skm + half * FEW_KM_BLK + (c >> 6) * FEW_KM_HALF + (c & 63);
-        const float4 s4 = *reinterpret_cast<const float4*>(p), z4 = *reinterpret_cast<const float4*>(p + FEW_KM_KIND);
-        *reinterpret_cast<uint2*>(mine + FEW_W + half * FEW_W_BLK + c * 2) =
-            make_uint2(key_width(s4.x, z4.x) | key_width(s4.y, z4.y) << 16, key_width(s4.z, z4.z) | key_width(s4.w, z4.w) << 16);
-        wave_sync();
-      }
-      eta = value_error(an);
-      rows.vmax = fmaxf(rows.vmax, an.y);
-      masked = (int64_t)u * 2 + 2 > a.nb;
-      bits = (int64_t)u * 2 + half < a.nb ? 0xffffu : 0u;
-      load_keys(u + step);
-      bound_scores(rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(mine + FEW_W + bsel * FEW_W_BLK + half * 128 + ks * 16); });
-    } else {
-      const int t0 = (u - units) * 32;
-      if (u - step < units) rows.sealed = rows.sum;   // the wave's first of these
-      uint32_t* const bad = reinterpret_cast<uint32_t*>(mine + FEW_BAD);
-      if (l < 2) bad[l] = 0u;
-      wave_sync();
-      load_exact<64, 32>(a, head, t0, l, reinterpret_cast<uint4*>(mine + FEW_K), reinterpret_cast<uint4*>(mine + FEW_V),
-                         reinterpret_cast<float*>(mine + FEW_NORM), bad);
-      wave_sync();
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) kf[ks] = __builtin_bit_cast(f16x8, reinterpret_cast<const uint4*>(mine + FEW_K)[(half * 8 + ks) * 32 + n32]);
-      masked = true;
-      bits = open_exact(rows, a, b, t0 + half * BLK, reinterpret_cast<const float*>(mine + FEW_NORM) + half * BLK, bad[half]);
-    }
-    if (sealed) {
-#pragma unroll
-      for (int oct = 0; oct < 2; ++oct) {
-        const uint8_t* const p = mine + FEW_VM + half * FEW_VM_BLK + oct * 128 + (n32 >> 4) * 64;
-        const uint32_t c[4] = {vc[oct].x, vc[oct].y, vc[oct].z, vc[oct].w};
-#pragma unroll
-        for (int ct = 0; ct < 4; ++ct)
-          vf[oct][ct] = __builtin_bit_cast(f16x8, values8(c[ct], reinterpret_cast<const uint4*>(p)[ct], reinterpret_cast<const uint4*>(p + 256)[ct]));
-      }
-      load_values(u + step);
-    } else {
-#pragma unroll
-      for (int oct = 0; oct < 2; ++oct)
-#pragma unroll
-        for (int ct = 0; ct < 4; ++ct)
-          vf[oct][ct] = __builtin_bit_cast(f16x8, reinterpret_cast<const uint4*>(mine + FEW_V)[(half * 2 + oct) * D + ct * 32 + n32]);
-    }
-    attend32(rows, masked, bits, eta, [&](int ks) { return kf[ks]; }, [&](int oct, int ct) { return vf[oct][ct]; });
+        },
+        [&] {
+          wave_sync();
+          load_keys(u + step);
+          bound_scores(rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(mine + FEW_W + bsel * FEW_W_BLK + half * 128 + ks * 16); });
+        },
+        [&](int oct, int ct) {
+          const uint8_t* const p = mine + FEW_VM + half * FEW_VM_BLK + oct * 128 + (n32 >> 4) * 64 + ct * 16;
+          const uint32_t c = ct == 0 ? vc[oct].x : (ct == 1 ? vc[oct].y : (ct == 2 ? vc[oct].z : vc[oct].w));
+          return __builtin_bit_cast(f16x8, values8(c, *reinterpret_cast<const uint4*>(p), *reinterpret_cast<const uint4*>(p + 256)));
+        });
+    load_values(u + step);
     wave_sync();
   }
-  if (u - step < units) rows.sealed = rows.sum;   // no other tokens
+  rows.sealed = rows.sum;
+  for (; u < all; u += step) {
+    const int t0 = (u - units) * 32;
+    uint8_t* const bad = mine + FEW_BAD;
+    wave_sync();
+    if (l < 8) reinterpret_cast<uint32_t*>(bad)[l] = 0u;
+    wave_sync();
+    load_exact<64, 32>(a, head, t0, l, reinterpret_cast<uint4*>(mine + FEW_K), reinterpret_cast<uint4*>(mine + FEW_V),
+                       reinterpret_cast<float*>(mine + FEW_NORM), bad);
+    wave_sync();
+    const uint32_t bits = open_exact(rows, a, b, t0 + half * BLK, reinterpret_cast<const float*>(mine + FEW_NORM) + half * BLK, bad + half * BLK);
+    attend32(
+        rows, true, bits, 0.0f, [&](int ks) { return __builtin_bit_cast(f16x8, reinterpret_cast<const uint4*>(mine + FEW_K)[(half * 8 + ks) * 32 + n32]); },
+        [] {}, [&](int oct, int ct) { return __builtin_bit_cast(f16x8, reinterpret_cast<const uint4*>(mine + FEW_V)[(half * 2 + oct) * D + ct * 32 + n32]); });
+  }
   end_rows(rows);
   put_rows(rows, s_set[w]);
   __syncthreads();
@@ -515,8 +510,8 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   constexpr int MT = S::MT, TOK = S::TOK, QUADS = S::QUADS, BLKS = S::BLKS;
   __shared__ __align__(16) uint8_t s_main[S::BYTES];
   __shared__ float s_eta[2][BLKS];
-  __shared__ float s_norm[TOK];
-  __shared__ uint32_t s_bad[BLKS];
+  __shared__ __align__(16) float s_norm[TOK];
+  __shared__ __align__(16) uint8_t s_bad[TOK];
 
   const int tid = threadIdx.x, l = tid & 63, n32 = l & 31, half = l >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -569,87 +564,87 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   int buf = 0;
   __syncthreads();
 
-  for (; u < all; u += step, buf ^= 1) {
-    const bool sealed = u < units;
+  const auto key_of = [&](const uint4* s_k, int unit, int ks) { return __builtin_bit_cast(f16x8, s_k[(half * 8 + ks) * TOK + unit * 32 + n32]); };
+  const auto value_of = [&](const uint4* s_v, int blk, int oct, int ct) { return __builtin_bit_cast(f16x8, s_v[(blk * 2 + oct) * D + ct * 32 + n32]); };
+  for (; u < units; u += step, buf ^= 1) {
     uint4* const s_k = reinterpret_cast<uint4*>(s_main + buf * S::TILE);
     uint4* const s_v = s_k + 16 * TOK;
-    if (sealed) {
 #pragma unroll
-      for (int qd = 0; qd < QUADS; ++qd) {
-        const int blk = qd * 4 + wb;
-        float* const meta = reinterpret_cast<float*>(s_meta);
-        if (w < 4) {
-          *reinterpret_cast<uint4*>(meta + l * 4 + (l >> 4) * 4) = raw[qd][2];
-          wave_sync();
-          const float* const sg = meta + c8 * 16 + (c8 >> 2) * 4;
-          const float* const zz = sg + D + 8;
-          uint4 h[2][2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float4 s0 = *reinterpret_cast<const float4*>(sg + e * 8), s1 = *reinterpret_cast<const float4*>(sg + e * 8 + 4);
-            const float4 z0 = *reinterpret_cast<const float4*>(zz + e * 8), z1 = *reinterpret_cast<const float4*>(zz + e * 8 + 4);
-#pragma unroll
-            for (int tt = 0; tt < 2; ++tt) {
-              const uint32_t x0 = e ? raw[qd][tt].z : raw[qd][tt].x, x1 = e ? raw[qd][tt].w : raw[qd][tt].y;
-              h[tt][e] = make_uint4(key2<0>(x0, s0.x, s0.y, z0.x, z0.y), key2<1>(x0, s0.z, s0.w, z0.z, z0.w), key2<0>(x1, s1.x, s1.y, z1.x, z1.y),
-                                    key2<1>(x1, s1.z, s1.w, z1.z, z1.w));
-            }
-          }
-#pragma unroll
-          for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) s_k[(2 * c8 + e) * TOK + key_place(blk, t8 + 8 * tt)] = h[tt][e];
-          // widths: two channels a lane
-          const int ch = c8 * 16 + 2 * t8;
-          const float2 s2 = *reinterpret_cast<const float2*>(sg + 2 * t8), z2 = *reinterpret_cast<const float2*>(zz + 2 * t8);
-          *reinterpret_cast<uint32_t*>(width_at(ring, ch >> 3, fresh + blk) + (ch & 7) * 2) = key_width(s2.x, z2.x) | key_width(s2.y, z2.y) << 16;
-        } else {
-          reinterpret_cast<uint2*>(meta)[l] = make_uint2(raw[qd][2].x, raw[qd][2].y);
-          wave_sync();
-          const int oc = l >> 5, gh = (l >> 4) & 1, n16 = l & 15;
-          const uint8_t* const p = s_meta + oc * 128 + gh * 64;
-          const uint32_t c[4] = {raw[qd][0].x, raw[qd][0].y, raw[qd][0].z, raw[qd][0].w};
-#pragma unroll
-          for (int g = 0; g < 4; ++g)
-            s_v[value_place(blk * 2 + oc, (gh * 4 + g) * 16 + n16)] = values8(c[g], reinterpret_cast<const uint4*>(p)[g], reinterpret_cast<const uint4*>(p + 256)[g]);
-          if (l == 0) s_eta[buf][blk] = value_error(an[qd]);
-          nu = fmaxf(nu, an[qd].y);
-        }
+    for (int qd = 0; qd < QUADS; ++qd) {
+      const int blk = qd * 4 + wb;
+      float* const meta = reinterpret_cast<float*>(s_meta);
+      if (w < 4) {
+        *reinterpret_cast<uint4*>(meta + l * 4 + (l >> 4) * 4) = raw[qd][2];
         wave_sync();
+        const float* const sg = meta + c8 * 16 + (c8 >> 2) * 4;
+        const float* const zz = sg + D + 8;
+        uint4 h[2][2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float4 s0 = *reinterpret_cast<const float4*>(sg + e * 8), s1 = *reinterpret_cast<const float4*>(sg + e * 8 + 4);
+          const float4 z0 = *reinterpret_cast<const float4*>(zz + e * 8), z1 = *reinterpret_cast<const float4*>(zz + e * 8 + 4);
+#pragma unroll
+          for (int tt = 0; tt < 2; ++tt) {
+            const uint32_t x0 = e ? raw[qd][tt].z : raw[qd][tt].x, x1 = e ? raw[qd][tt].w : raw[qd][tt].y;
+            h[tt][e] = make_uint4(key2<0>(x0, s0.x, s0.y, z0.x, z0.y), key2<1>(x0, s0.z, s0.w, z0.z, z0.w), key2<0>(x1, s1.x, s1.y, z1.x, z1.y),
+                                  key2<1>(x1, s1.z, s1.w, z1.z, z1.w));
+          }
+        }
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) s_k[(2 * c8 + e) * TOK + key_place(blk, t8 + 8 * tt)] = h[tt][e];
+        // widths: two channels a lane
+        const int ch = c8 * 16 + 2 * t8;
+        const float2 s2 = *reinterpret_cast<const float2*>(sg + 2 * t8), z2 = *reinterpret_cast<const float2*>(zz + 2 * t8);
+        *reinterpret_cast<uint32_t*>(width_at(ring, ch >> 3, fresh + blk) + (ch & 7) * 2) = key_width(s2.x, z2.x) | key_width(s2.y, z2.y) << 16;
+      } else {
+        reinterpret_cast<uint2*>(meta)[l] = make_uint2(raw[qd][2].x, raw[qd][2].y);
+        wave_sync();
+        const int oc = l >> 5, gh = (l >> 4) & 1, n16 = l & 15;
+        const uint8_t* const p = s_meta + oc * 128 + gh * 64;
+        const uint32_t c[4] = {raw[qd][0].x, raw[qd][0].y, raw[qd][0].z, raw[qd][0].w};
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          s_v[value_place(blk * 2 + oc, (gh * 4 + g) * 16 + n16)] = values8(c[g], reinterpret_cast<const uint4*>(p)[g], reinterpret_cast<const uint4*>(p + 256)[g]);
+        if (l == 0) s_eta[buf][blk] = value_error(an[qd]);
+        nu = fmaxf(nu, an[qd].y);
       }
-      load(u + step < units ? u + step : 0);
-      fresh += BLKS;
-    } else {
-      if (u - step < units) rows.sealed = rows.sum;   // the workgroup's first of these
-      __syncthreads();   // norms and bad tokens of the last tile are done with
-      if (tid < BLKS) {
-        s_bad[tid] = 0u;
-        s_eta[buf][tid] = 0.0f;
-      }
-      __syncthreads();
-      load_exact<512, TOK>(a, head, (u - units) * TOK, tid, s_k, s_v, s_norm, s_bad);
+      wave_sync();
     }
+    load(u + step < units ? u + step : 0);
+    fresh += BLKS;
     __syncthreads();
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const int unit = wt * MT + mt, blk = unit * 2 + half;   // 32 tokens; the lane's block
-      uint32_t bits;
-      if (sealed)
-        bits = (int64_t)u * BLKS + blk < a.nb ? 0xffffu : 0u;
-      else
-        bits = open_exact(rows, a, b, (u - units) * TOK + blk * BLK, s_norm + blk * BLK, s_bad[blk]);
       attend32(
-          rows, !sealed || (int64_t)(u + 1) * BLKS > a.nb, bits, s_eta[buf][blk],
-          [&](int ks) { return __builtin_bit_cast(f16x8, s_k[(half * 8 + ks) * TOK + unit * 32 + n32]); },
-          [&](int oct, int ct) { return __builtin_bit_cast(f16x8, s_v[(blk * 2 + oct) * D + ct * 32 + n32]); });
+          rows, (int64_t)(u + 1) * BLKS > a.nb, (int64_t)u * BLKS + blk < a.nb ? 0xffffu : 0u, s_eta[buf][blk], [&](int ks) { return key_of(s_k, unit, ks); },
+          [] {}, [&](int oct, int ct) { return value_of(s_v, blk, oct, ct); });
     }
-    if (sealed && (fresh == 32 || u + step >= units)) {
+    if (fresh == 32 || u + step >= units) {
       if (wt == 0) bound_scores(rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(width_at(ring, half * 8 + ks, n32)); });
       fresh = 0;
       ring ^= 1;
     }
   }
-  if (u - step < units) rows.sealed = rows.sum;   // no other tokens
+  rows.sealed = rows.sum;
+  for (; u < all; u += step, buf ^= 1) {
+    uint4* const s_k = reinterpret_cast<uint4*>(s_main + buf * S::TILE);
+    uint4* const s_v = s_k + 16 * TOK;
+    __syncthreads();   // norms and bad tokens of the last tile are done with
+    if (tid < TOK) s_bad[tid] = 0;
+    __syncthreads();
+    load_exact<512, TOK>(a, head, (u - units) * TOK, tid, s_k, s_v, s_norm, s_bad);
+    __syncthreads();
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int unit = wt * MT + mt, blk = unit * 2 + half;
+      const uint32_t bits = open_exact(rows, a, b, (u - units) * TOK + blk * BLK, s_norm + blk * BLK, s_bad + blk * BLK);
+      attend32(
+          rows, true, bits, 0.0f, [&](int ks) { return key_of(s_k, unit, ks); }, [] {}, [&](int oct, int ct) { return value_of(s_v, blk, oct, ct); });
+    }
+  }
   __syncthreads();
   if (w >= 4 && l == 0) s_norm[w - 4] = nu;
   __syncthreads();
