@@ -63,29 +63,35 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const f32x2 x = {lo, hi};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, f16x2));
 }
-// two keys of a dword of codes: code sigma + z
+// Eight keys of 16 consecutive codes' lower or upper half: code sigma + z in FP32, rounded to FP16.  (The stored bytes are code + 128: with
+// the top bits turned they convert as signed ones.)
 template <int I>
-__device__ __forceinline__ uint32_t key2(uint32_t codes, float s0, float s1, float z0, float z1) {
-  const uint32_t x = codes >> (16 * I);
-  return pack_f16(fmaf((float)(x & 255u) - 128.0f, s0, z0), fmaf((float)(x >> 8 & 255u) - 128.0f, s1, z1));
+__device__ __forceinline__ float key1(uint32_t codes, float sigma, float z) {
+  return fmaf((float)(int8_t)(codes >> (8 * I)), sigma, z);
 }
-// code scale + offset of two tokens, rounded once.  The scale's rounding to FP16 can take the largest code beyond the group's maximum, and
-// beyond FP16's range where that is at its end (keys cannot: z and sigma are FP32, the largest code is the maximum within 2^-23).
-__device__ __forceinline__ uint32_t value2(uint32_t code, uint32_t scale, uint32_t off) {
-  const f16x2 x = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, code), __builtin_bit_cast(f16x2, scale), __builtin_bit_cast(f16x2, off));
+__device__ __forceinline__ uint4 keys8(uint32_t c0, uint32_t c1, float4 s0, float4 s1, float4 z0, float4 z1) {
+  c0 ^= 0x80808080u, c1 ^= 0x80808080u;
+  return make_uint4(pack_f16(key1<0>(c0, s0.x, z0.x), key1<1>(c0, s0.y, z0.y)), pack_f16(key1<2>(c0, s0.z, z0.z), key1<3>(c0, s0.w, z0.w)),
+                    pack_f16(key1<0>(c1, s1.x, z1.x), key1<1>(c1, s1.y, z1.y)), pack_f16(key1<2>(c1, s1.z, z1.z), key1<3>(c1, s1.w, z1.w)));
+}
+// Eight tokens are paired 0 4, 1 5, 2 6, 3 7, for then one mask takes two codes out of a dword; weights, scales and offsets go along.
+__device__ __forceinline__ uint4 paired(uint4 x) {
+  return make_uint4(__builtin_amdgcn_perm(x.z, x.x, 0x05040100u), __builtin_amdgcn_perm(x.z, x.x, 0x07060302u),
+                    __builtin_amdgcn_perm(x.w, x.y, 0x05040100u), __builtin_amdgcn_perm(x.w, x.y, 0x07060302u));
+}
+// Two values: code scale + offset, rounded once; the codes as FP16 integers by the mantissa of 1024, which leaves exactly.  The scale's
+// rounding to FP16 can take the largest code beyond the group's maximum, and beyond FP16's range where that is at its end (keys cannot:
+// z and sigma are FP32, the largest code is the maximum within 2^-23).
+template <int I>
+__device__ __forceinline__ uint32_t value2(uint32_t codes, uint32_t scale, uint32_t off) {
+  const uint32_t biased = (codes >> (4 * I) & 0x000f000fu) | 0x64006400u;
+  const f16x2 code = __builtin_bit_cast(f16x2, biased) - __builtin_bit_cast(f16x2, 0x64006400u);
+  const f16x2 x = __builtin_elementwise_fma(code, __builtin_bit_cast(f16x2, scale), __builtin_bit_cast(f16x2, off));
   const f16x2 most = {(_Float16)F16_MAX, (_Float16)F16_MAX};
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_minimum(x, most));
 }
-// codes of tokens (2 I, 2 I + 1) of a dword as FP16 integers: dropped into the mantissa of 1024, which leaves exactly
-template <int I>
-__device__ __forceinline__ uint32_t codes2(uint32_t d) {
-  const uint32_t x = d >> (8 * I);
-  const uint32_t pair = (x & 0xfu) | (x << 12 & 0xf0000u) | 0x64006400u;
-  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, pair) - __builtin_bit_cast(f16x2, 0x64006400u));
-}
 __device__ __forceinline__ uint4 values8(uint32_t d, uint4 scale, uint4 off) {
-  return make_uint4(value2(codes2<0>(d), scale.x, off.x), value2(codes2<1>(d), scale.y, off.y), value2(codes2<2>(d), scale.z, off.z),
-                    value2(codes2<3>(d), scale.w, off.w));
+  return make_uint4(value2<0>(d, scale.x, off.x), value2<1>(d, scale.y, off.y), value2<2>(d, scale.z, off.z), value2<3>(d, scale.w, off.w));
 }
 // the width of a key channel in the bound, rounded up to FP16
 __device__ __forceinline__ uint32_t key_width(float sigma, float z) {
@@ -155,11 +161,12 @@ __device__ __forceinline__ void attend32(TreeRows& w, bool masked, uint32_t bits
   uint32_t p[8];
   float bs = 0.0f;
 #pragma unroll
-  for (int r = 0; r < 16; r += 2) {
-    const float x = __builtin_amdgcn_exp2f(fmaf(s[r], SCORE, -base));
-    const float y = __builtin_amdgcn_exp2f(fmaf(s[r + 1], SCORE, -base));
+  for (int r = 0; r < 8; ++r) {
+    const int i = (r & 4) * 2 + (r & 3);   // tokens i and i + 4
+    const float x = __builtin_amdgcn_exp2f(fmaf(s[i], SCORE, -base));
+    const float y = __builtin_amdgcn_exp2f(fmaf(s[i + 4], SCORE, -base));
     bs += x + y;
-    p[r / 2] = pack_f16(x, y);
+    p[r] = pack_f16(x, y);
   }
   const float e = bs * eta;
   w.sum += bs;
@@ -255,7 +262,7 @@ __device__ __forceinline__ void load_exact(const TreeArgs& a, int64_t head, int 
     for (int e = 0; e < 4; ++e) {
       uint32_t h[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) h[j] = __builtin_amdgcn_perm(x[2 * j + 1][e >> 1], x[2 * j][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+      for (int j = 0; j < 4; ++j) h[j] = __builtin_amdgcn_perm(x[j + 4][e >> 1], x[j][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
       values[value_place(oct, c + e)] = make_uint4(h[0], h[1], h[2], h[3]);
     }
   }
@@ -429,7 +436,7 @@ __global__ __launch_bounds__(256, 2) void tree_few_kernel(TreeArgs a) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       *reinterpret_cast<uint4*>(skm + i * FEW_KM_BLK + half * FEW_KM_KIND + ((l >> 4) & 1) * FEW_KM_HALF + (l & 15) * 4) = km[i];
-    *reinterpret_cast<uint4*>(mine + FEW_VM + half * FEW_VM_BLK + n32 * 16) = vm;
+    *reinterpret_cast<uint4*>(mine + FEW_VM + half * FEW_VM_BLK + n32 * 16) = paired(vm);
     wave_sync();
     // widths: four channels a lane
     {
@@ -449,8 +456,7 @@ __global__ __launch_bounds__(256, 2) void tree_few_kernel(TreeArgs a) {
           const float4 s0 = *reinterpret_cast<const float4*>(sg + ks * 8), s1 = *reinterpret_cast<const float4*>(sg + ks * 8 + 4);
           const float4 z0 = *reinterpret_cast<const float4*>(zz + ks * 8), z1 = *reinterpret_cast<const float4*>(zz + ks * 8 + 4);
           const uint32_t c0 = ks & 1 ? kc[ks >> 1].z : kc[ks >> 1].x, c1 = ks & 1 ? kc[ks >> 1].w : kc[ks >> 1].y;
-          return __builtin_bit_cast(f16x8, make_uint4(key2<0>(c0, s0.x, s0.y, z0.x, z0.y), key2<1>(c0, s0.z, s0.w, z0.z, z0.w),
-                                                      key2<0>(c1, s1.x, s1.y, z1.x, z1.y), key2<1>(c1, s1.z, s1.w, z1.z, z1.w)));
+          return __builtin_bit_cast(f16x8, keys8(c0, c1, s0, s1, z0, z1));
         },
         [&] {
           wave_sync();
@@ -549,9 +555,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
         raw[qd][2] = reinterpret_cast<const uint4*>(r + Q_KM + wb * KM_BYTES)[l];
       } else {
         raw[qd][0] = reinterpret_cast<const uint4*>(r + Q_VC + wb * VC_BYTES)[l];
-        const uint2 x = reinterpret_cast<const uint2*>(r + Q_VM + wb * VM_BYTES)[l];
-        raw[qd][2].x = x.x;
-        raw[qd][2].y = x.y;
+        raw[qd][2] = reinterpret_cast<const uint4*>(r + Q_VM + wb * VM_BYTES)[n32];
         an[qd] = reinterpret_cast<const float2*>(r + Q_AN)[wb];
       }
     }
@@ -586,8 +590,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
 #pragma unroll
           for (int tt = 0; tt < 2; ++tt) {
             const uint32_t x0 = e ? raw[qd][tt].z : raw[qd][tt].x, x1 = e ? raw[qd][tt].w : raw[qd][tt].y;
-            h[tt][e] = make_uint4(key2<0>(x0, s0.x, s0.y, z0.x, z0.y), key2<1>(x0, s0.z, s0.w, z0.z, z0.w), key2<0>(x1, s1.x, s1.y, z1.x, z1.y),
-                                  key2<1>(x1, s1.z, s1.w, z1.z, z1.w));
+            h[tt][e] = keys8(x0, x1, s0, s1, z0, z1);
           }
         }
 #pragma unroll
@@ -599,7 +602,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
         const float2 s2 = *reinterpret_cast<const float2*>(sg + 2 * t8), z2 = *reinterpret_cast<const float2*>(zz + 2 * t8);
         *reinterpret_cast<uint32_t*>(width_at(ring, ch >> 3, fresh + blk) + (ch & 7) * 2) = key_width(s2.x, z2.x) | key_width(s2.y, z2.y) << 16;
       } else {
-        reinterpret_cast<uint2*>(meta)[l] = make_uint2(raw[qd][2].x, raw[qd][2].y);
+        if (half == 0) reinterpret_cast<uint4*>(meta)[n32] = paired(raw[qd][2]);
         wave_sync();
         const int oc = l >> 5, gh = (l >> 4) & 1, n16 = l & 15;
         const uint8_t* const p = s_meta + oc * 128 + gh * 64;
@@ -663,7 +666,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   }
 }
 
-// ---- joining: a workgroup has 8 rows, a thread four channels of one ----------------------------------------------------------------
+// ---- joining the partial sets ---------------------------------------------------------------------------------------------------------
 
 struct TreeJoinArgs {
   const float* part;
@@ -674,53 +677,98 @@ struct TreeJoinArgs {
   int n, n_kv, group, row_tiles, nsplit;
 };
 
-__global__ __launch_bounds__(256) void tree_join_kernel(TreeJoinArgs a) {
-  const int row = threadIdx.x & 7, c = threadIdx.x >> 3;
-  const int head = blockIdx.x, tile = blockIdx.y >> 2, r32 = (blockIdx.y & 3) * 8 + row;
+// Eight rows a workgroup.  First every set's quantities of the rows, a set a thread, which gives the sets' weights; then the
+// accumulators, four channels of a row and every fourth set a thread, the first of them requested ahead of the weights.
+constexpr int JOIN_ROWS = 8, JOIN_AHEAD = 8;
+__global__ __launch_bounds__(1024) void tree_join_kernel(TreeJoinArgs a) {
+  extern __shared__ float s_f[];                     // [nsplit][JOIN_ROWS] weights
+  __shared__ __align__(16) float4 s_o[4][32][JOIN_ROWS];
+  __shared__ float s_m[16][JOIN_ROWS];
+  __shared__ float s_q[16][6][JOIN_ROWS];
+  __shared__ uint32_t s_bad[JOIN_ROWS];
+  const int tid = threadIdx.x, row = tid & 7, w = tid >> 6;
+  const int c = (tid >> 3) & 31, g = tid >> 8;       // channels 4 c .. 4 c + 3, sets g, g + 4, ...
+  const int head = blockIdx.x, tile = blockIdx.y >> 2, r32 = (blockIdx.y & 3) * JOIN_ROWS + row;
   const int r = tile * 32 + r32;
   const float* const sets = a.part + ((int64_t)head * a.row_tiles + tile) * a.nsplit * T_FLOATS;
-  __shared__ uint32_t s_bad[8];
-  if (threadIdx.x < 8) s_bad[threadIdx.x] = 0u;
+  const auto channels = [&](int i) { return reinterpret_cast<const float4*>(sets + (int64_t)i * T_FLOATS)[c * T_ROWS + r32]; };
+  float4 y[JOIN_AHEAD];
+#pragma unroll
+  for (int k = 0; k < JOIN_AHEAD; ++k) y[k] = channels(min(g + 4 * k, a.nsplit - 1));
+  if (tid < JOIN_ROWS) s_bad[tid] = 0u;
+
+  const auto lanes_max = [](float x) { return max_x32(max_x16(fmaxf(x, dpp_mov<0x128>(x)))); };   // over the lanes of a row: 8, 16, 32 apart
+  const auto lanes_sum = [](float x) { return sum_x32(sum_x16(x + dpp_mov<0x128>(x))); };
+  float m = -INFINITY;
+  for (int i = tid >> 3; i < a.nsplit; i += 128) m = fmaxf(m, sets[(int64_t)i * T_FLOATS + T_OFLOATS + T_M * T_ROWS + r32]);
+  m = lanes_max(m);
+  if ((tid & 63) < 8) s_m[w][row] = m;
   __syncthreads();
-  float M = -INFINITY;
-  for (int i = 0; i < a.nsplit; ++i) M = fmaxf(M, sets[i * T_FLOATS + T_OFLOATS + T_M * T_ROWS + r32]);
-  float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  float L = 0.0f, sealed = 0.0f, E = 0.0f, EM = 0.0f, DM = 0.0f, VM = 0.0f;
-  for (int i = 0; i < a.nsplit; ++i) {
-    const float* const st = sets + i * T_FLOATS + T_OFLOATS + r32;
+  float M = s_m[0][row];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) M = fmaxf(M, s_m[i][row]);
+  float q[6] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};   // sums: L, sealed, EV; maxima: EVMAX, DMAX, VMAX
+  for (int i = tid >> 3; i < a.nsplit; i += 128) {
+    const float* const st = sets + (int64_t)i * T_FLOATS + T_OFLOATS + r32;
     const float mi = st[T_M * T_ROWS];
     const float f = mi == M ? 1.0f : __builtin_amdgcn_exp2f(mi - M);
-    const float4 y = reinterpret_cast<const float4*>(sets + i * T_FLOATS)[c * T_ROWS + r32];
-    x.x = fmaf(f, y.x, x.x), x.y = fmaf(f, y.y, x.y), x.z = fmaf(f, y.z, x.z), x.w = fmaf(f, y.w, x.w);
-    L = fmaf(f, st[T_L * T_ROWS], L);
-    sealed = fmaf(f, st[T_SEALED * T_ROWS], sealed);
-    E = fmaf(f, st[T_EV * T_ROWS], E);
-    EM = fmaxf(EM, f * st[T_EVMAX * T_ROWS]);
-    DM = fmaxf(DM, st[T_DMAX * T_ROWS]);
-    VM = fmaxf(VM, st[T_VMAX * T_ROWS]);
+    s_f[i * JOIN_ROWS + row] = f;
+    q[0] = fmaf(f, st[T_L * T_ROWS], q[0]);
+    q[1] = fmaf(f, st[T_SEALED * T_ROWS], q[1]);
+    q[2] = fmaf(f, st[T_EV * T_ROWS], q[2]);
+    q[3] = fmaxf(q[3], f * st[T_EVMAX * T_ROWS]);
+    q[4] = fmaxf(q[4], st[T_DMAX * T_ROWS]);
+    q[5] = fmaxf(q[5], st[T_VMAX * T_ROWS]);
   }
-  const bool empty = L == 0.0f;   // the row attends nothing
-  const float inv = empty ? 0.0f : 1.0f / L;
-  // (a mean of values: where the rounding of the weights takes it beyond FP16's range, the values' largest, it stays there)
-  const auto mean = [&](float y) { return y *= inv, isfinite(y) ? __builtin_amdgcn_fmed3f(y, -F16_MAX, F16_MAX) : y; };
-  const f32x2 lo = {mean(x.x), mean(x.y)}, hi = {mean(x.z), mean(x.w)};
+#pragma unroll
+  for (int k = 0; k < 6; ++k) {
+    q[k] = k < 3 ? lanes_sum(q[k]) : lanes_max(q[k]);
+    if ((tid & 63) < 8) s_q[w][k][row] = q[k];
+  }
+  __syncthreads();
+  float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  const auto add = [&](float f, const float4& v) { x.x = fmaf(f, v.x, x.x), x.y = fmaf(f, v.y, x.y), x.z = fmaf(f, v.z, x.z), x.w = fmaf(f, v.w, x.w); };
+#pragma unroll
+  for (int k = 0; k < JOIN_AHEAD; ++k)
+    if (g + 4 * k < a.nsplit) add(s_f[(g + 4 * k) * JOIN_ROWS + row], y[k]);
+  for (int i = g + 4 * JOIN_AHEAD; i < a.nsplit; i += 4) add(s_f[i * JOIN_ROWS + row], channels(i));
+  s_o[g][c][row] = x;
+  __syncthreads();
   const bool mine = r < a.n * a.group;
   const int b = head / a.n_kv, kvh = head - b * a.n_kv, node = r / a.group;
   const int64_t out = ((int64_t)b * a.n + node) * a.n_kv * a.group + kvh * a.group + (r - node * a.group);
-  if (mine) {
-    reinterpret_cast<uint2*>(a.O + out * D)[c] =
-        make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, f16x2)), __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, f16x2)));
-    if (!(isfinite(lo[0]) && isfinite(lo[1]) && isfinite(hi[0]) && isfinite(hi[1]))) atomicOr(&s_bad[row], 1u);
+  float L = 0.0f, inv = 0.0f;
+  if (tid < 256) {
+#pragma unroll
+    for (int k = 1; k < 4; ++k) add(1.0f, s_o[k][c][row]);
+#pragma unroll
+    for (int k = 0; k < 6; ++k) {
+      q[k] = s_q[0][k][row];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) q[k] = k < 3 ? q[k] + s_q[i][k][row] : fmaxf(q[k], s_q[i][k][row]);
+    }
+    L = q[0];
+    inv = L == 0.0f ? 0.0f : 1.0f / L;
+    // (a mean of values: where the rounding of the weights takes it beyond FP16's range, the values' largest, it stays there)
+    const auto mean = [&](float v) { return v *= inv, isfinite(v) ? __builtin_amdgcn_fmed3f(v, -F16_MAX, F16_MAX) : v; };
+    const f32x2 lo = {mean(x.x), mean(x.y)}, hi = {mean(x.z), mean(x.w)};
+    if (mine) {
+      reinterpret_cast<uint2*>(a.O + out * D)[c] =
+          make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, f16x2)), __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, f16x2)));
+      if (!(isfinite(lo[0]) && isfinite(lo[1]) && isfinite(hi[0]) && isfinite(hi[1]))) s_bad[row] = 1u;
+    }
   }
   __syncthreads();
-  if (!mine || c != 0) return;
+  if (tid >= JOIN_ROWS || !mine) return;
+  const bool empty = L == 0.0f;   // the row attends nothing
+  const float DM = q[4], VM = q[5];
   cqa_node_cert ct;
-  ct.E_val = E * inv;
+  ct.E_val = q[2] * inv;
   ct.delta_h = DM;
   ct.v_max = VM;
-  ct.alpha_tail_hat = sealed * inv;
+  ct.alpha_tail_hat = q[1] * inv;
   ct.lse = empty ? -INFINITY : M * LN2 + logf(L);
-  ct.max_block_contrib = EM * inv;
+  ct.max_block_contrib = q[3] * inv;
   ct.reserved = 0.0f;
   float tail = 0.0f;
   if (ct.alpha_tail_hat > 0.0f && DM != 0.0f)
@@ -803,7 +851,7 @@ int32_t launch_tree(const Cache* c, int layer, const __half* q, const __half* kd
   j.group = a.group;
   j.row_tiles = a.row_tiles;
   j.nsplit = a.nsplit;
-  tree_join_kernel<<<dim3((uint32_t)heads, (uint32_t)a.row_tiles * 4), 256, 0, st>>>(j);
+  tree_join_kernel<<<dim3((uint32_t)heads, (uint32_t)a.row_tiles * (32 / JOIN_ROWS)), 1024, (size_t)a.nsplit * JOIN_ROWS * 4, st>>>(j);
   CQA_HIP(hipGetLastError());
   return CQA_OK;
 }
