@@ -126,23 +126,40 @@ __device__ __forceinline__ void start_rows(TreeRows& s, const TreeArgs& a, int b
     for (int r = 0; r < 16; ++r) s.o[ct][r] = 0.0f;
 }
 
-// Scores, softmax and values of 32 tokens.  key(ks), value(oct, ct): the A operands of the two products; between(): what is to be done
-// once the keys are; bits, where masked: the tokens of the lane's block that its row attends.
-template <typename Key, typename Between, typename Value>
-__device__ __forceinline__ void attend32(TreeRows& w, bool masked, uint32_t bits, float eta, Key key, Between between, Value value) {
-  f32x16 s;
+// Products of 32 tokens with the wave's rows.  key(ks), value(oct, ct): the A operands.
+template <typename Key>
+__device__ __forceinline__ void scores32(const TreeRows& w, f32x16& s, Key key) {
 #pragma unroll
   for (int r = 0; r < 16; ++r) s[r] = 0.0f;
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(key(ks), w.q[ks], s, 0, 0, 0);
-  between();
+}
+template <typename Value>
+__device__ __forceinline__ void values32(TreeRows& w, const uint32_t (&p)[8], Value value) {
+#pragma unroll
+  for (int oct = 0; oct < 2; ++oct)
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+      w.o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+          value(oct, ct), __builtin_bit_cast(f16x8, make_uint4(p[4 * oct], p[4 * oct + 1], p[4 * oct + 2], p[4 * oct + 3])), w.o[ct], 0, 0, 0);
+}
+// Scores of MT times 32 tokens to weights.  bits(mt), where masked: the tokens of the lane's block that its row attends; eta(mt): the block's
+// value error.
+template <int MT, typename Bits, typename Eta>
+__device__ __forceinline__ void softmax32(TreeRows& w, f32x16 (&s)[MT], uint32_t (&p)[MT][8], bool masked, Bits bits, Eta eta) {
   if (masked) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = bits >> r & 1u ? s[r] : -INFINITY;
-  }
-  float top = s[0];
+    for (int mt = 0; mt < MT; ++mt) {
+      const uint32_t x = bits(mt);
 #pragma unroll
-  for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+      for (int r = 0; r < 16; ++r) s[mt][r] = x >> r & 1u ? s[mt][r] : -INFINITY;
+    }
+  }
+  float top = -INFINITY;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[mt][r]);
   top = max_x32(top) * SCORE;
   if (__any(top > w.m)) {
     const float mn = fmaxf(w.m, top);
@@ -158,26 +175,32 @@ __device__ __forceinline__ void attend32(TreeRows& w, bool masked, uint32_t bits
       for (int r = 0; r < 16; ++r) w.o[ct][r] *= f;
   }
   const float base = w.m == -INFINITY ? 0.0f : w.m;   // nothing attended yet: every weight is exp2(-inf) = 0
-  uint32_t p[8];
-  float bs = 0.0f;
 #pragma unroll
-  for (int r = 0; r < 8; ++r) {
-    const int i = (r & 4) * 2 + (r & 3);   // tokens i and i + 4
-    const float x = __builtin_amdgcn_exp2f(fmaf(s[i], SCORE, -base));
-    const float y = __builtin_amdgcn_exp2f(fmaf(s[i + 4], SCORE, -base));
-    bs += x + y;
-    p[r] = pack_f16(x, y);
+  for (int mt = 0; mt < MT; ++mt) {
+    float bs = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const int i = (r & 4) * 2 + (r & 3);   // tokens i and i + 4
+      const float x = __builtin_amdgcn_exp2f(fmaf(s[mt][i], SCORE, -base));
+      const float y = __builtin_amdgcn_exp2f(fmaf(s[mt][i + 4], SCORE, -base));
+      bs += x + y;
+      p[mt][r] = pack_f16(x, y);
+    }
+    const float e = bs * eta(mt);
+    w.sum += bs;
+    w.ev += e;
+    w.evmax = fmaxf(w.evmax, e);
   }
-  const float e = bs * eta;
-  w.sum += bs;
-  w.ev += e;
-  w.evmax = fmaxf(w.evmax, e);
-#pragma unroll
-  for (int oct = 0; oct < 2; ++oct)
-#pragma unroll
-    for (int ct = 0; ct < 4; ++ct)
-      w.o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-          value(oct, ct), __builtin_bit_cast(f16x8, make_uint4(p[4 * oct], p[4 * oct + 1], p[4 * oct + 2], p[4 * oct + 3])), w.o[ct], 0, 0, 0);
+}
+// All of it; between(): what is to be done once the keys are.
+template <typename Key, typename Between, typename Value>
+__device__ __forceinline__ void attend32(TreeRows& w, bool masked, uint32_t bits, float eta, Key key, Between between, Value value) {
+  f32x16 s[1];
+  uint32_t p[1][8];
+  scores32(w, s[0], key);
+  between();
+  softmax32<1>(w, s, p, masked, [&](int) { return bits; }, [&](int) { return eta; });
+  values32(w, p[0], value);
 }
 
 // Delta of 32 blocks (or of fewer, repeated); width(ks): the A operand
@@ -495,8 +518,12 @@ __global__ __launch_bounds__(256, 2) void tree_few_kernel(TreeArgs a) {
 // ---- more rows: bound by the products -------------------------------------------------------------------------------------------------
 //
 // Eight waves, WR side by side over rows (32 each) and WT over tokens; four of them reconstruct the tile's keys and four its values
-// into LDS, a block each, for all.  Two tiles in LDS: the next one is written while the slower waves still read the last, one barrier a
-// tile; its codes are requested a tile ahead.
+// into LDS, a block each, for all.  A SIMD has a wave of either kind, and they take turns: while one multiplies (the last tile's
+// weights with its values, the next one's keys with the queries) the other one forms weights and reconstructs, with a barrier
+// between the phases, so that the matrix cores and the vector ALU of a SIMD both have work.  With phases numbered from 0, wave kind A (keys)
+// multiplies tile t in phase 2 t and works on its scores and the keys of t + 1 in 2 t + 1; kind B (values) a phase later, on its scores and the
+// values of t + 1 in 2 t + 2.  Keys of t are read in phases 2 t and 2 t + 1 and replaced (t + 2) in 2 t + 3; values of t are read in
+// 2 t + 2 and 2 t + 3 and replaced in 2 t + 4: two tiles in LDS.  Codes are requested a tile ahead of their reconstruction.
 template <int WR>
 struct ManyShape {
   static constexpr int WT = 8 / WR;
@@ -542,22 +569,20 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   uint4 raw[QUADS][3];
   float2 an[QUADS];
   float nu = 0.0f;
+  // The same requests for either kind of waves, at their own offsets: in a branch, what joins behind it is waited for there.
+  const uint32_t at0 = w < 4 ? Q_KC + wb * KC_BYTES + c8 * 256 + t8 * 16 : Q_VC + wb * VC_BYTES + l * 16;
+  const uint32_t at1 = w < 4 ? at0 + 128 : at0;
+  const uint32_t at2 = w < 4 ? Q_KM + wb * KM_BYTES + l * 16 : Q_VM + wb * VM_BYTES + n32 * 16;
   const auto load = [&](int u) {
 #pragma unroll
     for (int qd = 0; qd < QUADS; ++qd) {
       int quad = u * QUADS + qd;
       if (quad >= nquads) quad = 0;   // behind the last: any record of the head, its scores are masked
       const uint8_t* const r = base + (int64_t)quad * QUAD_BYTES;
-      if (w < 4) {
-        const uint8_t* const p = r + Q_KC + wb * KC_BYTES + c8 * 256 + t8 * 16;
-        raw[qd][0] = *reinterpret_cast<const uint4*>(p);
-        raw[qd][1] = *reinterpret_cast<const uint4*>(p + 128);
-        raw[qd][2] = reinterpret_cast<const uint4*>(r + Q_KM + wb * KM_BYTES)[l];
-      } else {
-        raw[qd][0] = reinterpret_cast<const uint4*>(r + Q_VC + wb * VC_BYTES)[l];
-        raw[qd][2] = reinterpret_cast<const uint4*>(r + Q_VM + wb * VM_BYTES)[n32];
-        an[qd] = reinterpret_cast<const float2*>(r + Q_AN)[wb];
-      }
+      raw[qd][0] = *reinterpret_cast<const uint4*>(r + at0);
+      raw[qd][1] = *reinterpret_cast<const uint4*>(r + at1);
+      raw[qd][2] = *reinterpret_cast<const uint4*>(r + at2);
+      an[qd] = reinterpret_cast<const float2*>(r + Q_AN)[wb];
     }
   };
   int u = split;
@@ -569,18 +594,31 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   __syncthreads();
 
   const auto key_of = [&](const uint4* s_k, int unit, int ks) { return __builtin_bit_cast(f16x8, s_k[(half * 8 + ks) * TOK + unit * 32 + n32]); };
+  // From one phase to the next: nothing of either is moved across.
+  const auto turn_over = [] {
+    __builtin_amdgcn_sched_barrier(0);
+    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
+  };
   const auto value_of = [&](const uint4* s_v, int blk, int oct, int ct) { return __builtin_bit_cast(f16x8, s_v[(blk * 2 + oct) * D + ct * 32 + n32]); };
-  for (; u < units; u += step, buf ^= 1) {
+  // The wave's part of a tile: keys and widths, or values and eta.
+  // Its metadata go through LDS, which is begun ahead of other work (stage).
+  const auto stage = [&](int qd) {
+    if (w < 4)
+      *reinterpret_cast<uint4*>(s_meta + (l * 4 + (l >> 4) * 4) * 4) = raw[qd][2];
+    else if (half == 0)
+      reinterpret_cast<uint4*>(s_meta)[n32] = paired(raw[qd][2]);
+    wave_sync();
+  };
+  const auto reconstruct = [&](int buf, int ring, int fresh) {
     uint4* const s_k = reinterpret_cast<uint4*>(s_main + buf * S::TILE);
     uint4* const s_v = s_k + 16 * TOK;
 #pragma unroll
     for (int qd = 0; qd < QUADS; ++qd) {
       const int blk = qd * 4 + wb;
-      float* const meta = reinterpret_cast<float*>(s_meta);
+      if (qd > 0) stage(qd);
       if (w < 4) {
-        *reinterpret_cast<uint4*>(meta + l * 4 + (l >> 4) * 4) = raw[qd][2];
-        wave_sync();
-        const float* const sg = meta + c8 * 16 + (c8 >> 2) * 4;
+        const float* const sg = reinterpret_cast<const float*>(s_meta) + c8 * 16 + (c8 >> 2) * 4;
         const float* const zz = sg + D + 8;
         uint4 h[2][2];
 #pragma unroll
@@ -602,8 +640,6 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
         const float2 s2 = *reinterpret_cast<const float2*>(sg + 2 * t8), z2 = *reinterpret_cast<const float2*>(zz + 2 * t8);
         *reinterpret_cast<uint32_t*>(width_at(ring, ch >> 3, fresh + blk) + (ch & 7) * 2) = key_width(s2.x, z2.x) | key_width(s2.y, z2.y) << 16;
       } else {
-        if (half == 0) reinterpret_cast<uint4*>(meta)[n32] = paired(raw[qd][2]);
-        wave_sync();
         const int oc = l >> 5, gh = (l >> 4) & 1, n16 = l & 15;
         const uint8_t* const p = s_meta + oc * 128 + gh * 64;
         const uint32_t c[4] = {raw[qd][0].x, raw[qd][0].y, raw[qd][0].z, raw[qd][0].w};
@@ -615,21 +651,72 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
       }
       wave_sync();
     }
-    load(u + step < units ? u + step : 0);
-    fresh += BLKS;
-    __syncthreads();
+  };
+  // The values of the tile in `buf ^ 1` with the weights p, and the keys of that in `buf` to scores.  Operands are read AHEAD products
+  // ahead of their use; the scores' chains of MT tiles alternate.
+  constexpr int AHEAD = 8;
+  const auto multiply = [&](int buf, const uint32_t (&p)[MT][8], f32x16 (&sc)[MT], bool keys) {
+    const uint4* const s_k = reinterpret_cast<const uint4*>(s_main + buf * S::TILE);
+    const uint4* const s_v = reinterpret_cast<const uint4*>(s_main + (buf ^ 1) * S::TILE) + 16 * TOK;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      const int unit = wt * MT + mt, blk = unit * 2 + half;   // 32 tokens; the lane's block
-      attend32(
-          rows, (int64_t)(u + 1) * BLKS > a.nb, (int64_t)u * BLKS + blk < a.nb ? 0xffffu : 0u, s_eta[buf][blk], [&](int ks) { return key_of(s_k, unit, ks); },
-          [] {}, [&](int oct, int ct) { return value_of(s_v, blk, oct, ct); });
+    for (int mt = 0; mt < MT; ++mt) values32(rows, p[mt], [&](int oct, int ct) { return value_of(s_v, (wt * MT + mt) * 2 + half, oct, ct); });
+    if (keys) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[mt][r] = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) sc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key_of(s_k, wt * MT + mt, ks), rows.q[ks], sc[mt], 0, 0, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+      for (int i = 0; i < 16 * MT - AHEAD; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
     }
-    if (fresh == 32 || u + step >= units) {
-      if (wt == 0) bound_scores(rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(width_at(ring, half * 8 + ks, n32)); });
-      fresh = 0;
-      ring ^= 1;
+  };
+  f32x16 sc[MT];
+  uint32_t p[MT][8];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int r = 0; r < 8; ++r) p[mt][r] = 0u;
+  if (u < units) {
+    // the values that the first turn's weights, zeros, meet
+    for (int i = tid; i < 16 * TOK; i += 512) (reinterpret_cast<uint4*>(s_main + S::TILE) + 16 * TOK)[i] = make_uint4(0u, 0u, 0u, 0u);
+    stage(0);
+    reconstruct(0, 0, 0);
+    load(u + step < units ? u + step : 0);
+    fresh = BLKS;
+    __syncthreads();
+    if (w >= 4) turn_over();
+    for (; u < units; u += step, buf ^= 1) {
+      __builtin_amdgcn_s_setprio(1);
+      multiply(buf, p, sc, true);
+      const bool full = fresh == 32;
+      if (full || u + step >= units) {
+        if (wt == 0) bound_scores(rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(width_at(ring, half * 8 + ks, n32)); });
+        fresh = 0;
+        ring ^= 1;
+      }
+      __builtin_amdgcn_s_setprio(0);
+      turn_over();
+      if (u + step < units) stage(0);
+      softmax32<MT>(
+          rows, sc, p, (int64_t)(u + 1) * BLKS > a.nb, [&](int mt) { return (int64_t)u * BLKS + (wt * MT + mt) * 2 + half < a.nb ? 0xffffu : 0u; },
+          [&](int mt) { return s_eta[buf][(wt * MT + mt) * 2 + half]; });
+      if (u + step < units) {
+        reconstruct(buf ^ 1, ring, fresh);
+        load(u + 2 * step < units ? u + 2 * step : 0);
+        fresh += BLKS;
+      }
+      turn_over();
     }
+    if (w < 4) turn_over();
+    multiply(buf, p, sc, false);
   }
   rows.sealed = rows.sum;
   for (; u < all; u += step, buf ^= 1) {
