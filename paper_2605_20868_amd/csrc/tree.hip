@@ -20,6 +20,8 @@
 //
 // A further workgroup per group of rows attends the trailing FP16 tokens and the drafted ones, which are exact, under the mask.
 #include <algorithm>
+#include <type_traits>
+#include <utility>
 
 #include "cqa_internal.h"
 #include "reduce_inl.h"
@@ -35,6 +37,16 @@ constexpr float SCORE = 0.08838834764831845f * 1.4426950408889634f;   // 1 / sqr
 constexpr float HALF_SCORE = 0.5f * 0.08838834764831845f;
 constexpr float F16_MAX = 65504.0f;
 constexpr float LN2 = 0.6931471805599453f;
+
+// f(0), f(1), ... f(N - 1), each with its index as a constant
+template <typename F, int... I>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F f) {
+  each_of(std::make_integer_sequence<int, N>{}, f);
+}
 
 // ---- partial set of a split and 32 rows: the accumulators by (four channels, row), then one float per row for each quantity
 enum { T_M = 0, T_L, T_SEALED, T_EV, T_EVMAX, T_DMAX, T_VMAX };
@@ -518,12 +530,14 @@ __global__ __launch_bounds__(256, 2) void tree_few_kernel(TreeArgs a) {
 // ---- more rows: bound by the products -------------------------------------------------------------------------------------------------
 //
 // Eight waves, WR side by side over rows (32 each) and WT over tokens; four of them reconstruct the tile's keys and four its values
-// into LDS, a block each, for all.  A SIMD has a wave of either kind, and they take turns: while one multiplies (the last tile's
-// weights with its values, the next one's keys with the queries) the other one forms weights and reconstructs, with a barrier
-// between the phases, so that the matrix cores and the vector ALU of a SIMD both have work.  With phases numbered from 0, wave kind A (keys)
-// multiplies tile t in phase 2 t and works on its scores and the keys of t + 1 in 2 t + 1; kind B (values) a phase later, on its scores and the
-// values of t + 1 in 2 t + 2.  Keys of t are read in phases 2 t and 2 t + 1 and replaced (t + 2) in 2 t + 3; values of t are read in
-// 2 t + 2 and 2 t + 3 and replaced in 2 t + 4: two tiles in LDS.  Codes are requested a tile ahead of their reconstruction.
+// into LDS, a block each, for all.  A SIMD has a wave of either kind, and they take turns with a barrier between the phases: while one
+// multiplies (the last tile's weights with its values, the next one's keys with the queries) and reconstructs between its products,
+// the other one turns scores into weights, so that the matrix cores and the vector ALU of a SIMD both have work.  Phases numbered from 0:
+//   keys' waves    phase 2 t      values of t - 1, scores of t, reconstruct the keys of t + 1      phase 2 t + 1  weights of t
+//   values' waves  phase 2 t + 1  values of t - 1, scores of t, reconstruct the values of t        phase 2 t + 2  weights of t
+// Keys of t are read in 2 t and 2 t + 1 and replaced (t + 2) in 2 t + 2; values of t are read in 2 t + 2 and 2 t + 3 and replaced
+// in 2 t + 5: two tiles in LDS.  eta of t comes with the keys in 2 t - 2 and is read until 2 t + 2: four of them.  Codes are requested a tile
+// ahead.  (Reconstruction in the weights' phase: products 1310 cycles, weights and reconstruction 2600, of which the products' wave waited half.)
 template <int WR>
 struct ManyShape {
   static constexpr int WT = 8 / WR;
@@ -533,7 +547,7 @@ struct ManyShape {
   static constexpr int TILE = 2 * TOK * D * 2;    // keys [16 runs][TOK], values [TOK / 8][128], 16 bytes each
   // LDS: two tiles, the waves' metadata of a block (16 bytes more behind each 64 floats), the widths of 32 blocks while the next 32 come;
   // at the end the waves' sets, where there are some to be joined
-  static constexpr int META = KM_BYTES + 3 * 16, META_AT = 2 * TILE, WIDTH_AT = META_AT + 8 * META, END = WIDTH_AT + 2 * 32 * D * 2;
+  static constexpr int META = KM_BYTES + 4 * 16, META_AT = 2 * TILE, WIDTH_AT = META_AT + 8 * META, END = WIDTH_AT + 2 * 32 * D * 2;
   static constexpr int BYTES = WT > 1 && 8 * T_FLOATS * 4 > END ? 8 * T_FLOATS * 4 : END;
 };
 
@@ -542,7 +556,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   using S = ManyShape<WR>;
   constexpr int MT = S::MT, TOK = S::TOK, QUADS = S::QUADS, BLKS = S::BLKS;
   __shared__ __align__(16) uint8_t s_main[S::BYTES];
-  __shared__ float s_eta[2][BLKS];
+  __shared__ float s_eta[4][BLKS];
   __shared__ __align__(16) float s_norm[TOK];
   __shared__ __align__(16) uint8_t s_bad[TOK];
 
@@ -577,7 +591,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
 #pragma unroll
     for (int qd = 0; qd < QUADS; ++qd) {
       int quad = u * QUADS + qd;
-      if (quad >= nquads) quad = 0;   // behind the last: any record of the head, its scores are masked
+      if (u >= units || quad >= nquads) quad = 0;   // behind the last: any record of the head
       const uint8_t* const r = base + (int64_t)quad * QUAD_BYTES;
       raw[qd][0] = *reinterpret_cast<const uint4*>(r + at0);
       raw[qd][1] = *reinterpret_cast<const uint4*>(r + at1);
@@ -601,81 +615,81 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
     __builtin_amdgcn_sched_barrier(0);
   };
   const auto value_of = [&](const uint4* s_v, int blk, int oct, int ct) { return __builtin_bit_cast(f16x8, s_v[(blk * 2 + oct) * D + ct * 32 + n32]); };
-  // The wave's part of a tile: keys and widths, or values and eta.
-  // Its metadata go through LDS, which is begun ahead of other work (stage).
-  const auto stage = [&](int qd) {
-    if (w < 4)
+  // The wave's part of a tile, keys and widths and eta, or values.  Metadata go through LDS (stage): 512 bytes of either kind, the
+  // second one (zero points, offsets) 544 bytes behind the first.
+  const auto stage = [&](auto keys, int qd) {
+    if constexpr (keys.value)
       *reinterpret_cast<uint4*>(s_meta + (l * 4 + (l >> 4) * 4) * 4) = raw[qd][2];
     else if (half == 0)
-      reinterpret_cast<uint4*>(s_meta)[n32] = paired(raw[qd][2]);
+      *reinterpret_cast<uint4*>(s_meta + (n32 >> 4) * 544 + (n32 & 15) * 16) = paired(raw[qd][2]);
     wave_sync();
   };
-  const auto reconstruct = [&](int buf, int ring, int fresh) {
-    uint4* const s_k = reinterpret_cast<uint4*>(s_main + buf * S::TILE);
-    uint4* const s_v = s_k + 16 * TOK;
+  // The reconstruction of the wave's block of quad qd in PIECES pieces of some five operations, J = 0, 1, ...; metadata are read a group of
+  // five pieces ahead of their use, the first ones by begin.
+  constexpr int PIECES = 24;
+  uint4 m4[2][4], out4;
+  float2 w2[2];
+  const auto begin = [&](auto keys) {
+    const uint8_t* const m = s_meta + (keys.value ? (c8 * 16 + (c8 >> 2) * 4) * 4 : (l >> 5) * 128 + ((l >> 4) & 1) * 64);
+    if constexpr (keys.value) {
 #pragma unroll
-    for (int qd = 0; qd < QUADS; ++qd) {
-      const int blk = qd * 4 + wb;
-      if (qd > 0) stage(qd);
-      if (w < 4) {
-        const float* const sg = reinterpret_cast<const float*>(s_meta) + c8 * 16 + (c8 >> 2) * 4;
-        const float* const zz = sg + D + 8;
-        uint4 h[2][2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float4 s0 = *reinterpret_cast<const float4*>(sg + e * 8), s1 = *reinterpret_cast<const float4*>(sg + e * 8 + 4);
-          const float4 z0 = *reinterpret_cast<const float4*>(zz + e * 8), z1 = *reinterpret_cast<const float4*>(zz + e * 8 + 4);
-#pragma unroll
-          for (int tt = 0; tt < 2; ++tt) {
-            const uint32_t x0 = e ? raw[qd][tt].z : raw[qd][tt].x, x1 = e ? raw[qd][tt].w : raw[qd][tt].y;
-            h[tt][e] = keys8(x0, x1, s0, s1, z0, z1);
-          }
-        }
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) s_k[(2 * c8 + e) * TOK + key_place(blk, t8 + 8 * tt)] = h[tt][e];
-        // widths: two channels a lane
-        const int ch = c8 * 16 + 2 * t8;
-        const float2 s2 = *reinterpret_cast<const float2*>(sg + 2 * t8), z2 = *reinterpret_cast<const float2*>(zz + 2 * t8);
-        *reinterpret_cast<uint32_t*>(width_at(ring, ch >> 3, fresh + blk) + (ch & 7) * 2) = key_width(s2.x, z2.x) | key_width(s2.y, z2.y) << 16;
-      } else {
-        const int oc = l >> 5, gh = (l >> 4) & 1, n16 = l & 15;
-        const uint8_t* const p = s_meta + oc * 128 + gh * 64;
-        const uint32_t c[4] = {raw[qd][0].x, raw[qd][0].y, raw[qd][0].z, raw[qd][0].w};
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          s_v[value_place(blk * 2 + oc, (gh * 4 + g) * 16 + n16)] = values8(c[g], reinterpret_cast<const uint4*>(p)[g], reinterpret_cast<const uint4*>(p + 256)[g]);
-        if (l == 0) s_eta[buf][blk] = value_error(an[qd]);
-        nu = fmaxf(nu, an[qd].y);
-      }
-      wave_sync();
+      for (int i = 0; i < 4; ++i) m4[0][i] = *reinterpret_cast<const uint4*>(m + (i >> 1) * 544 + (i & 1) * 16);
+    } else {
+      m4[0][0] = *reinterpret_cast<const uint4*>(m);
+      m4[0][1] = *reinterpret_cast<const uint4*>(m + 544);
     }
   };
-  // The values of the tile in `buf ^ 1` with the weights p, and the keys of that in `buf` to scores.  Operands are read AHEAD products
-  // ahead of their use; the scores' chains of MT tiles alternate.
-  constexpr int AHEAD = 8;
-  const auto multiply = [&](int buf, const uint32_t (&p)[MT][8], f32x16 (&sc)[MT], bool keys) {
-    const uint4* const s_k = reinterpret_cast<const uint4*>(s_main + buf * S::TILE);
-    const uint4* const s_v = reinterpret_cast<const uint4*>(s_main + (buf ^ 1) * S::TILE) + 16 * TOK;
+  const auto reconstruct = [&](auto keys, auto qd_, auto j_, int buf, int ring, int slot, int turn) {
+    constexpr int qd = qd_.value, J = j_.value, G = J / 5, R = J % 5;
+    uint4* const s_k = reinterpret_cast<uint4*>(s_main + buf * S::TILE);
+    uint4* const s_v = s_k + 16 * TOK;
+    const int blk = qd * 4 + wb;
+    if constexpr (keys.value) {
+      const uint8_t* const m = s_meta + (c8 * 16 + (c8 >> 2) * 4) * 4;
+      const int ch = c8 * 16 + 2 * t8;
+      if constexpr (G < 4 && R == 0) {
+        if constexpr (G == 1)
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) values32(rows, p[mt], [&](int oct, int ct) { return value_of(s_v, (wt * MT + mt) * 2 + half, oct, ct); });
-    if (keys) {
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sc[mt][r] = 0.0f;
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) sc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key_of(s_k, wt * MT + mt, ks), rows.q[ks], sc[mt], 0, 0, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
-#pragma unroll
-      for (int i = 0; i < 16 * MT - AHEAD; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          for (int i = 0; i < 4; ++i) m4[1][i] = *reinterpret_cast<const uint4*>(m + 32 + (i >> 1) * 544 + (i & 1) * 16);
+        if constexpr (G == 2) {   // of the widths: two channels a lane
+          w2[0] = reinterpret_cast<const float2*>(m)[t8];
+          w2[1] = reinterpret_cast<const float2*>(m + 544)[t8];
+        }
+      } else if constexpr (G < 4) {
+        // eight channels E of token t8 + 8 T, two a piece
+        constexpr int E = G >> 1, T = G & 1, I = R - 1;
+        const uint4& x = raw[qd][T];
+        const uint32_t c = (E ? (I < 2 ? x.z : x.w) : (I < 2 ? x.x : x.y)) ^ 0x80808080u;
+        const uint4 sg = m4[E][I >> 1], zz = m4[E][2 + (I >> 1)];
+        const uint32_t y = pack_f16(key1<2 * (I & 1)>(c, __uint_as_float(I & 1 ? sg.z : sg.x), __uint_as_float(I & 1 ? zz.z : zz.x)),
+                                    key1<2 * (I & 1) + 1>(c, __uint_as_float(I & 1 ? sg.w : sg.y), __uint_as_float(I & 1 ? zz.w : zz.y)));
+        (I == 0 ? out4.x : I == 1 ? out4.y : I == 2 ? out4.z : out4.w) = y;
+        if constexpr (I == 3) s_k[(2 * c8 + E) * TOK + key_place(blk, t8 + 8 * T)] = out4;
+      } else if constexpr (R == 0) {
+        out4.x = key_width(w2[0].x, w2[1].x);
+      } else if constexpr (R == 1) {
+        *reinterpret_cast<uint32_t*>(width_at(ring, ch >> 3, slot + blk) + (ch & 7) * 2) = out4.x | key_width(w2[0].y, w2[1].y) << 16;
+      } else if constexpr (R == 2) {
+        s_eta[turn & 3][blk] = value_error(an[qd]);   // (every lane the same)
+        nu = fmaxf(nu, an[qd].y);
       }
-      __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+    } else if constexpr (G < 4) {
+      // eight tokens of octet oc of channel (gh 4 + G) 16 + n16, two a piece
+      const int oc = l >> 5, gh = (l >> 4) & 1, n16 = l & 15;
+      if constexpr (R == 0) {
+        if constexpr (G < 3) {
+          const uint8_t* const m = s_meta + oc * 128 + gh * 64 + (G + 1) * 16;
+          m4[(G + 1) & 1][0] = *reinterpret_cast<const uint4*>(m);
+          m4[(G + 1) & 1][1] = *reinterpret_cast<const uint4*>(m + 544);
+        }
+      } else {
+        constexpr int I = R - 1;
+        const uint4 &x = raw[qd][0], &sc = m4[G & 1][0], &of = m4[G & 1][1];
+        const uint32_t y = value2<I>(G == 0 ? x.x : G == 1 ? x.y : G == 2 ? x.z : x.w, I == 0 ? sc.x : I == 1 ? sc.y : I == 2 ? sc.z : sc.w,
+                                     I == 0 ? of.x : I == 1 ? of.y : I == 2 ? of.z : of.w);
+        (I == 0 ? out4.x : I == 1 ? out4.y : I == 2 ? out4.z : out4.w) = y;
+        if constexpr (I == 3) s_v[value_place(blk * 2 + oc, (gh * 4 + G) * 16 + n16)] = out4;
+      }
     }
   };
   f32x16 sc[MT];
@@ -684,39 +698,99 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
     for (int r = 0; r < 8; ++r) p[mt][r] = 0u;
+  const auto add_values = [&](int buf) {
+    const uint4* const s_v = reinterpret_cast<const uint4*>(s_main + buf * S::TILE) + 16 * TOK;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) values32(rows, p[mt], [&](int oct, int ct) { return value_of(s_v, (wt * MT + mt) * 2 + half, oct, ct); });
+  };
+  // The products of a phase in their order, operands read AHEAD products ahead, and behind each some pieces of the reconstruction.  (Left to
+  // the compiler, which cannot tell the tiles apart, each operand was read when it was needed: 3310 cycles a phase.)
+  constexpr int PRODUCTS = 16 * MT, AHEAD = 6, FROM = 2, EACH = (PIECES * QUADS + PRODUCTS - FROM - 1) / (PRODUCTS - FROM);
+  const auto sealed_tiles = [&](auto keys) {
+    for (int turn = 0; u < units; u += step, buf ^= 1, ++turn) {
+      const bool last = u + step >= units, full = fresh == 32;
+      const int ring1 = full ? ring ^ 1 : ring, slot = full ? 0 : fresh;   // where the next tile's widths go
+      const uint4* const s_k = reinterpret_cast<const uint4*>(s_main + buf * S::TILE);
+      const uint4* const s_v = reinterpret_cast<const uint4*>(s_main + (buf ^ 1) * S::TILE) + 16 * TOK;
+      f16x8 f[AHEAD];
+      // product I: values (mt, octet, channel tile), then keys (channels, mt): the accumulators take turns
+      const auto operand = [&](auto i_) {
+        constexpr int I = i_.value, K = I - 8 * MT;
+        if constexpr (K < 0)
+          f[I % AHEAD] = value_of(s_v, (wt * MT + I / 8) * 2 + half, (I & 7) >> 2, I & 3);
+        else
+          f[I % AHEAD] = key_of(s_k, wt * MT + K % MT, K / MT);
+      };
+      const auto product = [&](auto i_) {
+        constexpr int I = i_.value, K = I - 8 * MT;
+        if constexpr (K < 0) {
+          const uint32_t* const x = &p[I / 8][(I & 4)];
+          rows.o[I & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[I % AHEAD], __builtin_bit_cast(f16x8, make_uint4(x[0], x[1], x[2], x[3])), rows.o[I & 3], 0, 0, 0);
+        } else {
+          if constexpr (K < MT)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[K][r] = 0.0f;
+          sc[K % MT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[I % AHEAD], rows.q[K / MT], sc[K % MT], 0, 0, 0);
+        }
+      };
+      __builtin_amdgcn_s_setprio(1);
+      stage(keys, 0);
+      each<AHEAD>(operand);
+      begin(keys);
+      __builtin_amdgcn_sched_barrier(0);
+      each<PRODUCTS>([&](auto i_) {
+        constexpr int I = i_.value;
+        product(i_);
+        if constexpr (I + AHEAD < PRODUCTS) operand(std::integral_constant<int, I + AHEAD>{});
+        // (keys, behind the last tile: of the head's first record, which nothing reads, and its widths, which are the head's)
+        if constexpr (I >= FROM)
+          each<EACH>([&](auto k_) {
+            constexpr int P = (I - FROM) * EACH + k_.value, QD = P / PIECES, J = P % PIECES;
+            if constexpr (P < PIECES * QUADS) {
+              if constexpr (QD > 0 && J == 0) {
+                stage(keys, QD);
+                begin(keys);
+              }
+              reconstruct(keys, std::integral_constant<int, QD>{}, std::integral_constant<int, J>{}, keys.value ? buf ^ 1 : buf, ring1, slot, turn + 1);
+            }
+          });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      load(keys.value ? u + 2 * step : u + step);
+      if (full || last) {
+        if (wt == 0) bound_scores(rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(width_at(ring, half * 8 + ks, n32)); });
+      }
+      ring = ring1;
+      fresh = slot + BLKS;
+      __builtin_amdgcn_s_setprio(0);
+      turn_over();
+      softmax32<MT>(
+          rows, sc, p, (int64_t)(u + 1) * BLKS > a.nb, [&](int mt) { return (int64_t)u * BLKS + (wt * MT + mt) * 2 + half < a.nb ? 0xffffu : 0u; },
+          [&](int mt) { return s_eta[turn & 3][(wt * MT + mt) * 2 + half]; });
+      turn_over();
+    }
+  };
   if (u < units) {
     // the values that the first turn's weights, zeros, meet
     for (int i = tid; i < 16 * TOK; i += 512) (reinterpret_cast<uint4*>(s_main + S::TILE) + 16 * TOK)[i] = make_uint4(0u, 0u, 0u, 0u);
-    stage(0);
-    reconstruct(0, 0, 0);
-    load(u + step < units ? u + step : 0);
+    if (w < 4) {
+      each<QUADS>([&](auto qd) {
+        stage(std::true_type{}, qd.value);
+        begin(std::true_type{});
+        each<PIECES>([&](auto j) { reconstruct(std::true_type{}, qd, j, 0, 0, 0, 0); });
+      });
+      load(u + step);
+    }
     fresh = BLKS;
     __syncthreads();
-    if (w >= 4) turn_over();
-    for (; u < units; u += step, buf ^= 1) {
-      __builtin_amdgcn_s_setprio(1);
-      multiply(buf, p, sc, true);
-      const bool full = fresh == 32;
-      if (full || u + step >= units) {
-        if (wt == 0) bound_scores(rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(width_at(ring, half * 8 + ks, n32)); });
-        fresh = 0;
-        ring ^= 1;
-      }
-      __builtin_amdgcn_s_setprio(0);
+    if (w < 4) {
+      sealed_tiles(std::true_type{});
       turn_over();
-      if (u + step < units) stage(0);
-      softmax32<MT>(
-          rows, sc, p, (int64_t)(u + 1) * BLKS > a.nb, [&](int mt) { return (int64_t)u * BLKS + (wt * MT + mt) * 2 + half < a.nb ? 0xffffu : 0u; },
-          [&](int mt) { return s_eta[buf][(wt * MT + mt) * 2 + half]; });
-      if (u + step < units) {
-        reconstruct(buf ^ 1, ring, fresh);
-        load(u + 2 * step < units ? u + 2 * step : 0);
-        fresh += BLKS;
-      }
+    } else {
       turn_over();
+      sealed_tiles(std::false_type{});
     }
-    if (w < 4) turn_over();
-    multiply(buf, p, sc, false);
+    add_values(buf ^ 1);
   }
   rows.sealed = rows.sum;
   for (; u < all; u += step, buf ^= 1) {
@@ -736,7 +810,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
     }
   }
   __syncthreads();
-  if (w >= 4 && l == 0) s_norm[w - 4] = nu;
+  if (w < 4 && l == 0) s_norm[w] = nu;
   __syncthreads();
   rows.vmax = fmaxf(rows.vmax, fmaxf(fmaxf(s_norm[0], s_norm[1]), fmaxf(s_norm[2], s_norm[3])));
   end_rows(rows);
