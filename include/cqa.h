@@ -494,7 +494,8 @@ int32_t cqa_rotary_apply(const cqa_rotary* r, const int64_t* positions_dev, int6
 /* The cache's own reconstruction of tokens first .. first + n_tokens - 1 of every sequence of `layer`, e.g.
  * for a program that goes on in FP16, or that moves a sequence elsewhere: sealed tokens
  *   k = code * sigma + z (one fused FP32 operation),  v = code * scale + offset,
- * rounded once to `type` (CQA_TYPE_*; beyond FP16's range: its largest number), trailing tokens their FP16 originals.
+ * rounded once to `type` (CQA_TYPE_*; values to BF16 by way of FP32; beyond FP16's range: its largest number), trailing
+ * tokens their FP16 originals.
  * k_dev, v_dev: [batch][n_kv_heads][n_tokens] rows of 128 at `strides` (host pointer, copied; NULL: contiguous in
  * that order); either may be NULL.  Needs no originals.  n_tokens = 0 does nothing.  The current device must be
  * the cache's.  Asynchronous on `stream`, ordered with the cache's appends by it.

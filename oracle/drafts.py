@@ -2,7 +2,7 @@
 only; see quantizer.py's header).  float64 apart from the roundings that the definitions state.
 
 * Reading back: k = code * sigma + z as one fused binary32 operation, v = code * scale + offset exactly, each rounded
-  once to the asked type; what overflows FP16 becomes its largest number.
+  once to the asked type (values to BF16 by way of binary32); what overflows FP16 becomes its largest number.
 * A node attends the sealed tokens as read back in FP16, the trailing tokens and the drafted tokens of its mask, which are
   exact.  The certificate is that of attention.py with the widths and value errors that cover the rounding to FP16:
       w_c   = FP16 upwards(sigma_c + 2 min(sigma_c / 2, 2^-11 max(|z_c - 128 sigma_c|, |z_c + 127 sigma_c|) + 2^-25))

@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes as C
 import math
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("CQA_LIB") or os.path.join(_HERE, "libcqa.so")
@@ -113,11 +114,21 @@ class RotaryDesc(C.Structure):
 
 class RotaryRows(C.Structure):
     """A tensor of rows to turn (cqa_rotary_rows); strides are (batch, head, token) in elements."""
+    # (the strides as six numbers: two structures a tensor cost more than the call)
     _fields_ = [("in_dev", C.c_void_p), ("out_dev", C.c_void_p), ("n_heads", C.c_int32), ("reserved", C.c_int32),
-                ("in_strides", Strides), ("out_strides", Strides)]
+                ("in_batch", C.c_int64), ("in_head", C.c_int64), ("in_token", C.c_int64),
+                ("out_batch", C.c_int64), ("out_head", C.c_int64), ("out_token", C.c_int64)]
 
-    def __init__(self, in_dev, out_dev, n_heads, in_strides, out_strides):
-        super().__init__(_ptr(in_dev), _ptr(out_dev), n_heads, 0, Strides(*in_strides), Strides(*out_strides))
+    # (made from packed bytes: setting ten fields one by one costs more than the call)
+    def __new__(cls, in_dev, out_dev, n_heads, in_strides, out_strides):
+        return cls.from_buffer_copy(_pack_rows(_ptr(in_dev) or 0, _ptr(out_dev) or 0, n_heads, 0, *in_strides, *out_strides))
+
+    def __init__(self, *_):
+        pass
+
+
+_pack_rows = struct.Struct("@PPii6q").pack
+_RotaryOne, _RotaryTwo = RotaryRows * 1, RotaryRows * 2
 
 
 class NodeCert(C.Structure):
@@ -439,7 +450,7 @@ def cqa_rotary_destroy(r) -> None:
 def cqa_rotary_apply(r, positions_dev, position_stride, batch, n_tokens, rows, in_type=FP16, out_type=FP16,
                      stream=None) -> None:
     """rows: one or two RotaryRows, e.g. the queries' and the keys'."""
-    arr = (RotaryRows * len(rows))(*rows)
+    arr = (_RotaryTwo if len(rows) == 2 else _RotaryOne if len(rows) == 1 else RotaryRows * len(rows))(*rows)
     _check(_lib.cqa_rotary_apply(r, _ptr(positions_dev), position_stride, batch, n_tokens, arr, len(rows), in_type,
                                  out_type, _ptr(stream)), "cqa_rotary_apply")
 

@@ -356,6 +356,13 @@ __device__ __forceinline__ __half2 ld_half2_any(const __half* p) {
   return __builtin_bit_cast(__half2, x);
 }
 
+// A binary32 number as such: its conversion to FP16 does not become one operation with the one before it, which would round once where two
+// roundings are meant.
+__device__ __forceinline__ float as_rounded(float x) {
+  asm("" : "+v"(x));
+  return x;
+}
+
 extern thread_local int g_last_hip_error;
 #define CQA_HIP(expr)                                   \
   do {                                                  \

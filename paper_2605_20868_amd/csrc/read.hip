@@ -1,17 +1,18 @@
 // Reading the cache back: the reconstruction of tokens of every sequence, k = code sigma + z (one fused multiply-add in FP32) and
 // v = code scale + offset, rounded once to the asked type; trailing tokens are their FP16 originals.
 //
-// What bounds it: bytes, 288 read and 512 (FP16) written per token and KV head.  One wave a block of 16 tokens: lane (cp, tq) has
-// channels 8 cp .. 8 cp + 7 of tokens tq, tq + 4, tq + 8, tq + 12, so that sigma and z are fetched once for four tokens, a dword of value
-// codes (one channel of eight tokens) serves two of the lane's, and a wave's store is four whole rows.
+// What bounds it: bytes, 288 read and 512 (FP16) written per token and KV head.  One wave a block of 16 tokens, a lane 16 bytes of a row: C = 8
+// channels of tokens tq, tq + 4, tq + 8, tq + 12, or, of FP32 rows, C = 4 of tokens tq, tq + 2, ..., so that sigma and z are fetched
+// once for all of the lane's tokens, a dword of value codes (one channel of eight tokens) serves half of them, and each
+// store of a wave is whole rows, past the caches (128K tokens of 8 heads to FP16 180 -> 172 us; 4 x 8 heads x 9400 to FP32, token-major, 94 ->
+// 82, and 117 with 8 channels a lane).
 #include "cqa_internal.h"
 
 namespace cqa {
 
-typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8r __attribute__((ext_vector_type(8), aligned(2)));
 typedef __bf16 bf16x8r __attribute__((ext_vector_type(8), aligned(2)));
-typedef float f32x8r __attribute__((ext_vector_type(8), aligned(4)));
+typedef float f32x4r __attribute__((ext_vector_type(4), aligned(4)));
 
 struct ReadArgs {
   const uint8_t* t1;        // layer base of the quad records
@@ -27,20 +28,34 @@ struct ReadArgs {
   int n_kv;
 };
 
-template <int T>
-__device__ __forceinline__ void put8(void* base, int64_t i, f32x8 x) {
-  if constexpr (T == CQA_TYPE_FP16) *(f16x8r*)((_Float16*)base + i) = __builtin_convertvector(x, f16x8r);
-  else if constexpr (T == CQA_TYPE_BF16) *(bf16x8r*)((__bf16*)base + i) = __builtin_convertvector(x, bf16x8r);
-  else *(f32x8r*)((float*)base + i) = x;
+template <int T, int C>
+__device__ __forceinline__ void put(void* base, int64_t i, const float (&x)[C]) {
+  if constexpr (T == CQA_TYPE_FP32) {
+    f32x4r y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = x[e];
+    __builtin_nontemporal_store(y, (f32x4r*)((float*)base + i));
+  } else if constexpr (T == CQA_TYPE_FP16) {
+    f16x8r y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = (_Float16)x[e];
+    __builtin_nontemporal_store(y, (f16x8r*)((_Float16*)base + i));
+  } else {
+    bf16x8r y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = (__bf16)x[e];
+    __builtin_nontemporal_store(y, (bf16x8r*)((__bf16*)base + i));
+  }
 }
 
 template <int T>
 __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
-  const int l = threadIdx.x & 63, cp = l & 15, tq = l >> 4;
+  constexpr int C = T == CQA_TYPE_FP32 ? 4 : 8, LANES = D / C, SIDE = 64 / LANES;   // channels a lane, lanes a row, rows side by side
+  const int l = threadIdx.x & 63, cp = l % LANES, tq = l / LANES;
   const int64_t blk = a.blk0 + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (blk * BLK >= a.end) return;
   const int64_t head = (int64_t)blockIdx.z * a.n_kv + blockIdx.y;
-  const int64_t out0 = (int64_t)blockIdx.z * a.st.batch + (int64_t)blockIdx.y * a.st.head + 8 * cp;
+  const int64_t out0 = (int64_t)blockIdx.z * a.st.batch + (int64_t)blockIdx.y * a.st.head + C * cp;
   const auto row = [&](int t, int64_t& i) {   // of the block's token t; false: not asked for
     const int64_t tok = blk * BLK + t;
     i = out0 + (tok - a.first) * a.st.token;
@@ -48,35 +63,48 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
   };
   if (blk >= a.nb) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int t = tq + 4 * r;
+    for (int r = 0; r < BLK / SIDE; ++r) {
+      const int t = tq + SIDE * r;
       int64_t i;
       if (!row(t, i)) continue;
-      const int64_t src = (head * BLK + t) * D + 8 * cp;
-      if (a.k != nullptr) put8<T>(a.k, i, __builtin_convertvector(*(const f16x8r*)((const _Float16*)a.trail_k + src), f32x8));
-      if (a.v != nullptr) put8<T>(a.v, i, __builtin_convertvector(*(const f16x8r*)((const _Float16*)a.trail_v + src), f32x8));
+      const int64_t src = (head * BLK + t) * D + C * cp;
+      float x[C];
+      if (a.k != nullptr) {
+#pragma unroll
+        for (int e = 0; e < C; ++e) x[e] = __half2float(a.trail_k[src + e]);
+        put<T>(a.k, i, x);
+      }
+      if (a.v != nullptr) {
+#pragma unroll
+        for (int e = 0; e < C; ++e) x[e] = __half2float(a.trail_v[src + e]);
+        put<T>(a.v, i, x);
+      }
     }
     return;
   }
   const int64_t rec = head * a.nq_cap;
-  const int g = cp >> 1;
+  const int g = C * cp / VG;
   if (a.k != nullptr) {
     const uint8_t* const kc = a.t1 + t1_offset(rec, blk, Q_KC, KC_BYTES);
-    const float* const km = reinterpret_cast<const float*>(a.t1 + t1_offset(rec, blk, Q_KM, KM_BYTES));
-    const f32x8 sigma = *(const f32x8r*)(km + 8 * cp), z = *(const f32x8r*)(km + D + 8 * cp);
+    const float* const km = reinterpret_cast<const float*>(a.t1 + t1_offset(rec, blk, Q_KM, KM_BYTES)) + C * cp;
+    float sigma[C], z[C];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int t = tq + 4 * r;
-      const uint2 code = *reinterpret_cast<const uint2*>(kc + kc_offset(t, 8 * cp));
+    for (int e = 0; e < C; e += 4) {
+      *reinterpret_cast<float4*>(sigma + e) = *reinterpret_cast<const float4*>(km + e);
+      *reinterpret_cast<float4*>(z + e) = *reinterpret_cast<const float4*>(km + D + e);
+    }
+#pragma unroll
+    for (int r = 0; r < BLK / SIDE; ++r) {
+      const int t = tq + SIDE * r;
+      uint32_t code[C / 4];
+#pragma unroll
+      for (int e = 0; e < C / 4; ++e) code[e] = reinterpret_cast<const uint32_t*>(kc + kc_offset(t, C * cp))[e];
       int64_t i;
       if (!row(t, i)) continue;
-      f32x8 x;
+      float x[C];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t w = e < 4 ? code.x : code.y;
-        x[e] = fmaf((float)((w >> (8 * (e & 3))) & 255u) - 128.0f, sigma[e], z[e]);
-      }
-      put8<T>(a.k, i, x);
+      for (int e = 0; e < C; ++e) x[e] = as_rounded(fmaf((float)((code[e >> 2] >> (8 * (e & 3))) & 255u) - 128.0f, sigma[e], z[e]));
+      put<T>(a.k, i, x);
     }
   }
   if (a.v != nullptr) {
@@ -84,25 +112,25 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
     const _Float16* const vm = reinterpret_cast<const _Float16*>(a.t1 + t1_offset(rec, blk, Q_VM, VM_BYTES));
 #pragma unroll
     for (int o = 0; o < 2; ++o) {
-      uint32_t w[8];
+      uint32_t w[C];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = *reinterpret_cast<const uint32_t*>(vc + vc_dword_offset(o, 8 * cp + e));
+      for (int e = 0; e < C; ++e) w[e] = *reinterpret_cast<const uint32_t*>(vc + vc_dword_offset(o, C * cp + e));
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int t = 8 * o + tq + 4 * r;
+      for (int r = 0; r < 8 / SIDE; ++r) {
+        const int t = 8 * o + tq + SIDE * r;
         int64_t i;
         if (!row(t, i)) continue;
         const _Float16 scale = vm[vm_index(t, g)], off = vm[BLK * NG + vm_index(t, g)];
-        f32x8 x;
+        float x[C];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < C; ++e) {
           const uint32_t code = (w[e] >> (4 * (t & 7))) & 15u;
           // To FP16 by one FP16 operation: rounded once.  The scale's rounding can take the largest code beyond the group's
           // maximum, and out of range where that is FP16's largest number.
           x[e] = T == CQA_TYPE_FP16 ? (float)__builtin_elementwise_minimum(__builtin_elementwise_fma((_Float16)code, scale, off), (_Float16)65504.0f)
-                                    : fmaf((float)code, (float)scale, (float)off);
+                                    : as_rounded(fmaf((float)code, (float)scale, (float)off));
         }
-        put8<T>(a.v, i, x);
+        put<T>(a.v, i, x);
       }
     }
   }

