@@ -97,8 +97,10 @@ __device__ __forceinline__ uint4 paired(uint4 x) {
 // z and sigma are FP32, the largest code is the maximum within 2^-23).
 template <int I>
 __device__ __forceinline__ uint32_t value2(uint32_t codes, uint32_t scale, uint32_t off) {
-  const uint32_t biased = (codes >> (4 * I) & 0x000f000fu) | 0x64006400u;
-  const f16x2 code = __builtin_bit_cast(f16x2, biased) - __builtin_bit_cast(f16x2, 0x64006400u);
+  uint32_t bias = 0x64006400u;
+  asm("" : "+v"(bias));   // (in a register, so that mask and bias are one operation)
+  const uint32_t biased = (codes >> (4 * I) & 0x000f000fu) | bias;
+  const f16x2 code = __builtin_bit_cast(f16x2, biased) - __builtin_bit_cast(f16x2, bias);
   const f16x2 x = __builtin_elementwise_fma(code, __builtin_bit_cast(f16x2, scale), __builtin_bit_cast(f16x2, off));
   const f16x2 most = {(_Float16)F16_MAX, (_Float16)F16_MAX};
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_minimum(x, most));
@@ -222,10 +224,12 @@ __device__ __forceinline__ void bound_scores(TreeRows& w, Width width) {
   f32x16 d;
 #pragma unroll
   for (int r = 0; r < 16; ++r) d[r] = 0.0f;
+  uint32_t no_signs = 0x7fff7fffu;
+  asm volatile("" : "+s"(no_signs));   // |q| is formed here: kept over the callers' loops it would take 32 registers
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) {
     uint4 y = __builtin_bit_cast(uint4, w.q[ks]);
-    y.x &= 0x7fff7fffu, y.y &= 0x7fff7fffu, y.z &= 0x7fff7fffu, y.w &= 0x7fff7fffu;
+    y.x &= no_signs, y.y &= no_signs, y.z &= no_signs, y.w &= no_signs;
     d = __builtin_amdgcn_mfma_f32_32x32x16_f16(width(ks), __builtin_bit_cast(f16x8, y), d, 0, 0, 0);
   }
 #pragma unroll
@@ -706,7 +710,8 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   };
   // The products of a phase in their order, operands read AHEAD products ahead, and behind each some pieces of the reconstruction.  (Left to
   // the compiler, which cannot tell the tiles apart, each operand was read when it was needed: 3310 cycles a phase.)
-  constexpr int PRODUCTS = 16 * MT, AHEAD = 6, FROM = 2, EACH = (PIECES * QUADS + PRODUCTS - FROM - 1) / (PRODUCTS - FROM);
+  constexpr int PRODUCTS = 16 * MT, AHEAD = 6, FROM = 2, EACH = QUADS == 2 ? 4 : 2, BEHIND = FROM + PIECES * QUADS / EACH;
+  static_assert(PIECES * QUADS % EACH == 0 && BEHIND < PRODUCTS, "the pieces end ahead of the products");
   const auto sealed_tiles = [&](auto keys) {
     for (int turn = 0; u < units; u += step, buf ^= 1, ++turn) {
       const bool last = u + step >= units, full = fresh == 32;
@@ -755,9 +760,9 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
               reconstruct(keys, std::integral_constant<int, QD>{}, std::integral_constant<int, J>{}, keys.value ? buf ^ 1 : buf, ring1, slot, turn + 1);
             }
           });
+        if constexpr (I == BEHIND) load(keys.value ? u + 2 * step : u + step);
         __builtin_amdgcn_sched_barrier(0);
       });
-      load(keys.value ? u + 2 * step : u + step);
       if (full || last) {
         if (wt == 0) bound_scores(rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(width_at(ring, half * 8 + ks, n32)); });
       }
