@@ -347,6 +347,11 @@ __device__ __forceinline__ int group_shift(int n_q, int n_kv) { return n_q >= 4 
 typedef uint32_t u32_any __attribute__((aligned(2)));
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 __device__ __forceinline__ uint32_t ld4_any(const __half* p) { return *reinterpret_cast<const u32_any*>(p); }
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ uint2 ld8_any(const __half* p) {
+  const u32x2_any v = *reinterpret_cast<const u32x2_any*>(p);
+  return make_uint2(v.x, v.y);
+}
 __device__ __forceinline__ uint4 ld16_any(const __half* p) {
   const u32x4_any v = *reinterpret_cast<const u32x4_any*>(p);
   return make_uint4(v.x, v.y, v.z, v.w);

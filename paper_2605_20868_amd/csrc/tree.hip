@@ -68,7 +68,11 @@ struct TreeArgs {
   int n, words, trail;     // drafted nodes, mask words of one, trailing tokens
   int n_kv, group;
   int row_tiles;           // of 32 rows
-  int nsplit;              // partial sets per row
+  int nsplit;              // partial sets per row; 1: the split pass finishes the rows itself
+  __half* O;               // [Bt][n][Hq][128]
+  cqa_node_cert* cert;     // [Bt][n][Hq]
+  uint32_t* flags;
+  cqa_tolerances tol;
 };
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
@@ -280,9 +284,9 @@ __device__ __forceinline__ void load_exact(const TreeArgs& a, int64_t head, int 
     uint32_t x[8][2];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const __half* const p = token(a.trail_v, a.vd, t0 + oct * 8 + j) + c;
-      x[j][0] = ld4_any(p);
-      x[j][1] = ld4_any(p + 2);
+      const uint2 y = ld8_any(token(a.trail_v, a.vd, t0 + oct * 8 + j) + c);
+      x[j][0] = y.x;
+      x[j][1] = y.y;
     }
     float norm2 = 0.0f;
 #pragma unroll
@@ -326,9 +330,8 @@ __device__ __forceinline__ uint32_t open_tokens(const TreeArgs& a, int b, int no
   if (j < 0) x |= (1u << min(-j, BLK)) - 1u;
   return x & 0xffffu;
 }
-// ... with what the lane's row takes from them besides: the largest value norm, and no sum where one is not a number
-__device__ __forceinline__ uint32_t open_exact(TreeRows& w, const TreeArgs& a, int b, int first, const float* norms, const uint8_t* bad) {
-  const uint32_t bits = open_tokens(a, b, w.node, first);
+// What the lane's row takes from its open tokens besides: the largest value norm, and no sum where one is not a number
+__device__ __forceinline__ void open_exact(TreeRows& w, uint32_t bits, const float* norms, const uint8_t* bad) {
   uint32_t hit = 0u;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -338,7 +341,6 @@ __device__ __forceinline__ uint32_t open_exact(TreeRows& w, const TreeArgs& a, i
                                  fmaxf(bits >> (4 * i + 2) & 1u ? x.z : 0.0f, bits >> (4 * i + 3) & 1u ? x.w : 0.0f)));
   }
   if (bits & hit) w.sum = NAN;   // stays
-  return bits;
 }
 
 // Joins the halves of the rows.
@@ -414,6 +416,109 @@ __device__ __forceinline__ void join_sets(const float* sets, int stride, float* 
     st[T_VMAX * T_ROWS] = VM;
   }
 }
+// ---- rows whose sets are all there: outputs --------------------------------------------------------------------------------------------
+
+// Row r of a KV group among the outputs.
+__device__ __forceinline__ int64_t row_out(const TreeArgs& a, int head, int r) {
+  const int b = head / a.n_kv, kvh = head - b * a.n_kv, node = r / a.group;
+  return ((int64_t)b * a.n + node) * a.n_kv * a.group + kvh * a.group + (r - node * a.group);
+}
+// Four channels; whether one is no finite number.
+__device__ __forceinline__ bool put_channels(const TreeArgs& a, int64_t out, int c, float4 x, float inv) {
+  // (a mean of values: where the rounding of the weights takes it beyond FP16's range, the values' largest, it stays there)
+  const auto mean = [&](float v) { return v *= inv, isfinite(v) ? __builtin_amdgcn_fmed3f(v, -F16_MAX, F16_MAX) : v; };
+  const float y[4] = {mean(x.x), mean(x.y), mean(x.z), mean(x.w)};
+  reinterpret_cast<uint2*>(a.O + out * D)[c] = make_uint2(pack_f16(y[0], y[1]), pack_f16(y[2], y[3]));
+  return !(isfinite(y[0]) && isfinite(y[1]) && isfinite(y[2]) && isfinite(y[3]));
+}
+__device__ __forceinline__ float mean_factor(float L) { return L == 0.0f ? 0.0f : 1.0f / L; }   // 0: the row attends nothing
+__device__ __forceinline__ void put_certificate(const TreeArgs& a, int64_t out, float M, float L, float sealed, float E, float EM, float DM, float VM,
+                                                bool bad) {
+  const float inv = mean_factor(L);
+  const bool empty = L == 0.0f;
+  cqa_node_cert ct;
+  ct.E_val = E * inv;
+  ct.delta_h = DM;
+  ct.v_max = VM;
+  ct.alpha_tail_hat = sealed * inv;
+  ct.lse = empty ? -INFINITY : M * LN2 + logf(L);
+  ct.max_block_contrib = EM * inv;
+  ct.reserved = 0.0f;
+  float tail = 0.0f;
+  if (ct.alpha_tail_hat > 0.0f && DM != 0.0f)
+    tail = fminf(1.0f, expf((float)a.tol.mass_exp * DM) * ct.alpha_tail_hat) * expm1f(2.0f * DM);
+  const float full = tanhf(DM);
+  ct.E_key = 2.0f * VM * (a.tol.key_bound_mode == 0 ? fminf(full, tail) : (a.tol.key_bound_mode == 1 ? tail : full));
+  uint32_t fl = a.tol.force_flags;
+  if (ct.E_key > a.tol.eps_key) fl |= CQA_FLAG_KEY;
+  if (ct.E_val > a.tol.eps_val || ct.max_block_contrib > a.tol.v_tol) fl |= CQA_FLAG_VAL;
+  if (ct.E_key + ct.E_val > a.tol.eps_total) fl |= CQA_FLAG_TOTAL;
+  if (bad || !isfinite(ct.E_key) || !isfinite(ct.E_val) || !isfinite(DM) || !isfinite(VM) || (!empty && !isfinite(ct.lse))) fl |= CQA_FLAG_PRECOND;
+  a.cert[out] = ct;
+  a.flags[out] = fl;
+}
+// A wave's rows, from its registers.
+__device__ __forceinline__ void finish_rows(const TreeRows& w, const TreeArgs& a, int head, int tile) {
+  const int l = threadIdx.x & 63, half = l >> 5, r = tile * T_ROWS + (l & 31);
+  if (r >= a.n * a.group) return;   // (both halves)
+  const int64_t out = row_out(a, head, r);
+  const float inv = mean_factor(w.sum);
+  bool bad = false;
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4)
+      bad |= put_channels(a, out, (r4 >> 1) * 16 + ct * 4 + (r4 & 1) * 2 + half, make_float4(w.o[ct][4 * r4], w.o[ct][4 * r4 + 1], w.o[ct][4 * r4 + 2], w.o[ct][4 * r4 + 3]), inv);
+  bad = __shfl_xor((int)bad, 32) != 0 || bad;
+  if (half == 0) put_certificate(a, out, w.m, w.sum, w.sealed, w.ev, w.evmax, w.dmax, w.vmax, bad);
+}
+// ROWS rows from r32 = `first` of a tile on, of which all sets, up to N of them (n, `stride` floats apart), are at `sets`, by THREADS threads;
+// s_bad [ROWS] is zero and comes to say which rows have a channel that is no finite number.  Where CERT, only the certificate.
+template <int N, int ROWS, int THREADS, bool CERT>
+__device__ __forceinline__ void finish_sets(const float* sets, int64_t stride, int n, const TreeArgs& a, int head, int tile, int first, int tid, uint32_t* s_bad) {
+  const int row = tid % ROWS, r32 = first + row, r = tile * T_ROWS + r32;
+  if (r >= a.n * a.group || (CERT && tid >= ROWS)) return;
+  const int64_t out = row_out(a, head, r);
+  // (places behind the last set read it again, with weight 0: no request stands in a branch)
+  const auto quantity = [&](int i, int t) { return sets[(int64_t)min(i, n - 1) * stride + T_OFLOATS + t * T_ROWS + r32]; };
+  float f[N], l[N], M = -INFINITY, L = 0.0f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    f[i] = quantity(i, T_M);
+    l[i] = quantity(i, T_L);
+    M = fmaxf(M, f[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    f[i] = i >= n ? 0.0f : (f[i] == M ? 1.0f : __builtin_amdgcn_exp2f(f[i] - M));
+    L = fmaf(f[i], l[i], L);
+  }
+  if constexpr (CERT) {
+    float SL = 0.0f, E = 0.0f, EM = 0.0f, DM = 0.0f, VM = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      SL = fmaf(f[i], quantity(i, T_SEALED), SL);
+      E = fmaf(f[i], quantity(i, T_EV), E);
+      EM = fmaxf(EM, f[i] * quantity(i, T_EVMAX));
+      DM = fmaxf(DM, quantity(i, T_DMAX));
+      VM = fmaxf(VM, quantity(i, T_VMAX));
+    }
+    put_certificate(a, out, M, L, SL, E, EM, DM, VM, s_bad[row] != 0u);
+  } else {
+    const float inv = mean_factor(L);
+#pragma unroll
+    for (int c = tid / ROWS; c < 32; c += THREADS / ROWS) {
+      float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float4 y = reinterpret_cast<const float4*>(sets + (int64_t)min(i, n - 1) * stride)[c * T_ROWS + r32];
+        x.x = fmaf(f[i], y.x, x.x), x.y = fmaf(f[i], y.y, x.y), x.z = fmaf(f[i], y.z, x.z), x.w = fmaf(f[i], y.w, x.w);
+      }
+      if (put_channels(a, out, c, x, inv)) s_bad[row] = 1u;
+    }
+  }
+}
+
 __device__ __forceinline__ float* set_of(const TreeArgs& a, int64_t head, int tile, int split) {
   return a.part + ((head * a.row_tiles + tile) * a.nsplit + split) * T_FLOATS;
 }
@@ -423,14 +528,16 @@ __device__ __forceinline__ float* set_of(const TreeArgs& a, int64_t head, int ti
 // A wave takes pairs of blocks by itself and reconstructs them in registers, in the operands' layout: a 16-byte piece of key codes (16
 // channels of a token) is two operands' part of its lane, a dword of value codes (8 tokens of a channel) one.  Only the metadata, which 16
 // lanes share, goes through LDS, the wave's own part of it, so that no wave waits for another until the waves' sets are joined.
+constexpr int FEW_WAVES = 8;
 constexpr int FEW_KM_HALF = 64 + 4, FEW_KM_KIND = 2 * FEW_KM_HALF, FEW_KM_BLK = 2 * FEW_KM_KIND + 8;   // floats; padded: the four
 constexpr int FEW_VM_BLK = VM_BYTES + 32, FEW_W_BLK = 2 * D + 16;                                      // addresses of a read in four sets of banks
 constexpr int FEW_KM = 0, FEW_VM = FEW_KM + 2 * FEW_KM_BLK * 4, FEW_W = FEW_VM + 2 * FEW_VM_BLK, FEW_META_END = FEW_W + 2 * FEW_W_BLK;
 constexpr int FEW_K = 0, FEW_V = FEW_K + 32 * D * 2, FEW_NORM = FEW_V + 32 * D * 2, FEW_BAD = FEW_NORM + 32 * 4, FEW_EXACT_END = FEW_BAD + 32;
 static_assert(FEW_META_END <= T_FLOATS * 4 && FEW_EXACT_END <= T_FLOATS * 4 && FEW_VM % 16 == 0 && FEW_W % 16 == 0, "a wave's part of LDS");
 
-__global__ __launch_bounds__(256, 2) void tree_few_kernel(TreeArgs a) {
-  __shared__ __align__(16) float s_set[4][T_FLOATS];
+__global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
+  __shared__ __align__(16) float s_set[FEW_WAVES][T_FLOATS];
+  __shared__ uint32_t s_flag[T_ROWS];
   const int tid = threadIdx.x, l = tid & 63, n32 = l & 31, half = l >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t head = blockIdx.x;
@@ -442,9 +549,9 @@ __global__ __launch_bounds__(256, 2) void tree_few_kernel(TreeArgs a) {
   const uint8_t* const base = a.t1 + head * a.nq_cap * QUAD_BYTES;
   const int units = (int)((a.nb + 1) >> 1);                 // pairs of sealed blocks
   const int all = units + (a.trail + a.n + 31) / 32;        // ... and of 32 other tokens
-  const int step = 4 * a.nsplit;
+  const int step = FEW_WAVES * a.nsplit;
   const int bsel = (n32 >> 2) & 1, tok = (n32 >> 3) * 4 + (n32 & 3);   // the lane's token as a row of the keys' operand
-  uint4 kc[4], km[2], vc[2], vm;
+  uint4 kc[4], km0, km1, vc0, vc1, vm;   // (arrays of two went to LDS)
   float2 an;
   // (behind the last pair: the head's first, which is not used)
   const auto record = [&](int u) { return base + (int64_t)(u < units ? u >> 1 : 0) * QUAD_BYTES; };
@@ -454,18 +561,18 @@ __global__ __launch_bounds__(256, 2) void tree_few_kernel(TreeArgs a) {
     const uint8_t* const p = r + Q_KC + (b0 + bsel) * KC_BYTES + half * 1024 + tok * 16;
 #pragma unroll
     for (int i = 0; i < 4; ++i) kc[i] = *reinterpret_cast<const uint4*>(p + i * 256);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) km[i] = reinterpret_cast<const uint4*>(r + Q_KM + (b0 + i) * KM_BYTES)[l];
+    km0 = reinterpret_cast<const uint4*>(r + Q_KM + b0 * KM_BYTES)[l];
+    km1 = reinterpret_cast<const uint4*>(r + Q_KM + (b0 + 1) * KM_BYTES)[l];
     an = reinterpret_cast<const float2*>(r + Q_AN)[b0 + half];
   };
   const auto load_values = [&](int u) {
     const uint8_t* const r = record(u);
     const int b0 = (u & 1) * 2;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) vc[i] = reinterpret_cast<const uint4*>(r + Q_VC + (b0 + half) * VC_BYTES + i * 512)[n32];
+    vc0 = reinterpret_cast<const uint4*>(r + Q_VC + (b0 + half) * VC_BYTES)[n32];
+    vc1 = reinterpret_cast<const uint4*>(r + Q_VC + (b0 + half) * VC_BYTES + 512)[n32];
     vm = reinterpret_cast<const uint4*>(r + Q_VM + b0 * VM_BYTES)[l];
   };
-  int u = split * 4 + w;
+  int u = split * FEW_WAVES + w;
   load_keys(u);
   load_values(u);
   start_rows(rows, a, b, kvh, tile);
@@ -473,9 +580,9 @@ __global__ __launch_bounds__(256, 2) void tree_few_kernel(TreeArgs a) {
   for (; u < units; u += step) {
     // metadata: sigma and z by (block, kind, half of the channels), scales and offsets by block
     float* const skm = reinterpret_cast<float*>(mine + FEW_KM);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      *reinterpret_cast<uint4*>(skm + i * FEW_KM_BLK + half * FEW_KM_KIND + ((l >> 4) & 1) * FEW_KM_HALF + (l & 15) * 4) = km[i];
+    float* const at = skm + half * FEW_KM_KIND + ((l >> 4) & 1) * FEW_KM_HALF + (l & 15) * 4;
+    *reinterpret_cast<uint4*>(at) = km0;
+    *reinterpret_cast<uint4*>(at + FEW_KM_BLK) = km1;
     *reinterpret_cast<uint4*>(mine + FEW_VM + half * FEW_VM_BLK + n32 * 16) = paired(vm);
     wave_sync();
     // widths: four channels a lane
@@ -505,7 +612,8 @@ __global__ __launch_bounds__(256, 2) void tree_few_kernel(TreeArgs a) {
         },
         [&](int oct, int ct) {
           const uint8_t* const p = mine + FEW_VM + half * FEW_VM_BLK + oct * 128 + (n32 >> 4) * 64 + ct * 16;
-          const uint32_t c = ct == 0 ? vc[oct].x : (ct == 1 ? vc[oct].y : (ct == 2 ? vc[oct].z : vc[oct].w));
+          const uint4 v = oct ? vc1 : vc0;
+          const uint32_t c = ct == 0 ? v.x : (ct == 1 ? v.y : (ct == 2 ? v.z : v.w));
           return __builtin_bit_cast(f16x8, values8(c, *reinterpret_cast<const uint4*>(p), *reinterpret_cast<const uint4*>(p + 256)));
         });
     load_values(u + step);
@@ -514,6 +622,7 @@ __global__ __launch_bounds__(256, 2) void tree_few_kernel(TreeArgs a) {
   rows.sealed = rows.sum;
   for (; u < all; u += step) {
     const int t0 = (u - units) * 32;
+    const uint32_t bits = open_tokens(a, b, rows.node, t0 + half * BLK);
     uint8_t* const bad = mine + FEW_BAD;
     wave_sync();
     if (l < 8) reinterpret_cast<uint32_t*>(bad)[l] = 0u;
@@ -521,15 +630,22 @@ __global__ __launch_bounds__(256, 2) void tree_few_kernel(TreeArgs a) {
     load_exact<64, 32>(a, head, t0, l, reinterpret_cast<uint4*>(mine + FEW_K), reinterpret_cast<uint4*>(mine + FEW_V),
                        reinterpret_cast<float*>(mine + FEW_NORM), bad);
     wave_sync();
-    const uint32_t bits = open_exact(rows, a, b, t0 + half * BLK, reinterpret_cast<const float*>(mine + FEW_NORM) + half * BLK, bad + half * BLK);
+    open_exact(rows, bits, reinterpret_cast<const float*>(mine + FEW_NORM) + half * BLK, bad + half * BLK);
     attend32(
         rows, true, bits, 0.0f, [&](int ks) { return __builtin_bit_cast(f16x8, reinterpret_cast<const uint4*>(mine + FEW_K)[(half * 8 + ks) * 32 + n32]); },
         [] {}, [&](int oct, int ct) { return __builtin_bit_cast(f16x8, reinterpret_cast<const uint4*>(mine + FEW_V)[(half * 2 + oct) * D + ct * 32 + n32]); });
   }
   end_rows(rows);
   put_rows(rows, s_set[w]);
+  if (tid < T_ROWS) s_flag[tid] = 0u;
   __syncthreads();
-  join_sets<4, 256>(s_set[0], T_FLOATS, set_of(a, head, tile, split), tid);
+  if (a.nsplit > 1) {
+    join_sets<FEW_WAVES, 512>(s_set[0], T_FLOATS, set_of(a, head, tile, split), tid);
+    return;
+  }
+  finish_sets<FEW_WAVES, T_ROWS, 512, false>(s_set[0], T_FLOATS, FEW_WAVES, a, (int)head, tile, 0, tid, s_flag);
+  __syncthreads();
+  finish_sets<FEW_WAVES, T_ROWS, 512, true>(s_set[0], T_FLOATS, FEW_WAVES, a, (int)head, tile, 0, tid, s_flag);
 }
 
 // ---- more rows: bound by the products -------------------------------------------------------------------------------------------------
@@ -564,6 +680,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   __shared__ float s_eta[4][BLKS];
   __shared__ __align__(16) float s_norm[TOK];
   __shared__ __align__(16) uint8_t s_bad[TOK];
+  __shared__ uint32_t s_flag[32 * WR];
 
   const int tid = threadIdx.x, l = tid & 63, n32 = l & 31, half = l >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -802,6 +919,9 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   for (; u < all; u += step, buf ^= 1) {
     uint4* const s_k = reinterpret_cast<uint4*>(s_main + buf * S::TILE);
     uint4* const s_v = s_k + 16 * TOK;
+    uint32_t bits[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) bits[mt] = open_tokens(a, b, rows.node, (u - units) * TOK + ((wt * MT + mt) * 2 + half) * BLK);
     __syncthreads();   // norms and bad tokens of the last tile are done with
     if (tid < TOK) s_bad[tid] = 0;
     __syncthreads();
@@ -810,9 +930,9 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const int unit = wt * MT + mt, blk = unit * 2 + half;
-      const uint32_t bits = open_exact(rows, a, b, (u - units) * TOK + blk * BLK, s_norm + blk * BLK, s_bad + blk * BLK);
+      open_exact(rows, bits[mt], s_norm + blk * BLK, s_bad + blk * BLK);
       attend32(
-          rows, true, bits, 0.0f, [&](int ks) { return key_of(s_k, unit, ks); }, [] {}, [&](int oct, int ct) { return value_of(s_v, blk, oct, ct); });
+          rows, true, bits[mt], 0.0f, [&](int ks) { return key_of(s_k, unit, ks); }, [] {}, [&](int oct, int ct) { return value_of(s_v, blk, oct, ct); });
     }
   }
   __syncthreads();
@@ -821,33 +941,51 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   rows.vmax = fmaxf(rows.vmax, fmaxf(fmaxf(s_norm[0], s_norm[1]), fmaxf(s_norm[2], s_norm[3])));
   end_rows(rows);
   if constexpr (S::WT == 1) {
-    if (tile0 + wr < a.row_tiles) put_rows(rows, set_of(a, head, tile0 + wr, split));
+    if (tile0 + wr >= a.row_tiles) return;
+    if (a.nsplit > 1)
+      put_rows(rows, set_of(a, head, tile0 + wr, split));
+    else
+      finish_rows(rows, a, (int)head, tile0 + wr);
   } else {
     // the token waves' sets are joined through LDS
     float* const sets = reinterpret_cast<float*>(s_main);
     put_rows(rows, sets + w * T_FLOATS);
+    if (tid < 32 * WR) s_flag[tid] = 0u;
     __syncthreads();
     constexpr int PER = 512 / WR;   // threads a joined set: set i of row wave r is that of wave i * WR + r
     const int r = tid / PER;
-    if (tile0 + r < a.row_tiles) join_sets<S::WT, PER>(sets + r * T_FLOATS, WR * T_FLOATS, set_of(a, head, tile0 + r, split), tid % PER);
+    const bool there = tile0 + r < a.row_tiles;
+    if (a.nsplit > 1) {
+      if (there) join_sets<S::WT, PER>(sets + r * T_FLOATS, WR * T_FLOATS, set_of(a, head, tile0 + r, split), tid % PER);
+      return;
+    }
+    if (there)
+      finish_sets<S::WT, T_ROWS, PER, false>(sets + r * T_FLOATS, WR * T_FLOATS, S::WT, a, (int)head, tile0 + r, 0, tid % PER, s_flag + r * T_ROWS);
+    __syncthreads();
+    if (there)
+      finish_sets<S::WT, T_ROWS, PER, true>(sets + r * T_FLOATS, WR * T_FLOATS, S::WT, a, (int)head, tile0 + r, 0, tid % PER, s_flag + r * T_ROWS);
   }
 }
 
 // ---- joining the partial sets ---------------------------------------------------------------------------------------------------------
 
-struct TreeJoinArgs {
-  const float* part;
-  __half* O;               // [Bt][n][Hq][128]
-  cqa_node_cert* cert;     // [Bt][n][Hq]
-  uint32_t* flags;
-  cqa_tolerances tol;
-  int n, n_kv, group, row_tiles, nsplit;
-};
+// Few sets: eight rows a workgroup, four channels of one a thread.
+constexpr int JOIN_ROWS = 8, JOIN_FEW = 8;
+__global__ __launch_bounds__(256) void tree_join_few_kernel(TreeArgs a) {
+  __shared__ uint32_t s_bad[JOIN_ROWS];
+  const int head = blockIdx.x, tile = blockIdx.y >> 2, first = (blockIdx.y & 3) * JOIN_ROWS;
+  if (threadIdx.x < JOIN_ROWS) s_bad[threadIdx.x] = 0u;
+  __syncthreads();
+  const float* const sets = set_of(a, head, tile, 0);
+  finish_sets<JOIN_FEW, JOIN_ROWS, 256, false>(sets, T_FLOATS, a.nsplit, a, head, tile, first, threadIdx.x, s_bad);
+  __syncthreads();
+  finish_sets<JOIN_FEW, JOIN_ROWS, 256, true>(sets, T_FLOATS, a.nsplit, a, head, tile, first, threadIdx.x, s_bad);
+}
 
-// Eight rows a workgroup.  First every set's quantities of the rows, a set a thread, which gives the sets' weights; then the
+// Many sets: eight rows a workgroup.  First every set's quantities of the rows, a set a thread, which gives the sets' weights; then the
 // accumulators, four channels of a row and every fourth set a thread, the first of them requested ahead of the weights.
-constexpr int JOIN_ROWS = 8, JOIN_AHEAD = 8;
-__global__ __launch_bounds__(1024) void tree_join_kernel(TreeJoinArgs a) {
+constexpr int JOIN_AHEAD = 8;
+__global__ __launch_bounds__(1024) void tree_join_kernel(TreeArgs a) {
   extern __shared__ float s_f[];                     // [nsplit][JOIN_ROWS] weights
   __shared__ __align__(16) float4 s_o[4][32][JOIN_ROWS];
   __shared__ float s_m[16][JOIN_ROWS];
@@ -901,10 +1039,6 @@ __global__ __launch_bounds__(1024) void tree_join_kernel(TreeJoinArgs a) {
   for (int i = g + 4 * JOIN_AHEAD; i < a.nsplit; i += 4) add(s_f[i * JOIN_ROWS + row], channels(i));
   s_o[g][c][row] = x;
   __syncthreads();
-  const bool mine = r < a.n * a.group;
-  const int b = head / a.n_kv, kvh = head - b * a.n_kv, node = r / a.group;
-  const int64_t out = ((int64_t)b * a.n + node) * a.n_kv * a.group + kvh * a.group + (r - node * a.group);
-  float L = 0.0f, inv = 0.0f;
   if (tid < 256) {
 #pragma unroll
     for (int k = 1; k < 4; ++k) add(1.0f, s_o[k][c][row]);
@@ -914,42 +1048,11 @@ __global__ __launch_bounds__(1024) void tree_join_kernel(TreeJoinArgs a) {
 #pragma unroll
       for (int i = 1; i < 16; ++i) q[k] = k < 3 ? q[k] + s_q[i][k][row] : fmaxf(q[k], s_q[i][k][row]);
     }
-    L = q[0];
-    inv = L == 0.0f ? 0.0f : 1.0f / L;
-    // (a mean of values: where the rounding of the weights takes it beyond FP16's range, the values' largest, it stays there)
-    const auto mean = [&](float v) { return v *= inv, isfinite(v) ? __builtin_amdgcn_fmed3f(v, -F16_MAX, F16_MAX) : v; };
-    const f32x2 lo = {mean(x.x), mean(x.y)}, hi = {mean(x.z), mean(x.w)};
-    if (mine) {
-      reinterpret_cast<uint2*>(a.O + out * D)[c] =
-          make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, f16x2)), __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, f16x2)));
-      if (!(isfinite(lo[0]) && isfinite(lo[1]) && isfinite(hi[0]) && isfinite(hi[1]))) s_bad[row] = 1u;
-    }
+    if (r < a.n * a.group && put_channels(a, row_out(a, head, r), c, x, mean_factor(q[0]))) s_bad[row] = 1u;
   }
   __syncthreads();
-  if (tid >= JOIN_ROWS || !mine) return;
-  const bool empty = L == 0.0f;   // the row attends nothing
-  const float DM = q[4], VM = q[5];
-  cqa_node_cert ct;
-  ct.E_val = q[2] * inv;
-  ct.delta_h = DM;
-  ct.v_max = VM;
-  ct.alpha_tail_hat = q[1] * inv;
-  ct.lse = empty ? -INFINITY : M * LN2 + logf(L);
-  ct.max_block_contrib = q[3] * inv;
-  ct.reserved = 0.0f;
-  float tail = 0.0f;
-  if (ct.alpha_tail_hat > 0.0f && DM != 0.0f)
-    tail = fminf(1.0f, expf((float)a.tol.mass_exp * DM) * ct.alpha_tail_hat) * expm1f(2.0f * DM);
-  const float full = tanhf(DM);
-  ct.E_key = 2.0f * VM * (a.tol.key_bound_mode == 0 ? fminf(full, tail) : (a.tol.key_bound_mode == 1 ? tail : full));
-  uint32_t fl = a.tol.force_flags;
-  if (ct.E_key > a.tol.eps_key) fl |= CQA_FLAG_KEY;
-  if (ct.E_val > a.tol.eps_val || ct.max_block_contrib > a.tol.v_tol) fl |= CQA_FLAG_VAL;
-  if (ct.E_key + ct.E_val > a.tol.eps_total) fl |= CQA_FLAG_TOTAL;
-  if (s_bad[row] != 0u || !isfinite(ct.E_key) || !isfinite(ct.E_val) || !isfinite(DM) || !isfinite(VM) || (!empty && !isfinite(ct.lse)))
-    fl |= CQA_FLAG_PRECOND;
-  a.cert[out] = ct;
-  a.flags[out] = fl;
+  if (tid < JOIN_ROWS && r < a.n * a.group)
+    put_certificate(a, row_out(a, head, r), M, q[0], q[1], q[2], q[3], q[4], q[5], s_bad[row] != 0u);
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------------------
@@ -957,13 +1060,15 @@ __global__ __launch_bounds__(1024) void tree_join_kernel(TreeJoinArgs a) {
 // Rows of a KV group a workgroup takes.
 static int tree_rows(int n_rows) { return n_rows <= 32 ? 32 : (n_rows <= 64 ? 64 : (n_rows <= 128 ? 128 : 256)); }
 
-// Partial sets: as many workgroups as the device holds at a time, each with something to do at the cache's full length.
+// Partial sets: as many workgroups as the device holds at a time, each with something to do.  Short caches are one workgroup's, which finishes the
+// rows itself: up to two pairs of blocks a wave of few rows, or three tiles of more, take less than a second launch.
 static int tree_splits(int n_cu, int64_t heads, int n_rows, int n_draft, int64_t tokens) {
   const int rows = tree_rows(n_rows);
   const int64_t z = (n_rows + rows - 1) / rows;
-  const int64_t most = std::max<int64_t>(1, (rows == 32 ? 2 : 1) * (int64_t)n_cu / (heads * z));
-  const int64_t tok = rows == 32 || rows == 64 ? 128 : 64;   // of a workgroup's tile, or of its four waves' units
-  return (int)std::min(most, (tokens + n_draft + tok - 1) / tok);
+  const int64_t most = std::max<int64_t>(1, (int64_t)n_cu / (heads * z));
+  const int64_t tok = rows == 32 ? 32 * FEW_WAVES : (rows == 64 ? 128 : 64);   // of the waves' units, or of a tile
+  const int64_t tiles = (tokens + n_draft + tok - 1) / tok;
+  return tiles <= (rows == 32 ? 2 : 3) ? 1 : (int)std::min(most, tiles);
 }
 
 int64_t tree_ws_bytes(const Cache* c, int n_draft) {
@@ -1000,25 +1105,23 @@ int32_t launch_tree(const Cache* c, int layer, const __half* q, const __half* kd
   const int n_rows = n_draft * a.group;
   a.row_tiles = (n_rows + 31) / 32;
   a.nsplit = tree_splits(c->n_cu, heads, n_rows, n_draft, c->length[layer]);
+  a.O = O;
+  a.cert = cert;
+  a.flags = flags;
+  a.tol = tol;
   switch (tree_rows(n_rows)) {
-    case 32: tree_few_kernel<<<dim3((uint32_t)heads, (uint32_t)a.nsplit, 1), 256, 0, st>>>(a); break;
+    case 32: tree_few_kernel<<<dim3((uint32_t)heads, (uint32_t)a.nsplit, 1), 64 * FEW_WAVES, 0, st>>>(a); break;
     case 64: launch_many<2>(a, heads, st); break;
     case 128: launch_many<4>(a, heads, st); break;
     default: launch_many<8>(a, heads, st); break;
   }
   CQA_HIP(hipGetLastError());
-  TreeJoinArgs j;
-  j.part = ws;
-  j.O = O;
-  j.cert = cert;
-  j.flags = flags;
-  j.tol = tol;
-  j.n = n_draft;
-  j.n_kv = a.n_kv;
-  j.group = a.group;
-  j.row_tiles = a.row_tiles;
-  j.nsplit = a.nsplit;
-  tree_join_kernel<<<dim3((uint32_t)heads, (uint32_t)a.row_tiles * (32 / JOIN_ROWS)), 1024, (size_t)a.nsplit * JOIN_ROWS * 4, st>>>(j);
+  if (a.nsplit == 1) return CQA_OK;
+  const dim3 grid((uint32_t)heads, (uint32_t)a.row_tiles * (T_ROWS / JOIN_ROWS));
+  if (a.nsplit <= JOIN_FEW)
+    tree_join_few_kernel<<<grid, 256, 0, st>>>(a);
+  else
+    tree_join_kernel<<<grid, 1024, (size_t)a.nsplit * JOIN_ROWS * 4, st>>>(a);
   CQA_HIP(hipGetLastError());
   return CQA_OK;
 }
