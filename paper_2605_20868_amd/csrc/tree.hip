@@ -130,13 +130,22 @@ struct TreeRows {
   int node;
 };
 
-__device__ __forceinline__ void start_rows(TreeRows& s, const TreeArgs& a, int b, int kvh, int tile) {
+// Rows of the queries on their way to the operands: 16 lanes fetch a row, four rows a request (a lane that fetched its own operand's
+// pieces would ask for a line each), and the operands' pieces are read back, 16 bytes more between rows.
+constexpr int Q_ROW = D * 2 + 16, Q_TILE = T_ROWS * Q_ROW;
+__device__ __forceinline__ uint4 fetch_rows(const TreeArgs& a, int b, int kvh, int first) {
+  const int l = threadIdx.x & 63, r = min(first + (l >> 4), a.n * a.group - 1), node = r / a.group;
+  return ld16_any(a.q + (((int64_t)b * a.n + node) * a.n_kv * a.group + kvh * a.group + (r - node * a.group)) * D + (l & 15) * 8);
+}
+__device__ __forceinline__ void keep_rows(uint8_t* at, int row, uint4 x) {
   const int l = threadIdx.x & 63;
-  const int r = min(tile * 32 + (l & 31), a.n * a.group - 1);
-  s.node = r / a.group;
-  const __half* row = a.q + (((int64_t)b * a.n + s.node) * a.n_kv * a.group + kvh * a.group + (r - s.node * a.group)) * D + (l >> 5) * 64;
+  *reinterpret_cast<uint4*>(at + (row + (l >> 4)) * Q_ROW + (l & 15) * 16) = x;
+}
+__device__ __forceinline__ void start_rows(TreeRows& s, const TreeArgs& a, int tile, const uint8_t* at) {
+  const int l = threadIdx.x & 63;
+  s.node = min(tile * T_ROWS + (l & 31), a.n * a.group - 1) / a.group;
 #pragma unroll
-  for (int ks = 0; ks < 8; ++ks) s.q[ks] = __builtin_bit_cast(f16x8, ld16_any(row + ks * 8));
+  for (int ks = 0; ks < 8; ++ks) s.q[ks] = *reinterpret_cast<const f16x8*>(at + (l & 31) * Q_ROW + ((l >> 5) * 8 + ks) * 16);
   s.m = -INFINITY;
   s.sum = s.sealed = s.ev = s.evmax = s.dmax = s.vmax = 0.0f;
 #pragma unroll
@@ -254,17 +263,29 @@ template <int THREADS, int TOK>
 __device__ __forceinline__ void load_exact(const TreeArgs& a, int64_t head, int t0, int tid, uint4* keys, uint4* values, float* norms, uint8_t* bad) {
   const int total = a.trail + a.n;
   const auto finite = [](uint32_t x) { return (uint32_t)((x & 0x7c00u) != 0x7c00u) & (uint32_t)((x & 0x7c000000u) != 0x7c000000u); };
-  // (every address is a token's: the requests stand in no branch)
+  // (every address is a token's: the requests stand in no branch, and all come first)
+  const __half* const tk = a.trail_k + head * BLK * D;
+  const __half* const tv = a.trail_v + head * BLK * D;
+  const __half* const dk = a.kd + (head * a.n - a.trail) * D;
+  const __half* const dv = a.vd + (head * a.n - a.trail) * D;
   const auto token = [&](const __half* trail, const __half* drafts, int pos) {
     pos = min(pos, total - 1);
-    return pos < a.trail ? trail + (head * BLK + pos) * D : drafts + (head * a.n + pos - a.trail) * D;
+    return (pos < a.trail ? trail : drafts) + pos * D;
   };
-  constexpr int NK = TOK * 16 / THREADS;
+  constexpr int NK = TOK * 16 / THREADS, NV = (TOK * 4 + THREADS - 1) / THREADS;
   uint4 kx[NK];
+  uint2 vx[NV][8];
 #pragma unroll
   for (int k = 0; k < NK; ++k) {
     const int i = tid + k * THREADS;
-    kx[k] = ld16_any(token(a.trail_k, a.kd, t0 + (i >> 4)) + (i & 15) * 8);
+    kx[k] = ld16_any(token(tk, dk, t0 + (i >> 4)) + (i & 15) * 8);
+  }
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int i = tid + k * THREADS;
+    if (THREADS > TOK * 4 && i >= TOK * 4) break;   // (whole waves)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) vx[k][j] = ld8_any(token(tv, dv, t0 + (i >> 5) * 8 + j) + (i & 31) * 4);
   }
 #pragma unroll
   for (int k = 0; k < NK; ++k) {
@@ -278,15 +299,14 @@ __device__ __forceinline__ void load_exact(const TreeArgs& a, int64_t head, int 
   }
   // four channels of eight tokens
 #pragma unroll
-  for (int k = 0; k < (TOK * 4 + THREADS - 1) / THREADS; ++k) {
+  for (int k = 0; k < NV; ++k) {
     const int i = tid + k * THREADS, oct = i >> 5, c = (i & 31) * 4;
-    if (THREADS > TOK * 4 && i >= TOK * 4) break;   // (whole waves)
+    if (THREADS > TOK * 4 && i >= TOK * 4) break;
     uint32_t x[8][2];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const uint2 y = ld8_any(token(a.trail_v, a.vd, t0 + oct * 8 + j) + c);
-      x[j][0] = y.x;
-      x[j][1] = y.y;
+      x[j][0] = vx[k][j].x;
+      x[j][1] = vx[k][j].y;
     }
     float norm2 = 0.0f;
 #pragma unroll
@@ -532,11 +552,15 @@ constexpr int FEW_WAVES = 8;
 constexpr int FEW_KM_HALF = 64 + 4, FEW_KM_KIND = 2 * FEW_KM_HALF, FEW_KM_BLK = 2 * FEW_KM_KIND + 8;   // floats; padded: the four
 constexpr int FEW_VM_BLK = VM_BYTES + 32, FEW_W_BLK = 2 * D + 16;                                      // addresses of a read in four sets of banks
 constexpr int FEW_KM = 0, FEW_VM = FEW_KM + 2 * FEW_KM_BLK * 4, FEW_W = FEW_VM + 2 * FEW_VM_BLK, FEW_META_END = FEW_W + 2 * FEW_W_BLK;
-constexpr int FEW_K = 0, FEW_V = FEW_K + 32 * D * 2, FEW_NORM = FEW_V + 32 * D * 2, FEW_BAD = FEW_NORM + 32 * 4, FEW_EXACT_END = FEW_BAD + 32;
-static_assert(FEW_META_END <= T_FLOATS * 4 && FEW_EXACT_END <= T_FLOATS * 4 && FEW_VM % 16 == 0 && FEW_W % 16 == 0, "a wave's part of LDS");
+constexpr int FEW_EXACT = 64;   // trailing tokens and, as many as a group of 32 rows has nodes, drafted ones
+static_assert(BLK - 1 + T_ROWS <= FEW_EXACT && FEW_META_END <= T_FLOATS * 4 && 2 * FEW_EXACT * D * 2 <= 2 * T_FLOATS * 4 && FEW_VM % 16 == 0 && FEW_W % 16 == 0, "a wave's part of LDS");
 
 __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
+  fetch_args<sizeof(TreeArgs)>();
   __shared__ __align__(16) float s_set[FEW_WAVES][T_FLOATS];
+  __shared__ __align__(16) uint8_t s_q[Q_TILE];
+  __shared__ __align__(16) float s_norm[FEW_EXACT];
+  __shared__ __align__(16) uint8_t s_bad[FEW_EXACT];
   __shared__ uint32_t s_flag[T_ROWS];
   const int tid = threadIdx.x, l = tid & 63, n32 = l & 31, half = l >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -548,7 +572,6 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
 
   const uint8_t* const base = a.t1 + head * a.nq_cap * QUAD_BYTES;
   const int units = (int)((a.nb + 1) >> 1);                 // pairs of sealed blocks
-  const int all = units + (a.trail + a.n + 31) / 32;        // ... and of 32 other tokens
   const int step = FEW_WAVES * a.nsplit;
   const int bsel = (n32 >> 2) & 1, tok = (n32 >> 3) * 4 + (n32 & 3);   // the lane's token as a row of the keys' operand
   uint4 kc[4], km0, km1, vc0, vc1, vm;   // (arrays of two went to LDS)
@@ -573,9 +596,12 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
     vm = reinterpret_cast<const uint4*>(r + Q_VM + b0 * VM_BYTES)[l];
   };
   int u = split * FEW_WAVES + w;
+  const uint4 q_in = fetch_rows(a, b, kvh, tile * T_ROWS + 4 * w);
   load_keys(u);
   load_values(u);
-  start_rows(rows, a, b, kvh, tile);
+  keep_rows(s_q, 4 * w, q_in);
+  __syncthreads();
+  start_rows(rows, a, tile, s_q);
 
   for (; u < units; u += step) {
     // metadata: sigma and z by (block, kind, half of the channels), scales and offsets by block
@@ -620,20 +646,23 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
     wave_sync();
   }
   rows.sealed = rows.sum;
-  for (; u < all; u += step) {
-    const int t0 = (u - units) * 32;
-    const uint32_t bits = open_tokens(a, b, rows.node, t0 + half * BLK);
-    uint8_t* const bad = mine + FEW_BAD;
-    wave_sync();
-    if (l < 8) reinterpret_cast<uint32_t*>(bad)[l] = 0u;
-    wave_sync();
-    load_exact<64, 32>(a, head, t0, l, reinterpret_cast<uint4*>(mine + FEW_K), reinterpret_cast<uint4*>(mine + FEW_V),
-                       reinterpret_cast<float*>(mine + FEW_NORM), bad);
-    wave_sync();
-    open_exact(rows, bits, reinterpret_cast<const float*>(mine + FEW_NORM) + half * BLK, bad + half * BLK);
-    attend32(
-        rows, true, bits, 0.0f, [&](int ks) { return __builtin_bit_cast(f16x8, reinterpret_cast<const uint4*>(mine + FEW_K)[(half * 8 + ks) * 32 + n32]); },
-        [] {}, [&](int oct, int ct) { return __builtin_bit_cast(f16x8, reinterpret_cast<const uint4*>(mine + FEW_V)[(half * 2 + oct) * D + ct * 32 + n32]); });
+  // The other tokens are the workgroup's whose turn is the next: it fetches them together, and two of its waves attend them.
+  if (split == (units + FEW_WAVES - 1) / FEW_WAVES % a.nsplit) {
+    uint4* const s_k = reinterpret_cast<uint4*>(s_set);
+    uint4* const s_v = s_k + 16 * FEW_EXACT;
+    const uint32_t bits = open_tokens(a, b, rows.node, (2 * w + half) * BLK);
+    if (tid < FEW_EXACT / 4) reinterpret_cast<uint32_t*>(s_bad)[tid] = 0u;
+    __syncthreads();
+    load_exact<64 * FEW_WAVES, FEW_EXACT>(a, head, 0, tid, s_k, s_v, s_norm, s_bad);
+    __syncthreads();
+    if (w * 32 < a.trail + a.n) {
+      const int blk = 2 * w + half;
+      open_exact(rows, bits, s_norm + blk * BLK, s_bad + blk * BLK);
+      attend32(
+          rows, true, bits, 0.0f, [&](int ks) { return __builtin_bit_cast(f16x8, s_k[(half * 8 + ks) * FEW_EXACT + w * 32 + n32]); }, [] {},
+          [&](int oct, int ct) { return __builtin_bit_cast(f16x8, s_v[(blk * 2 + oct) * D + ct * 32 + n32]); });
+    }
+    __syncthreads();   // (the waves' sets come where the tokens are)
   }
   end_rows(rows);
   put_rows(rows, s_set[w]);
@@ -674,6 +703,7 @@ struct ManyShape {
 
 template <int WR>
 __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
+  fetch_args<sizeof(TreeArgs)>();
   using S = ManyShape<WR>;
   constexpr int MT = S::MT, TOK = S::TOK, QUADS = S::QUADS, BLKS = S::BLKS;
   __shared__ __align__(16) uint8_t s_main[S::BYTES];
@@ -723,7 +753,17 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   };
   int u = split;
   load(u);
-  start_rows(rows, a, b, kvh, tile0 + wr);
+  {
+    static_assert(8 * Q_TILE <= S::WIDTH_AT, "the queries' way leads past the widths");
+    uint8_t* const s_q = s_main + w * Q_TILE;
+    uint4 x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = fetch_rows(a, b, kvh, (tile0 + wr) * T_ROWS + 4 * i);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) keep_rows(s_q, 4 * i, x[i]);
+    wave_sync();
+    start_rows(rows, a, tile0 + wr, s_q);
+  }
   for (int i = tid; i < 2 * 32 * D * 2 / 4; i += 512) reinterpret_cast<uint32_t*>(s_main + S::WIDTH_AT)[i] = 0u;
   int fresh = 0, ring = 0;   // blocks whose widths have come into the half `ring`
   int buf = 0;
