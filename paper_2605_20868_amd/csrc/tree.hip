@@ -69,6 +69,7 @@ struct TreeArgs {
   int n_kv, group;
   int row_tiles;           // of 32 rows
   int nsplit;              // partial sets per row; 1: the split pass finishes the rows itself
+  int share, over, least, last;   // more rows: sealed tiles of a workgroup, how many have one more, those of the `last` workgroups
   __half* O;               // [Bt][n][Hq][128]
   cqa_node_cert* cert;     // [Bt][n][Hq]
   uint32_t* flags;
@@ -726,9 +727,9 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
 
   const uint8_t* const base = a.t1 + head * a.nq_cap * QUAD_BYTES;
   const int nquads = (int)((a.nb + 3) >> 2);
-  const int units = (nquads + QUADS - 1) / QUADS;
-  const int all = units + (a.trail + a.n + TOK - 1) / TOK;
-  const int step = a.nsplit;
+  const int even = a.nsplit - a.last, mid = min(split, even);
+  const int from = mid * a.share + min(mid, a.over) + (split - mid) * a.least;
+  const int units = from + (split < even ? a.share + (split < a.over) : a.least);   // the workgroup's tiles: from .. units - 1
   // the wave's block of each quad of the tile: keys, lane (run pair c8, token t8) has 16 channels of tokens t8 and t8 + 8; values, lane (octet
   // oc, n = gh 16 + n16) has four channels of eight tokens
   const int t8 = l & 7, c8 = l >> 3;
@@ -751,7 +752,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
       an[qd] = reinterpret_cast<const float2*>(r + Q_AN)[wb];
     }
   };
-  int u = split;
+  int u = from;
   load(u);
   {
     static_assert(8 * Q_TILE <= S::WIDTH_AT, "the queries' way leads past the widths");
@@ -870,8 +871,8 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   constexpr int PRODUCTS = 16 * MT, AHEAD = 6, FROM = 2, EACH = QUADS == 2 ? 4 : 2, BEHIND = FROM + PIECES * QUADS / EACH;
   static_assert(PIECES * QUADS % EACH == 0 && BEHIND < PRODUCTS, "the pieces end ahead of the products");
   const auto sealed_tiles = [&](auto keys) {
-    for (int turn = 0; u < units; u += step, buf ^= 1, ++turn) {
-      const bool last = u + step >= units, full = fresh == 32;
+    for (int turn = 0; u < units; ++u, buf ^= 1, ++turn) {
+      const bool last = u + 1 >= units, full = fresh == 32;
       const int ring1 = full ? ring ^ 1 : ring, slot = full ? 0 : fresh;   // where the next tile's widths go
       const uint4* const s_k = reinterpret_cast<const uint4*>(s_main + buf * S::TILE);
       const uint4* const s_v = reinterpret_cast<const uint4*>(s_main + (buf ^ 1) * S::TILE) + 16 * TOK;
@@ -917,7 +918,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
               reconstruct(keys, std::integral_constant<int, QD>{}, std::integral_constant<int, J>{}, keys.value ? buf ^ 1 : buf, ring1, slot, turn + 1);
             }
           });
-        if constexpr (I == BEHIND) load(keys.value ? u + 2 * step : u + step);
+        if constexpr (I == BEHIND) load(keys.value ? u + 2 : u + 1);
         __builtin_amdgcn_sched_barrier(0);
       });
       if (full || last) {
@@ -942,7 +943,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
         begin(std::true_type{});
         each<PIECES>([&](auto j) { reconstruct(std::true_type{}, qd, j, 0, 0, 0, 0); });
       });
-      load(u + step);
+      load(u + 1);
     }
     fresh = BLKS;
     __syncthreads();
@@ -956,16 +957,17 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
     add_values(buf ^ 1);
   }
   rows.sealed = rows.sum;
-  for (; u < all; u += step, buf ^= 1) {
+  // the other tokens' tiles: dealt to the workgroups from the last one down
+  for (int t0 = (a.nsplit - 1 - split) * TOK; t0 < a.trail + a.n; t0 += a.nsplit * TOK, buf ^= 1) {
     uint4* const s_k = reinterpret_cast<uint4*>(s_main + buf * S::TILE);
     uint4* const s_v = s_k + 16 * TOK;
     uint32_t bits[MT];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) bits[mt] = open_tokens(a, b, rows.node, (u - units) * TOK + ((wt * MT + mt) * 2 + half) * BLK);
+    for (int mt = 0; mt < MT; ++mt) bits[mt] = open_tokens(a, b, rows.node, t0 + ((wt * MT + mt) * 2 + half) * BLK);
     __syncthreads();   // norms and bad tokens of the last tile are done with
     if (tid < TOK) s_bad[tid] = 0;
     __syncthreads();
-    load_exact<512, TOK>(a, head, (u - units) * TOK, tid, s_k, s_v, s_norm, s_bad);
+    load_exact<512, TOK>(a, head, t0, tid, s_k, s_v, s_norm, s_bad);
     __syncthreads();
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -1100,15 +1102,30 @@ __global__ __launch_bounds__(1024) void tree_join_kernel(TreeArgs a) {
 // Rows of a KV group a workgroup takes.
 static int tree_rows(int n_rows) { return n_rows <= 32 ? 32 : (n_rows <= 64 ? 64 : (n_rows <= 128 ? 128 : 256)); }
 
+static int tile_tokens(int rows) { return rows == 64 ? 128 : 64; }   // of more than 32 rows
+
 // Partial sets: as many workgroups as the device holds at a time, each with something to do.  Short caches are one workgroup's, which finishes the
 // rows itself: up to two pairs of blocks a wave of few rows, or three tiles of more, take less than a second launch.
 static int tree_splits(int n_cu, int64_t heads, int n_rows, int n_draft, int64_t tokens) {
   const int rows = tree_rows(n_rows);
   const int64_t z = (n_rows + rows - 1) / rows;
   const int64_t most = std::max<int64_t>(1, (int64_t)n_cu / (heads * z));
-  const int64_t tok = rows == 32 ? 32 * FEW_WAVES : (rows == 64 ? 128 : 64);   // of the waves' units, or of a tile
+  const int64_t tok = rows == 32 ? 32 * FEW_WAVES : tile_tokens(rows);   // of the waves' units, or of a tile
   const int64_t tiles = (tokens + n_draft + tok - 1) / tok;
   return tiles <= (rows == 32 ? 2 : 3) ? 1 : (int)std::min(most, tiles);
+}
+
+// Sealed tiles of more than 32 rows by workgroup: the trailing and drafted tokens' tiles are the last workgroups', EXACT tiles' work each, and
+// the sealed ones are dealt so that all end together.
+constexpr int EXACT = 3;
+static void tree_shares(TreeArgs& a, int n_rows) {
+  const int tok = tile_tokens(tree_rows(n_rows));
+  const int tiles = (int)(((a.nb + 3) / 4 * 64 + tok - 1) / tok), exact = (a.trail + a.n + tok - 1) / tok;
+  a.last = exact < a.nsplit ? exact : 0;
+  a.least = std::max(0, (tiles + EXACT * exact) / a.nsplit - EXACT);
+  const int rest = tiles - a.last * a.least, even = a.nsplit - a.last;
+  a.share = rest / even;
+  a.over = rest % even;
 }
 
 int64_t tree_ws_bytes(const Cache* c, int n_draft) {
@@ -1145,6 +1162,7 @@ int32_t launch_tree(const Cache* c, int layer, const __half* q, const __half* kd
   const int n_rows = n_draft * a.group;
   a.row_tiles = (n_rows + 31) / 32;
   a.nsplit = tree_splits(c->n_cu, heads, n_rows, n_draft, c->length[layer]);
+  tree_shares(a, n_rows);
   a.O = O;
   a.cert = cert;
   a.flags = flags;
