@@ -453,11 +453,15 @@ __device__ __forceinline__ bool put_channels(const TreeArgs& a, int64_t out, int
   return !(isfinite(y[0]) && isfinite(y[1]) && isfinite(y[2]) && isfinite(y[3]));
 }
 __device__ __forceinline__ float mean_factor(float L) { return L == 0.0f ? 0.0f : 1.0f / L; }   // 0: the row attends nothing
-__device__ __forceinline__ void put_certificate(const TreeArgs& a, int64_t out, float M, float L, float sealed, float E, float EM, float DM, float VM,
-                                                bool bad) {
+struct Certificate {
+  cqa_node_cert ct;
+  uint32_t flags;
+};
+__device__ __forceinline__ Certificate certificate(const TreeArgs& a, float M, float L, float sealed, float E, float EM, float DM, float VM) {
   const float inv = mean_factor(L);
   const bool empty = L == 0.0f;
-  cqa_node_cert ct;
+  Certificate x;
+  cqa_node_cert& ct = x.ct;
   ct.E_val = E * inv;
   ct.delta_h = DM;
   ct.v_max = VM;
@@ -474,9 +478,13 @@ __device__ __forceinline__ void put_certificate(const TreeArgs& a, int64_t out, 
   if (ct.E_key > a.tol.eps_key) fl |= CQA_FLAG_KEY;
   if (ct.E_val > a.tol.eps_val || ct.max_block_contrib > a.tol.v_tol) fl |= CQA_FLAG_VAL;
   if (ct.E_key + ct.E_val > a.tol.eps_total) fl |= CQA_FLAG_TOTAL;
-  if (bad || !isfinite(ct.E_key) || !isfinite(ct.E_val) || !isfinite(DM) || !isfinite(VM) || (!empty && !isfinite(ct.lse))) fl |= CQA_FLAG_PRECOND;
-  a.cert[out] = ct;
-  a.flags[out] = fl;
+  if (!isfinite(ct.E_key) || !isfinite(ct.E_val) || !isfinite(DM) || !isfinite(VM) || (!empty && !isfinite(ct.lse))) fl |= CQA_FLAG_PRECOND;
+  x.flags = fl;
+  return x;
+}
+__device__ __forceinline__ void put_certificate(const TreeArgs& a, int64_t out, const Certificate& x, bool bad) {
+  a.cert[out] = x.ct;
+  a.flags[out] = x.flags | (bad ? CQA_FLAG_PRECOND : 0u);
 }
 // A wave's rows, from its registers.
 __device__ __forceinline__ void finish_rows(const TreeRows& w, const TreeArgs& a, int head, int tile) {
@@ -491,53 +499,60 @@ __device__ __forceinline__ void finish_rows(const TreeRows& w, const TreeArgs& a
     for (int r4 = 0; r4 < 4; ++r4)
       bad |= put_channels(a, out, (r4 >> 1) * 16 + ct * 4 + (r4 & 1) * 2 + half, make_float4(w.o[ct][4 * r4], w.o[ct][4 * r4 + 1], w.o[ct][4 * r4 + 2], w.o[ct][4 * r4 + 3]), inv);
   bad = __shfl_xor((int)bad, 32) != 0 || bad;
-  if (half == 0) put_certificate(a, out, w.m, w.sum, w.sealed, w.ev, w.evmax, w.dmax, w.vmax, bad);
+  if (half == 0) put_certificate(a, out, certificate(a, w.m, w.sum, w.sealed, w.ev, w.evmax, w.dmax, w.vmax), bad);
 }
-// ROWS rows from r32 = `first` of a tile on, of which all sets, up to N of them (n, `stride` floats apart), are at `sets`, by THREADS threads;
-// s_bad [ROWS] is zero and comes to say which rows have a channel that is no finite number.  Where CERT, only the certificate.
-template <int N, int ROWS, int THREADS, bool CERT>
+// ROWS rows from r32 = `first` of a tile on, of which all sets, up to N of them (n, `stride` floats apart), are at `sets`, by THREADS threads:
+// the last 64 have the certificates, the others the channels.  Every thread of the workgroup comes here, for the barrier; s_bad [ROWS] is zero
+// and comes to say which rows have a channel that is no finite number.
+template <int N, int ROWS, int THREADS>
 __device__ __forceinline__ void finish_sets(const float* sets, int64_t stride, int n, const TreeArgs& a, int head, int tile, int first, int tid, uint32_t* s_bad) {
+  constexpr int WIDE = THREADS - 64;
+  static_assert(WIDE > 0 && WIDE % ROWS == 0 && ROWS <= 64, "whole rows");
   const int row = tid % ROWS, r32 = first + row, r = tile * T_ROWS + r32;
-  if (r >= a.n * a.group || (CERT && tid >= ROWS)) return;
+  const bool there = r < a.n * a.group, certifies = there && tid >= WIDE && tid < WIDE + ROWS;
   const int64_t out = row_out(a, head, r);
   // (places behind the last set read it again, with weight 0: no request stands in a branch)
   const auto quantity = [&](int i, int t) { return sets[(int64_t)min(i, n - 1) * stride + T_OFLOATS + t * T_ROWS + r32]; };
-  float f[N], l[N], M = -INFINITY, L = 0.0f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    f[i] = quantity(i, T_M);
-    l[i] = quantity(i, T_L);
-    M = fmaxf(M, f[i]);
-  }
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    f[i] = i >= n ? 0.0f : (f[i] == M ? 1.0f : __builtin_amdgcn_exp2f(f[i] - M));
-    L = fmaf(f[i], l[i], L);
-  }
-  if constexpr (CERT) {
-    float SL = 0.0f, E = 0.0f, EM = 0.0f, DM = 0.0f, VM = 0.0f;
+  Certificate ct;
+  if (there && (tid < WIDE || certifies)) {
+    float f[N], l[N], M = -INFINITY, L = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      SL = fmaf(f[i], quantity(i, T_SEALED), SL);
-      E = fmaf(f[i], quantity(i, T_EV), E);
-      EM = fmaxf(EM, f[i] * quantity(i, T_EVMAX));
-      DM = fmaxf(DM, quantity(i, T_DMAX));
-      VM = fmaxf(VM, quantity(i, T_VMAX));
+      f[i] = quantity(i, T_M);
+      l[i] = quantity(i, T_L);
+      M = fmaxf(M, f[i]);
     }
-    put_certificate(a, out, M, L, SL, E, EM, DM, VM, s_bad[row] != 0u);
-  } else {
-    const float inv = mean_factor(L);
 #pragma unroll
-    for (int c = tid / ROWS; c < 32; c += THREADS / ROWS) {
-      float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int i = 0; i < N; ++i) {
+      f[i] = i >= n ? 0.0f : (f[i] == M ? 1.0f : __builtin_amdgcn_exp2f(f[i] - M));
+      L = fmaf(f[i], l[i], L);
+    }
+    if (certifies) {
+      float SL = 0.0f, E = 0.0f, EM = 0.0f, DM = 0.0f, VM = 0.0f;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float4 y = reinterpret_cast<const float4*>(sets + (int64_t)min(i, n - 1) * stride)[c * T_ROWS + r32];
-        x.x = fmaf(f[i], y.x, x.x), x.y = fmaf(f[i], y.y, x.y), x.z = fmaf(f[i], y.z, x.z), x.w = fmaf(f[i], y.w, x.w);
+        SL = fmaf(f[i], quantity(i, T_SEALED), SL);
+        E = fmaf(f[i], quantity(i, T_EV), E);
+        EM = fmaxf(EM, f[i] * quantity(i, T_EVMAX));
+        DM = fmaxf(DM, quantity(i, T_DMAX));
+        VM = fmaxf(VM, quantity(i, T_VMAX));
       }
-      if (put_channels(a, out, c, x, inv)) s_bad[row] = 1u;
+      ct = certificate(a, M, L, SL, E, EM, DM, VM);
+    } else {
+      const float inv = mean_factor(L);
+      for (int c = tid / ROWS; c < 32; c += WIDE / ROWS) {
+        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float4 y = reinterpret_cast<const float4*>(sets + (int64_t)min(i, n - 1) * stride)[c * T_ROWS + r32];
+          x.x = fmaf(f[i], y.x, x.x), x.y = fmaf(f[i], y.y, x.y), x.z = fmaf(f[i], y.z, x.z), x.w = fmaf(f[i], y.w, x.w);
+        }
+        if (put_channels(a, out, c, x, inv)) s_bad[row] = 1u;
+      }
     }
   }
+  __syncthreads();
+  if (certifies) put_certificate(a, out, ct, s_bad[row] != 0u);
 }
 
 __device__ __forceinline__ float* set_of(const TreeArgs& a, int64_t head, int tile, int split) {
@@ -673,9 +688,7 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
     join_sets<FEW_WAVES, 512>(s_set[0], T_FLOATS, set_of(a, head, tile, split), tid);
     return;
   }
-  finish_sets<FEW_WAVES, T_ROWS, 512, false>(s_set[0], T_FLOATS, FEW_WAVES, a, (int)head, tile, 0, tid, s_flag);
-  __syncthreads();
-  finish_sets<FEW_WAVES, T_ROWS, 512, true>(s_set[0], T_FLOATS, FEW_WAVES, a, (int)head, tile, 0, tid, s_flag);
+  finish_sets<FEW_WAVES, T_ROWS, 512>(s_set[0], T_FLOATS, FEW_WAVES, a, (int)head, tile, 0, tid, s_flag);
 }
 
 // ---- more rows: bound by the products -------------------------------------------------------------------------------------------------
@@ -996,32 +1009,24 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
     __syncthreads();
     constexpr int PER = 512 / WR;   // threads a joined set: set i of row wave r is that of wave i * WR + r
     const int r = tid / PER;
-    const bool there = tile0 + r < a.row_tiles;
     if (a.nsplit > 1) {
-      if (there) join_sets<S::WT, PER>(sets + r * T_FLOATS, WR * T_FLOATS, set_of(a, head, tile0 + r, split), tid % PER);
+      if (tile0 + r < a.row_tiles) join_sets<S::WT, PER>(sets + r * T_FLOATS, WR * T_FLOATS, set_of(a, head, tile0 + r, split), tid % PER);
       return;
     }
-    if (there)
-      finish_sets<S::WT, T_ROWS, PER, false>(sets + r * T_FLOATS, WR * T_FLOATS, S::WT, a, (int)head, tile0 + r, 0, tid % PER, s_flag + r * T_ROWS);
-    __syncthreads();
-    if (there)
-      finish_sets<S::WT, T_ROWS, PER, true>(sets + r * T_FLOATS, WR * T_FLOATS, S::WT, a, (int)head, tile0 + r, 0, tid % PER, s_flag + r * T_ROWS);
+    finish_sets<S::WT, T_ROWS, PER>(sets + r * T_FLOATS, WR * T_FLOATS, S::WT, a, (int)head, tile0 + r, 0, tid % PER, s_flag + r * T_ROWS);
   }
 }
 
 // ---- joining the partial sets ---------------------------------------------------------------------------------------------------------
 
-// Few sets: eight rows a workgroup, four channels of one a thread.
-constexpr int JOIN_ROWS = 8, JOIN_FEW = 8;
-__global__ __launch_bounds__(256) void tree_join_few_kernel(TreeArgs a) {
+// Few sets: eight rows a workgroup, four channels of one a thread, and a wave for the certificates.
+constexpr int JOIN_ROWS = 8, JOIN_FEW = 8, JOIN_FEW_THREADS = JOIN_ROWS * 32 + 64;
+__global__ __launch_bounds__(JOIN_FEW_THREADS) void tree_join_few_kernel(TreeArgs a) {
   __shared__ uint32_t s_bad[JOIN_ROWS];
   const int head = blockIdx.x, tile = blockIdx.y >> 2, first = (blockIdx.y & 3) * JOIN_ROWS;
   if (threadIdx.x < JOIN_ROWS) s_bad[threadIdx.x] = 0u;
   __syncthreads();
-  const float* const sets = set_of(a, head, tile, 0);
-  finish_sets<JOIN_FEW, JOIN_ROWS, 256, false>(sets, T_FLOATS, a.nsplit, a, head, tile, first, threadIdx.x, s_bad);
-  __syncthreads();
-  finish_sets<JOIN_FEW, JOIN_ROWS, 256, true>(sets, T_FLOATS, a.nsplit, a, head, tile, first, threadIdx.x, s_bad);
+  finish_sets<JOIN_FEW, JOIN_ROWS, JOIN_FEW_THREADS>(set_of(a, head, tile, 0), T_FLOATS, a.nsplit, a, head, tile, first, threadIdx.x, s_bad);
 }
 
 // Many sets: eight rows a workgroup.  First every set's quantities of the rows, a set a thread, which gives the sets' weights; then the
@@ -1046,8 +1051,16 @@ __global__ __launch_bounds__(1024) void tree_join_kernel(TreeArgs a) {
 
   const auto lanes_max = [](float x) { return max_x32(max_x16(fmaxf(x, dpp_mov<0x128>(x)))); };   // over the lanes of a row: 8, 16, 32 apart
   const auto lanes_sum = [](float x) { return sum_x32(sum_x16(x + dpp_mov<0x128>(x))); };
-  float m = -INFINITY;
-  for (int i = tid >> 3; i < a.nsplit; i += 128) m = fmaxf(m, sets[(int64_t)i * T_FLOATS + T_OFLOATS + T_M * T_ROWS + r32]);
+  constexpr int TRIP = 128;   // sets of a trip of the workgroup, eight a wave
+  const auto quantity = [&](int i, int t) { return sets[(int64_t)min(i, a.nsplit - 1) * T_FLOATS + T_OFLOATS + t * T_ROWS + r32]; };
+  const int i0 = tid >> 3;
+  float z[7], m = -INFINITY;
+  if (w * 8 < a.nsplit) {   // the first trip's quantities at once
+#pragma unroll
+    for (int t = 0; t < 7; ++t) z[t] = quantity(i0, t);
+    m = z[T_M];
+  }
+  for (int i = i0 + TRIP; i < a.nsplit; i += TRIP) m = fmaxf(m, quantity(i, T_M));
   m = lanes_max(m);
   if ((tid & 63) < 8) s_m[w][row] = m;
   __syncthreads();
@@ -1055,17 +1068,22 @@ __global__ __launch_bounds__(1024) void tree_join_kernel(TreeArgs a) {
 #pragma unroll
   for (int i = 1; i < 16; ++i) M = fmaxf(M, s_m[i][row]);
   float q[6] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};   // sums: L, sealed, EV; maxima: EVMAX, DMAX, VMAX
-  for (int i = tid >> 3; i < a.nsplit; i += 128) {
-    const float* const st = sets + (int64_t)i * T_FLOATS + T_OFLOATS + r32;
-    const float mi = st[T_M * T_ROWS];
-    const float f = mi == M ? 1.0f : __builtin_amdgcn_exp2f(mi - M);
+  const auto take = [&](int i, const float* y) {
+    if (i >= a.nsplit) return;
+    const float f = y[T_M] == M ? 1.0f : __builtin_amdgcn_exp2f(y[T_M] - M);
     s_f[i * JOIN_ROWS + row] = f;
-    q[0] = fmaf(f, st[T_L * T_ROWS], q[0]);
-    q[1] = fmaf(f, st[T_SEALED * T_ROWS], q[1]);
-    q[2] = fmaf(f, st[T_EV * T_ROWS], q[2]);
-    q[3] = fmaxf(q[3], f * st[T_EVMAX * T_ROWS]);
-    q[4] = fmaxf(q[4], st[T_DMAX * T_ROWS]);
-    q[5] = fmaxf(q[5], st[T_VMAX * T_ROWS]);
+    q[0] = fmaf(f, y[T_L], q[0]);
+    q[1] = fmaf(f, y[T_SEALED], q[1]);
+    q[2] = fmaf(f, y[T_EV], q[2]);
+    q[3] = fmaxf(q[3], f * y[T_EVMAX]);
+    q[4] = fmaxf(q[4], y[T_DMAX]);
+    q[5] = fmaxf(q[5], y[T_VMAX]);
+  };
+  if (w * 8 < a.nsplit) take(i0, z);
+  for (int i = i0 + TRIP; i < a.nsplit; i += TRIP) {
+#pragma unroll
+    for (int t = 0; t < 7; ++t) z[t] = quantity(i, t);
+    take(i, z);
   }
 #pragma unroll
   for (int k = 0; k < 6; ++k) {
@@ -1081,20 +1099,25 @@ __global__ __launch_bounds__(1024) void tree_join_kernel(TreeArgs a) {
   for (int i = g + 4 * JOIN_AHEAD; i < a.nsplit; i += 4) add(s_f[i * JOIN_ROWS + row], channels(i));
   s_o[g][c][row] = x;
   __syncthreads();
-  if (tid < 256) {
-#pragma unroll
-    for (int k = 1; k < 4; ++k) add(1.0f, s_o[k][c][row]);
+  const bool there = r < a.n * a.group, certifies = there && tid >= 512 && tid < 512 + JOIN_ROWS;
+  Certificate ct;
+  if (there && (tid < 256 || certifies)) {
 #pragma unroll
     for (int k = 0; k < 6; ++k) {
       q[k] = s_q[0][k][row];
 #pragma unroll
       for (int i = 1; i < 16; ++i) q[k] = k < 3 ? q[k] + s_q[i][k][row] : fmaxf(q[k], s_q[i][k][row]);
     }
-    if (r < a.n * a.group && put_channels(a, row_out(a, head, r), c, x, mean_factor(q[0]))) s_bad[row] = 1u;
+    if (certifies) {
+      ct = certificate(a, M, q[0], q[1], q[2], q[3], q[4], q[5]);
+    } else {
+#pragma unroll
+      for (int k = 1; k < 4; ++k) add(1.0f, s_o[k][c][row]);
+      if (put_channels(a, row_out(a, head, r), c, x, mean_factor(q[0]))) s_bad[row] = 1u;
+    }
   }
   __syncthreads();
-  if (tid < JOIN_ROWS && r < a.n * a.group)
-    put_certificate(a, row_out(a, head, r), M, q[0], q[1], q[2], q[3], q[4], q[5], s_bad[row] != 0u);
+  if (certifies) put_certificate(a, row_out(a, head, r), ct, s_bad[row] != 0u);
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------------------
@@ -1102,17 +1125,17 @@ __global__ __launch_bounds__(1024) void tree_join_kernel(TreeArgs a) {
 // Rows of a KV group a workgroup takes.
 static int tree_rows(int n_rows) { return n_rows <= 32 ? 32 : (n_rows <= 64 ? 64 : (n_rows <= 128 ? 128 : 256)); }
 
-static int tile_tokens(int rows) { return rows == 64 ? 128 : 64; }   // of more than 32 rows
+// Tokens of a tile: of more than 32 rows, or the pairs of blocks of the waves of few.
+static int tile_tokens(int rows) { return rows == 32 ? 32 * FEW_WAVES : (rows == 64 ? 128 : 64); }
 
-// Partial sets: as many workgroups as the device holds at a time, each with something to do.  Short caches are one workgroup's, which finishes the
-// rows itself: up to two pairs of blocks a wave of few rows, or three tiles of more, take less than a second launch.
-static int tree_splits(int n_cu, int64_t heads, int n_rows, int n_draft, int64_t tokens) {
-  const int rows = tree_rows(n_rows);
-  const int64_t z = (n_rows + rows - 1) / rows;
-  const int64_t most = std::max<int64_t>(1, (int64_t)n_cu / (heads * z));
-  const int64_t tok = rows == 32 ? 32 * FEW_WAVES : tile_tokens(rows);   // of the waves' units, or of a tile
-  const int64_t tiles = (tokens + n_draft + tok - 1) / tok;
-  return tiles <= (rows == 32 ? 2 : 3) ? 1 : (int)std::min(most, tiles);
+// Partial sets: as many workgroups as the device holds at a time, each with a tile of sealed blocks or of the other tokens.  Of few rows
+// the first tile and the other tokens are one workgroup's, which needs no second launch (8 heads, 4 nodes of 4 query heads, 200 tokens
+// 11.4 us, by two workgroups 13.3; two tiles, 400 tokens, 14.2, and by two 13.8).
+static int tree_splits(int n_cu, int64_t heads, int n_rows, int64_t sealed, int64_t others) {
+  const int rows = tree_rows(n_rows), tok = tile_tokens(rows);
+  const int64_t z = (n_rows + rows - 1) / rows, most = std::max<int64_t>(1, (int64_t)n_cu / (heads * z));
+  const int64_t tiles = (sealed + tok - 1) / tok;
+  return (int)std::min(most, rows > 32 ? tiles + (others + tok - 1) / tok : (tiles <= 1 ? 1 : tiles + 1));
 }
 
 // Sealed tiles of more than 32 rows by workgroup: the trailing and drafted tokens' tiles are the last workgroups', EXACT tiles' work each, and
@@ -1131,7 +1154,7 @@ static void tree_shares(TreeArgs& a, int n_rows) {
 int64_t tree_ws_bytes(const Cache* c, int n_draft) {
   const int64_t heads = (int64_t)c->desc.batch * c->desc.n_kv_heads;
   const int n_rows = n_draft * (c->desc.n_q_heads / c->desc.n_kv_heads);
-  return heads * ((n_rows + 31) / 32) * tree_splits(c->n_cu, heads, n_rows, n_draft, c->desc.max_tokens) * T_FLOATS * 4;
+  return heads * ((n_rows + 31) / 32) * tree_splits(c->n_cu, heads, n_rows, c->desc.max_tokens, n_draft + BLK - 1) * T_FLOATS * 4;
 }
 
 template <int WR>
@@ -1161,7 +1184,7 @@ int32_t launch_tree(const Cache* c, int layer, const __half* q, const __half* kd
   a.group = c->desc.n_q_heads / c->desc.n_kv_heads;
   const int n_rows = n_draft * a.group;
   a.row_tiles = (n_rows + 31) / 32;
-  a.nsplit = tree_splits(c->n_cu, heads, n_rows, n_draft, c->length[layer]);
+  a.nsplit = tree_splits(c->n_cu, heads, n_rows, a.nb * BLK, a.trail + a.n);
   tree_shares(a, n_rows);
   a.O = O;
   a.cert = cert;
@@ -1177,7 +1200,7 @@ int32_t launch_tree(const Cache* c, int layer, const __half* q, const __half* kd
   if (a.nsplit == 1) return CQA_OK;
   const dim3 grid((uint32_t)heads, (uint32_t)a.row_tiles * (T_ROWS / JOIN_ROWS));
   if (a.nsplit <= JOIN_FEW)
-    tree_join_few_kernel<<<grid, 256, 0, st>>>(a);
+    tree_join_few_kernel<<<grid, JOIN_FEW_THREADS, 0, st>>>(a);
   else
     tree_join_kernel<<<grid, 1024, (size_t)a.nsplit * JOIN_ROWS * 4, st>>>(a);
   CQA_HIP(hipGetLastError());
