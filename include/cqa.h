@@ -527,8 +527,9 @@ typedef struct cqa_node_cert {
  *   O_dev                    FP16 [batch][n_draft][n_q_heads][128]
  *   cert_dev, flags_dev      [batch][n_draft][n_q_heads]
  *   workspace_dev            cqa_tree_workspace_bytes(c, n_draft) bytes; calls that share one must be ordered
- * Sealed tokens are attended as cqa_cache_read gives them in FP16, trailing and drafted ones exactly; FP32 accumulation, the softmax's weights enter the value product in FP16.  The certificate is
- * that of cqa_certified_decode with what the rounding to FP16 adds: sigma_c becomes the next FP16 number from
+ * Sealed tokens are attended as cqa_cache_read gives them in FP16, trailing and drafted ones exactly; FP32 accumulation;
+ * the softmax's weights, times 2^14, enter the value product in FP16 (down to 2^-28 of the largest with 11 bits).  The
+ * certificate is that of cqa_certified_decode with what the rounding to FP16 adds: sigma_c becomes the next FP16 number from
  *   sigma_c + 2 min(sigma_c / 2, 2^-11 max(|z_c - 128 sigma_c|, |z_c + 127 sigma_c|) + 2^-25)
  * upwards, eta_b becomes eta_b + min(eta_b, 2^-11 (nu_b + eta_b) + 2^-21); v_max ranges over the tokens the node attends.
  * flags: KEY, VAL, TOTAL, PRECOND by tol's thresholds, force_flags; they only REQUEST precision, there is no ladder for

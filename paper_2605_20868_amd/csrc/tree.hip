@@ -16,9 +16,10 @@
 //   S^T [32 tokens][32 rows] = K^ Q^T.  The tile's 32 token rows are dealt to two blocks so that a lane's 16 results are the 16 tokens of
 //     one block for one row: the block's sum S_b is an in-lane sum, and what the lane holds is, packed, the B operand of
 //   O^T [128 channels][32 rows] += V^T P^T, whose 8 consecutive tokens per lane are what one dword of value codes holds.
-// Softmax in FP32 (running maximum per row, FP32 sums); the weights enter the second product as FP16, 2^-12 of a weight at most.
+// Softmax in FP32 (running maximum per row, FP32 sums); the weights enter the second product as FP16, off by 2^-12 of a weight at most.
 //
-// A further workgroup per group of rows attends the trailing FP16 tokens and the drafted ones, which are exact, under the mask.
+// Trailing FP16 tokens and drafted ones, which are exact, are attended behind the sealed ones, under the mask, by the workgroups that have
+// the fewest of those.
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -36,6 +37,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float SCORE = 0.08838834764831845f * 1.4426950408889634f;   // 1 / sqrt(d), in the exponent's base 2
 constexpr float HALF_SCORE = 0.5f * 0.08838834764831845f;
 constexpr float F16_MAX = 65504.0f;
+constexpr float MOST = 14.0f;   // the largest weight is 2^MOST: see softmax32
 constexpr float LN2 = 0.6931471805599453f;
 
 // f(0), f(1), ... f(N - 1), each with its index as a constant
@@ -172,8 +174,10 @@ __device__ __forceinline__ void values32(TreeRows& w, const uint32_t (&p)[8], Va
       w.o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
           value(oct, ct), __builtin_bit_cast(f16x8, make_uint4(p[4 * oct], p[4 * oct + 1], p[4 * oct + 2], p[4 * oct + 3])), w.o[ct], 0, 0, 0);
 }
-// Scores of MT times 32 tokens to weights.  bits(mt), where masked: the tokens of the lane's block that its row attends; eta(mt): the block's
-// value error.
+// Scores of MT times 32 tokens to weights, 2^MOST for a row's largest score so far: the row's m is that score less MOST.  The weights enter
+// the product with the values as FP16: those down to 2^-28 of the largest keep 11 bits, and a million lighter ones are together off by 2^-19
+// of it.  (With 1 for the largest, tokens of 2^-25 of it vanished, and all of the result with them where the heavy ones' values are zero.)
+// bits(mt), where masked: the tokens of the lane's block that its row attends; eta(mt): the block's value error.
 template <int MT, typename Bits, typename Eta>
 __device__ __forceinline__ void softmax32(TreeRows& w, f32x16 (&s)[MT], uint32_t (&p)[MT][8], bool masked, Bits bits, Eta eta) {
   if (masked) {
@@ -189,7 +193,7 @@ __device__ __forceinline__ void softmax32(TreeRows& w, f32x16 (&s)[MT], uint32_t
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
     for (int r = 0; r < 16; ++r) top = fmaxf(top, s[mt][r]);
-  top = max_x32(top) * SCORE;
+  top = fmaf(max_x32(top), SCORE, -MOST);
   if (__any(top > w.m)) {
     const float mn = fmaxf(w.m, top);
     const float f = mn == w.m ? 1.0f : __builtin_amdgcn_exp2f(w.m - mn);

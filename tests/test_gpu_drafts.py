@@ -247,6 +247,97 @@ def test_the_ends_of_the_range(ks, vs, qs):
         assert_nodes(ref, O, cert, flags)
 
 
+@pytest.mark.parametrize("n", [3, 12, 30, 40])
+def test_light_tokens_among_some_that_hold_nothing(n):
+    """A token of each block has a score 18.4 above the others' and the value 0: what comes out is those others, of weights that FP16 does not
+    hold beside 1.  Not off by more than FP16's step of their own."""
+    print("tree light tokens", n, flush=True)
+    n_tokens = 1000
+    k, v = np.zeros((1, 1, n_tokens, 128), np.float16), np.full((1, 1, n_tokens, 128), 30000.0, np.float16)
+    k[:, :, 3::16, 5], v[:, :, 3::16] = 16.0, 0.0
+    kd, vd = np.zeros((1, 1, n, 128), np.float16), np.zeros((1, 1, n, 128), np.float16)
+    q = np.zeros((1, n, 4, 128), np.float16)
+    q[..., 5] = 13.0
+    seen = np.eye(n, dtype=bool)[None]
+    oc = oracle.OracleLayerCache(1, 1)
+    oc.append(k, v)
+    ref = drafts.tree_decode(oc, q, kd, vd, seen, oracle.Tolerances())
+    assert 0.002 < ref[0][0][0]["O"][0] < 0.01
+    for b, i, h in np.ndindex(1, n, 4):
+        ref[b][i][h]["floor"] = 0.0
+    with GpuLayerCache(1, 4, 1, n_tokens, tier2=False) as gc:
+        gc.append(k, v)
+        assert_nodes(ref, *tree_call(gc, q, kd, vd, drafts.mask_words(seen)))
+
+
+@pytest.mark.parametrize("n,n_tokens", [(2, 700), (11, 390), (27, 203), (40, 150), (130, 75)])
+def test_more_sequences_than_compute_units(n, n_tokens):
+    """A workgroup has all of a sequence's tokens, several turns of them, and finishes its rows."""
+    print("tree of many sequences", n, n_tokens, flush=True)
+    rng = np.random.default_rng(20 + n)
+    bt, hkv, g = (43, 3, 2) if n > 100 else (87, 3, 4)
+    k, v, q, kd, vd = make(rng, bt, hkv, g, n_tokens, n)
+    seen = random_tree(rng, bt, n)
+    oc = oracle.OracleLayerCache(bt, hkv)
+    oc.append(k, v)
+    some = [0, 1, bt // 2, bt - 1]
+    part = oracle.OracleLayerCache(len(some), hkv)
+    part.append(k[some], v[some])
+    ref = drafts.tree_decode(part, q[some], kd[some], vd[some], seen[some], oracle.Tolerances())
+    with GpuLayerCache(bt, hkv * g, hkv, n_tokens, tier2=False) as gc:
+        gc.append(k, v)
+        O, cert, flags = tree_call(gc, q, kd, vd, drafts.mask_words(seen))
+        assert_nodes(ref, O[some], {f: x[some] for f, x in cert.items()}, flags[some])
+        assert np.isfinite(O).all() and (flags == 0).all()
+
+
+# the first and the last lengths of a tile, and of one and two workgroups
+@pytest.mark.parametrize("g,n", [(4, 3), (4, 9), (4, 20), (2, 127), (4, 256)])
+def test_lengths_at_the_tiles_ends(g, n):
+    print("tree lengths", g, n, flush=True)
+    rng = np.random.default_rng(30 + n)
+    few = [3, n - 1] if n > 100 else range(n)   # nodes that are compared
+    for n_tokens in (63, 64, 80, 127, 128, 129, 144, 192, 255, 256, 257, 272, 528, 1040):
+        k, v, q, kd, vd = make(rng, 1, 1, g, n_tokens, n)
+        seen = random_tree(rng, 1, n)
+        oc = oracle.OracleLayerCache(1, 1)
+        oc.append(k, v)
+        few = list(few)
+        ref = drafts.tree_decode(oc, q, kd, vd, seen, oracle.Tolerances()) if n <= 100 else None
+        with GpuLayerCache(1, g, 1, 1100, tier2=False) as gc:
+            gc.append(k, v)
+            O, cert, flags = tree_call(gc, q, kd, vd, drafts.mask_words(seen))
+            if ref is None:   # a few rows: of each, the call with that node's mask alone for all of them
+                for i in few:
+                    one = drafts.tree_decode(oc, q[:, i:i + 1], np.ascontiguousarray(kd[:, :, seen[0, i]]), np.ascontiguousarray(vd[:, :, seen[0, i]]),
+                                             np.ones((1, 1, int(seen[0, i].sum())), bool), oracle.Tolerances())
+                    assert_nodes(one, O[:, i:i + 1], {f: x[:, i:i + 1] for f, x in cert.items()}, flags[:, i:i + 1], (n_tokens, i))
+            else:
+                assert_nodes(ref, O, cert, flags, n_tokens)
+
+
+def test_a_cache_that_is_filled_again():
+    """What an earlier, longer sequence left behind the last block of a record is not the new one's: neither widths nor errors."""
+    print("tree after a reset", flush=True)
+    rng = np.random.default_rng(40)
+    with GpuLayerCache(1, 4, 1, 1100, tier2=False) as gc:
+        for n in (5, 30):
+            k, v, q, kd, vd = make(rng, 1, 1, 4, 1024, n)
+            gc.append((k.astype(np.float32) * 50).astype(np.float16), (v.astype(np.float32) * 50).astype(np.float16))
+            tree_call(gc, q, kd, vd, None)
+            for n_tokens in (0, 7, 16, 83, 100):
+                gc.cqa.cqa_cache_reset(gc.h, 0)
+                k, v, q, kd, vd = make(rng, 1, 1, 4, n_tokens, n)
+                seen = random_tree(rng, 1, n)
+                oc = oracle.OracleLayerCache(1, 1)
+                if n_tokens:
+                    oc.append(k, v)
+                    gc.append(k, v)
+                ref = drafts.tree_decode(oc, q, kd, vd, seen, oracle.Tolerances())
+                assert_nodes(ref, *tree_call(gc, q, kd, vd, drafts.mask_words(seen)), where=n_tokens)
+            gc.cqa.cqa_cache_reset(gc.h, 0)
+
+
 def test_one_node_agrees_with_the_appended_token_and_layers_are_apart():
     print("tree of one node against append + decode, three layers", flush=True)
     rng = np.random.default_rng(9)
