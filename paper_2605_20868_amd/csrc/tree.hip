@@ -104,9 +104,10 @@ __device__ __forceinline__ uint4 paired(uint4 x) {
 // z and sigma are FP32, the largest code is the maximum within 2^-23).
 template <int I>
 __device__ __forceinline__ uint32_t value2(uint32_t codes, uint32_t scale, uint32_t off) {
-  uint32_t bias = 0x64006400u;
+  // (odd ones where they are, on the mantissa of 64: shifts are common to two of them)
+  uint32_t bias = I & 1 ? 0x54005400u : 0x64006400u;
   asm("" : "+v"(bias));   // (in a register, so that mask and bias are one operation)
-  const uint32_t biased = (codes >> (4 * I) & 0x000f000fu) | bias;
+  const uint32_t biased = (codes >> (8 * (I >> 1)) & (I & 1 ? 0x00f000f0u : 0x000f000fu)) | bias;
   const f16x2 code = __builtin_bit_cast(f16x2, biased) - __builtin_bit_cast(f16x2, bias);
   const f16x2 x = __builtin_elementwise_fma(code, __builtin_bit_cast(f16x2, scale), __builtin_bit_cast(f16x2, off));
   const f16x2 most = {(_Float16)F16_MAX, (_Float16)F16_MAX};
@@ -570,8 +571,8 @@ __device__ __forceinline__ float* set_of(const TreeArgs& a, int64_t head, int ti
 // lanes share, goes through LDS, the wave's own part of it, so that no wave waits for another until the waves' sets are joined.
 constexpr int FEW_WAVES = 8;
 constexpr int FEW_KM_HALF = 64 + 4, FEW_KM_KIND = 2 * FEW_KM_HALF, FEW_KM_BLK = 2 * FEW_KM_KIND + 8;   // floats; padded: the four
-constexpr int FEW_VM_BLK = VM_BYTES + 32, FEW_W_BLK = 2 * D + 16;                                      // addresses of a read in four sets of banks
-constexpr int FEW_KM = 0, FEW_VM = FEW_KM + 2 * FEW_KM_BLK * 4, FEW_W = FEW_VM + 2 * FEW_VM_BLK, FEW_META_END = FEW_W + 2 * FEW_W_BLK;
+constexpr int FEW_VM_BLK = VM_BYTES + 32, FEW_W_RUN = 32 * 16 + 16;                                   // addresses of a read in four sets of banks
+constexpr int FEW_KM = 0, FEW_VM = FEW_KM + 2 * FEW_KM_BLK * 4, FEW_W = FEW_VM + 2 * FEW_VM_BLK, FEW_META_END = FEW_W + D / 8 * FEW_W_RUN;   // widths [run of 8 channels][32 blocks]
 constexpr int FEW_EXACT = 64;   // trailing tokens and, as many as a group of 32 rows has nodes, drafted ones
 static_assert(BLK - 1 + T_ROWS <= FEW_EXACT && FEW_META_END <= T_FLOATS * 4 && 2 * FEW_EXACT * D * 2 <= 2 * T_FLOATS * 4 && FEW_VM % 16 == 0 && FEW_W % 16 == 0, "a wave's part of LDS");
 
@@ -604,8 +605,13 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
     const uint8_t* const p = r + Q_KC + (b0 + bsel) * KC_BYTES + half * 1024 + tok * 16;
 #pragma unroll
     for (int i = 0; i < 4; ++i) kc[i] = *reinterpret_cast<const uint4*>(p + i * 256);
+  };
+  const auto load_meta = [&](int u) {
+    const uint8_t* const r = record(u);
+    const int b0 = (u & 1) * 2;
     km0 = reinterpret_cast<const uint4*>(r + Q_KM + b0 * KM_BYTES)[l];
     km1 = reinterpret_cast<const uint4*>(r + Q_KM + (b0 + 1) * KM_BYTES)[l];
+    vm = reinterpret_cast<const uint4*>(r + Q_VM + b0 * VM_BYTES)[l];
     an = reinterpret_cast<const float2*>(r + Q_AN)[b0 + half];
   };
   const auto load_values = [&](int u) {
@@ -613,55 +619,86 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
     const int b0 = (u & 1) * 2;
     vc0 = reinterpret_cast<const uint4*>(r + Q_VC + (b0 + half) * VC_BYTES)[n32];
     vc1 = reinterpret_cast<const uint4*>(r + Q_VC + (b0 + half) * VC_BYTES + 512)[n32];
-    vm = reinterpret_cast<const uint4*>(r + Q_VM + b0 * VM_BYTES)[l];
   };
   int u = split * FEW_WAVES + w;
   const uint4 q_in = fetch_rows(a, b, kvh, tile * T_ROWS + 4 * w);
+  load_meta(u);
   load_keys(u);
   load_values(u);
   keep_rows(s_q, 4 * w, q_in);
   __syncthreads();
   start_rows(rows, a, tile, s_q);
 
-  for (; u < units; u += step) {
+  const float* const sg = reinterpret_cast<const float*>(mine + FEW_KM) + bsel * FEW_KM_BLK + half * FEW_KM_HALF;
+  const uint8_t* const sc = mine + FEW_VM + half * FEW_VM_BLK + (n32 >> 4) * 64;
+  for (int turn = 0; u < units; u += step, ++turn) {
     // metadata: sigma and z by (block, kind, half of the channels), scales and offsets by block
     float* const skm = reinterpret_cast<float*>(mine + FEW_KM);
     float* const at = skm + half * FEW_KM_KIND + ((l >> 4) & 1) * FEW_KM_HALF + (l & 15) * 4;
     *reinterpret_cast<uint4*>(at) = km0;
     *reinterpret_cast<uint4*>(at + FEW_KM_BLK) = km1;
     *reinterpret_cast<uint4*>(mine + FEW_VM + half * FEW_VM_BLK + n32 * 16) = paired(vm);
+    const float eta = value_error(an);
+    rows.vmax = fmaxf(rows.vmax, an.y);
+    load_meta(u + step);
     wave_sync();
+    // Operands' metadata are read a product ahead of their use.
+    float4 m4[2][4];
+    const auto key_meta = [&](auto ks_) {
+      constexpr int ks = ks_.value;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m4[ks & 1][i] = *reinterpret_cast<const float4*>(sg + (i >> 1) * FEW_KM_KIND + ks * 8 + (i & 1) * 4);
+    };
+    key_meta(std::integral_constant<int, 0>{});
     // widths: four channels a lane
     {
       const int c = n32 * 4;
       const float* const p = skm + half * FEW_KM_BLK + (c >> 6) * FEW_KM_HALF + (c & 63);
       const float4 s4 = *reinterpret_cast<const float4*>(p), z4 = *reinterpret_cast<const float4*>(p + FEW_KM_KIND);
-      *reinterpret_cast<uint2*>(mine + FEW_W + half * FEW_W_BLK + c * 2) =
+      *reinterpret_cast<uint2*>(mine + FEW_W + (c >> 3) * FEW_W_RUN + ((turn & 15) * 2 + half) * 16 + (c & 4) * 2) =
           make_uint2(key_width(s4.x, z4.x) | key_width(s4.y, z4.y) << 16, key_width(s4.z, z4.z) | key_width(s4.w, z4.w) << 16);
     }
-    const float* const sg = skm + bsel * FEW_KM_BLK + half * FEW_KM_HALF;
-    const float* const zz = sg + FEW_KM_KIND;
-    const float eta = value_error(an);
-    rows.vmax = fmaxf(rows.vmax, an.y);
-    attend32(
-        rows, (int64_t)u * 2 + 2 > a.nb, (int64_t)u * 2 + half < a.nb ? 0xffffu : 0u, eta,
-        [&](int ks) {
-          const float4 s0 = *reinterpret_cast<const float4*>(sg + ks * 8), s1 = *reinterpret_cast<const float4*>(sg + ks * 8 + 4);
-          const float4 z0 = *reinterpret_cast<const float4*>(zz + ks * 8), z1 = *reinterpret_cast<const float4*>(zz + ks * 8 + 4);
-          const uint32_t c0 = ks & 1 ? kc[ks >> 1].z : kc[ks >> 1].x, c1 = ks & 1 ? kc[ks >> 1].w : kc[ks >> 1].y;
-          return __builtin_bit_cast(f16x8, keys8(c0, c1, s0, s1, z0, z1));
-        },
-        [&] {
-          wave_sync();
-          load_keys(u + step);
-          bound_scores(rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(mine + FEW_W + bsel * FEW_W_BLK + half * 128 + ks * 16); });
-        },
-        [&](int oct, int ct) {
-          const uint8_t* const p = mine + FEW_VM + half * FEW_VM_BLK + oct * 128 + (n32 >> 4) * 64 + ct * 16;
-          const uint4 v = oct ? vc1 : vc0;
-          const uint32_t c = ct == 0 ? v.x : (ct == 1 ? v.y : (ct == 2 ? v.z : v.w));
-          return __builtin_bit_cast(f16x8, values8(c, *reinterpret_cast<const uint4*>(p), *reinterpret_cast<const uint4*>(p + 256)));
-        });
+    f32x16 x[1];
+    uint32_t p[1][8];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[0][r] = 0.0f;
+    each<8>([&](auto ks_) {
+      constexpr int ks = ks_.value;
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (ks < 7) key_meta(std::integral_constant<int, ks + 1>{});
+      const uint32_t c0 = ks & 1 ? kc[ks >> 1].z : kc[ks >> 1].x, c1 = ks & 1 ? kc[ks >> 1].w : kc[ks >> 1].y;
+      const float4* const m = m4[ks & 1];
+      x[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, keys8(c0, c1, m[0], m[1], m[2], m[3])), rows.q[ks], x[0], 0, 0, 0);
+    });
+    __builtin_amdgcn_sched_barrier(0);
+    load_keys(u + step);
+    uint4 v4[2][2];
+    const auto value_meta = [&](auto i_) {
+      constexpr int I = i_.value;   // (octet, channel tile)
+      const uint8_t* const p = sc + (I >> 2) * 128 + (I & 3) * 16;
+      v4[I & 1][0] = *reinterpret_cast<const uint4*>(p);
+      v4[I & 1][1] = *reinterpret_cast<const uint4*>(p + 256);
+    };
+    value_meta(std::integral_constant<int, 0>{});
+    if ((turn & 15) == 15 || u + step >= units) {
+      wave_sync();
+      const int blk = min(n32, (turn & 15) * 2 + 1);
+      bound_scores(rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(mine + FEW_W + (half * 8 + ks) * FEW_W_RUN + blk * 16); });
+      wave_sync();
+    }
+    softmax32<1>(
+        rows, x, p, (int64_t)u * 2 + 2 > a.nb, [&](int) { return (int64_t)u * 2 + half < a.nb ? 0xffffu : 0u; }, [&](int) { return eta; });
+    each<8>([&](auto i_) {
+      constexpr int I = i_.value, ct = I & 3, oct = I >> 2;
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (I < 7) value_meta(std::integral_constant<int, I + 1>{});
+      const uint4 v = oct ? vc1 : vc0;
+      const uint32_t c = ct == 0 ? v.x : (ct == 1 ? v.y : (ct == 2 ? v.z : v.w));
+      rows.o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, values8(c, v4[I & 1][0], v4[I & 1][1])),
+                                                          __builtin_bit_cast(f16x8, make_uint4(p[0][4 * oct], p[0][4 * oct + 1], p[0][4 * oct + 2], p[0][4 * oct + 3])),
+                                                          rows.o[ct], 0, 0, 0);
+    });
+    __builtin_amdgcn_sched_barrier(0);
     load_values(u + step);
     wave_sync();
   }
