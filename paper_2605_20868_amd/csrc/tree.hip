@@ -88,7 +88,9 @@ template <int I>
 __device__ __forceinline__ uint32_t key2(uint32_t codes, float s0, float s1, float z0, float z1) {
   const uint32_t biased = __builtin_amdgcn_perm(0x64646464u, codes, I ? 0x04030402u : 0x04010400u);
   const f16x2 code = __builtin_bit_cast(f16x2, biased) - f16x2{(_Float16)1152.0f, (_Float16)1152.0f};
-  return pack_f16(as_rounded(fmaf((float)code[0], s0, z0)), as_rounded(fmaf((float)code[1], s1, z1)));
+  float x = fmaf((float)code[0], s0, z0), y = fmaf((float)code[1], s1, z1);
+  asm("" : "+v"(x), "+v"(y));   // both are binary32 numbers first (as_rounded)
+  return pack_f16(x, y);
 }
 __device__ __forceinline__ uint4 keys8(uint32_t c0, uint32_t c1, float4 s0, float4 s1, float4 z0, float4 z1) {
   return make_uint4(key2<0>(c0, s0.x, s0.y, z0.x, z0.y), key2<1>(c0, s0.z, s0.w, z0.z, z0.w), key2<0>(c1, s1.x, s1.y, z1.x, z1.y),
