@@ -518,44 +518,63 @@ __device__ __forceinline__ void finish_sets(const float* sets, int64_t stride, i
   const int row = tid % ROWS, r32 = first + row, r = tile * T_ROWS + r32;
   const bool there = r < a.n * a.group, certifies = there && tid >= WIDE && tid < WIDE + ROWS;
   const int64_t out = row_out(a, head, r);
-  // (places behind the last set read it again, with weight 0: no request stands in a branch)
-  const auto quantity = [&](int i, int t) { return sets[(int64_t)min(i, n - 1) * stride + T_OFLOATS + t * T_ROWS + r32]; };
+  // (places behind the last set read it again, with weight 0: no request stands in a branch, and none waits for another)
+  const auto set = [&](int i) { return sets + (int64_t)min(i, n - 1) * stride; };
+  const auto quantity = [&](int i, int t) { return set(i)[T_OFLOATS + t * T_ROWS + r32]; };
+  float f[N], l[N], M = -INFINITY, L = 0.0f;
+  const auto weigh = [&] {   // the sets' maxima in f become their weights
+#pragma unroll
+    for (int i = 0; i < N; ++i) M = fmaxf(M, f[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      f[i] = (f[i] == M ? 1.0f : __builtin_amdgcn_exp2f(f[i] - M)) * (i < n ? 1.0f : 0.0f);
+      L = fmaf(f[i], l[i], L);
+    }
+  };
   Certificate ct;
-  if (there && (tid < WIDE || certifies)) {
-    float f[N], l[N], M = -INFINITY, L = 0.0f;
+  if (certifies) {
+    float z[N][5];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       f[i] = quantity(i, T_M);
       l[i] = quantity(i, T_L);
-      M = fmaxf(M, f[i]);
+#pragma unroll
+      for (int t = 0; t < 5; ++t) z[i][t] = quantity(i, T_SEALED + t);
     }
+    weigh();
+    float SL = 0.0f, E = 0.0f, EM = 0.0f, DM = 0.0f, VM = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      f[i] = i >= n ? 0.0f : (f[i] == M ? 1.0f : __builtin_amdgcn_exp2f(f[i] - M));
-      L = fmaf(f[i], l[i], L);
+      SL = fmaf(f[i], z[i][0], SL);
+      E = fmaf(f[i], z[i][1], E);
+      EM = fmaxf(EM, f[i] * z[i][2]);
+      DM = fmaxf(DM, z[i][3]);
+      VM = fmaxf(VM, z[i][4]);
     }
-    if (certifies) {
-      float SL = 0.0f, E = 0.0f, EM = 0.0f, DM = 0.0f, VM = 0.0f;
+    ct = certificate(a, M, L, SL, E, EM, DM, VM);
+  } else if (there && tid < WIDE) {
+    int c = tid / ROWS;
+    float4 y[N];
+    const auto request = [&] {
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        SL = fmaf(f[i], quantity(i, T_SEALED), SL);
-        E = fmaf(f[i], quantity(i, T_EV), E);
-        EM = fmaxf(EM, f[i] * quantity(i, T_EVMAX));
-        DM = fmaxf(DM, quantity(i, T_DMAX));
-        VM = fmaxf(VM, quantity(i, T_VMAX));
-      }
-      ct = certificate(a, M, L, SL, E, EM, DM, VM);
-    } else {
-      const float inv = mean_factor(L);
-      for (int c = tid / ROWS; c < 32; c += WIDE / ROWS) {
-        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      for (int i = 0; i < N; ++i) y[i] = reinterpret_cast<const float4*>(set(i))[c * T_ROWS + r32];
+    };
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float4 y = reinterpret_cast<const float4*>(sets + (int64_t)min(i, n - 1) * stride)[c * T_ROWS + r32];
-          x.x = fmaf(f[i], y.x, x.x), x.y = fmaf(f[i], y.y, x.y), x.z = fmaf(f[i], y.z, x.z), x.w = fmaf(f[i], y.w, x.w);
-        }
-        if (put_channels(a, out, c, x, inv)) s_bad[row] = 1u;
-      }
+    for (int i = 0; i < N; ++i) {
+      f[i] = quantity(i, T_M);
+      l[i] = quantity(i, T_L);
+    }
+    request();
+    weigh();
+    const float inv = mean_factor(L);
+    while (true) {
+      float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int i = 0; i < N; ++i) x.x = fmaf(f[i], y[i].x, x.x), x.y = fmaf(f[i], y[i].y, x.y), x.z = fmaf(f[i], y[i].z, x.z), x.w = fmaf(f[i], y[i].w, x.w);
+      if (put_channels(a, out, c, x, inv)) s_bad[row] = 1u;
+      c += WIDE / ROWS;
+      if (c >= 32) break;
+      request();
     }
   }
   __syncthreads();
