@@ -1081,14 +1081,17 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
 
 // ---- joining the partial sets ---------------------------------------------------------------------------------------------------------
 
-// Few sets: eight rows a workgroup, four channels of one a thread, and a wave for the certificates.
-constexpr int JOIN_ROWS = 8, JOIN_FEW = 8, JOIN_FEW_THREADS = JOIN_ROWS * 32 + 64;
+// Up to N sets: eight rows a workgroup, four channels of one a thread, and a wave for the certificates.  Every thread requests N sets, so there
+// are two of these and the one for any number (8 heads, 500 tokens, 256 nodes of 4 query heads, 8 sets: 22.5 us with N = 8, 24.8 with 16; 2000
+// tokens, of 2 heads, 16 sets: 23.5 with 16, 27.0 by the one below; 8000 tokens, 4 nodes, 31 sets: 16.5 with 32, 16.0 below).
+constexpr int JOIN_ROWS = 8, JOIN_FEW_THREADS = JOIN_ROWS * 32 + 64;
+template <int N>
 __global__ __launch_bounds__(JOIN_FEW_THREADS) void tree_join_few_kernel(TreeArgs a) {
   __shared__ uint32_t s_bad[JOIN_ROWS];
   const int head = blockIdx.x, tile = blockIdx.y >> 2, first = (blockIdx.y & 3) * JOIN_ROWS;
   if (threadIdx.x < JOIN_ROWS) s_bad[threadIdx.x] = 0u;
   __syncthreads();
-  finish_sets<JOIN_FEW, JOIN_ROWS, JOIN_FEW_THREADS>(set_of(a, head, tile, 0), T_FLOATS, a.nsplit, a, head, tile, first, threadIdx.x, s_bad);
+  finish_sets<N, JOIN_ROWS, JOIN_FEW_THREADS>(set_of(a, head, tile, 0), T_FLOATS, a.nsplit, a, head, tile, first, threadIdx.x, s_bad);
 }
 
 // Many sets: eight rows a workgroup.  First every set's quantities of the rows, a set a thread, which gives the sets' weights; then the
@@ -1261,8 +1264,10 @@ int32_t launch_tree(const Cache* c, int layer, const __half* q, const __half* kd
   CQA_HIP(hipGetLastError());
   if (a.nsplit == 1) return CQA_OK;
   const dim3 grid((uint32_t)heads, (uint32_t)a.row_tiles * (T_ROWS / JOIN_ROWS));
-  if (a.nsplit <= JOIN_FEW)
-    tree_join_few_kernel<<<grid, JOIN_FEW_THREADS, 0, st>>>(a);
+  if (a.nsplit <= 8)
+    tree_join_few_kernel<8><<<grid, JOIN_FEW_THREADS, 0, st>>>(a);
+  else if (a.nsplit <= 16)
+    tree_join_few_kernel<16><<<grid, JOIN_FEW_THREADS, 0, st>>>(a);
   else
     tree_join_kernel<<<grid, 1024, (size_t)a.nsplit * JOIN_ROWS * 4, st>>>(a);
   CQA_HIP(hipGetLastError());
