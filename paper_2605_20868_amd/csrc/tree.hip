@@ -51,7 +51,7 @@ __device__ __forceinline__ void each(F f) {
 }
 
 // ---- partial set of a split and 32 rows: the accumulators by (four channels, row), then one float per row for each quantity
-enum { T_M = 0, T_L, T_SEALED, T_EV, T_EVMAX, T_DMAX, T_VMAX };
+enum { T_M = 0, T_L, T_SEALED, T_EV, T_EVMAX, T_DMAX, T_VMAX, T_BAD };   // T_BAD: 1 where an accumulator is no finite number, else 0
 constexpr int T_ROWS = 32;
 constexpr int T_OFLOATS = D * T_ROWS;
 constexpr int T_FLOATS = T_OFLOATS + 8 * T_ROWS;
@@ -390,8 +390,15 @@ __device__ __forceinline__ void put_rows(const TreeRows& w, float* to) {
       const int c = (r4 >> 1) * 16 + ct * 4 + (r4 & 1) * 2 + half;
       reinterpret_cast<float4*>(to)[c * T_ROWS + row] = make_float4(w.o[ct][4 * r4], w.o[ct][4 * r4 + 1], w.o[ct][4 * r4 + 2], w.o[ct][4 * r4 + 3]);
     }
+  float none = 0.0f;   // stays, unless a channel is no finite number
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) none = fmaf(0.0f, w.o[ct][r], none);
+  const float bad = max_x32(none == 0.0f ? 0.0f : 1.0f);
   if (half == 0) {
     float* const st = to + T_OFLOATS + row;
+    st[T_BAD * T_ROWS] = bad;
     st[T_M * T_ROWS] = w.m;
     st[T_L * T_ROWS] = w.sum;
     st[T_SEALED * T_ROWS] = w.sealed;
@@ -423,7 +430,7 @@ __device__ __forceinline__ void join_sets(const float* sets, int stride, float* 
     reinterpret_cast<float4*>(to)[c * T_ROWS + row] = x;
   }
   if (tid < 32) {
-    float L = 0.0f, SL = 0.0f, E = 0.0f, EM = 0.0f, DM = 0.0f, VM = 0.0f;
+    float L = 0.0f, SL = 0.0f, E = 0.0f, EM = 0.0f, DM = 0.0f, VM = 0.0f, bad = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float* const st = sets + i * stride + T_OFLOATS + row;
@@ -433,6 +440,7 @@ __device__ __forceinline__ void join_sets(const float* sets, int stride, float* 
       EM = fmaxf(EM, f[i] * st[T_EVMAX * T_ROWS]);
       DM = fmaxf(DM, st[T_DMAX * T_ROWS]);
       VM = fmaxf(VM, st[T_VMAX * T_ROWS]);
+      bad = fmaxf(bad, st[T_BAD * T_ROWS]);
     }
     float* const st = to + T_OFLOATS + row;
     st[T_M * T_ROWS] = M;
@@ -442,6 +450,7 @@ __device__ __forceinline__ void join_sets(const float* sets, int stride, float* 
     st[T_EVMAX * T_ROWS] = EM;
     st[T_DMAX * T_ROWS] = DM;
     st[T_VMAX * T_ROWS] = VM;
+    st[T_BAD * T_ROWS] = bad;
   }
 }
 // ---- rows whose sets are all there: outputs --------------------------------------------------------------------------------------------
@@ -509,10 +518,9 @@ __device__ __forceinline__ void finish_rows(const TreeRows& w, const TreeArgs& a
   if (half == 0) put_certificate(a, out, certificate(a, w.m, w.sum, w.sealed, w.ev, w.evmax, w.dmax, w.vmax), bad);
 }
 // ROWS rows from r32 = `first` of a tile on, of which all sets, up to N of them (n, `stride` floats apart), are at `sets`, by THREADS threads:
-// the last 64 have the certificates, the others the channels.  Every thread of the workgroup comes here, for the barrier; s_bad [ROWS] is zero
-// and comes to say which rows have a channel that is no finite number.
+// the last 64 have the certificates, the others the channels.
 template <int N, int ROWS, int THREADS>
-__device__ __forceinline__ void finish_sets(const float* sets, int64_t stride, int n, const TreeArgs& a, int head, int tile, int first, int tid, uint32_t* s_bad) {
+__device__ __forceinline__ void finish_sets(const float* sets, int64_t stride, int n, const TreeArgs& a, int head, int tile, int first, int tid) {
   constexpr int WIDE = THREADS - 64;
   static_assert(WIDE > 0 && WIDE % ROWS == 0 && ROWS <= 64, "whole rows");
   const int row = tid % ROWS, r32 = first + row, r = tile * T_ROWS + r32;
@@ -531,18 +539,17 @@ __device__ __forceinline__ void finish_sets(const float* sets, int64_t stride, i
       L = fmaf(f[i], l[i], L);
     }
   };
-  Certificate ct;
   if (certifies) {
-    float z[N][5];
+    float z[N][6];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       f[i] = quantity(i, T_M);
       l[i] = quantity(i, T_L);
 #pragma unroll
-      for (int t = 0; t < 5; ++t) z[i][t] = quantity(i, T_SEALED + t);
+      for (int t = 0; t < 6; ++t) z[i][t] = quantity(i, T_SEALED + t);
     }
     weigh();
-    float SL = 0.0f, E = 0.0f, EM = 0.0f, DM = 0.0f, VM = 0.0f;
+    float SL = 0.0f, E = 0.0f, EM = 0.0f, DM = 0.0f, VM = 0.0f, bad = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       SL = fmaf(f[i], z[i][0], SL);
@@ -550,8 +557,9 @@ __device__ __forceinline__ void finish_sets(const float* sets, int64_t stride, i
       EM = fmaxf(EM, f[i] * z[i][2]);
       DM = fmaxf(DM, z[i][3]);
       VM = fmaxf(VM, z[i][4]);
+      bad = fmaxf(bad, z[i][5]);
     }
-    ct = certificate(a, M, L, SL, E, EM, DM, VM);
+    put_certificate(a, out, certificate(a, M, L, SL, E, EM, DM, VM), bad != 0.0f);
   } else if (there && tid < WIDE) {
     int c = tid / ROWS;
     float4 y[N];
@@ -571,31 +579,33 @@ __device__ __forceinline__ void finish_sets(const float* sets, int64_t stride, i
       float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
       for (int i = 0; i < N; ++i) x.x = fmaf(f[i], y[i].x, x.x), x.y = fmaf(f[i], y[i].y, x.y), x.z = fmaf(f[i], y[i].z, x.z), x.w = fmaf(f[i], y[i].w, x.w);
-      if (put_channels(a, out, c, x, inv)) s_bad[row] = 1u;
+      put_channels(a, out, c, x, inv);
       c += WIDE / ROWS;
       if (c >= 32) break;
       request();
     }
   }
-  __syncthreads();
-  if (certifies) put_certificate(a, out, ct, s_bad[row] != 0u);
 }
 
 __device__ __forceinline__ float* set_of(const TreeArgs& a, int64_t head, int tile, int split) {
   return a.part + ((head * a.row_tiles + tile) * a.nsplit + split) * T_FLOATS;
 }
 
-// ---- up to 32 rows: bound by the cache's bytes and their reconstruction ------------------------------------------------------------
+// ---- 32 rows a workgroup: bound by the cache's bytes and their reconstruction ------------------------------------------------------------
 //
 // A wave takes pairs of blocks by itself and reconstructs them in registers, in the operands' layout: a 16-byte piece of key codes (16
 // channels of a token) is two operands' part of its lane, a dword of value codes (8 tokens of a channel) one.  Only the metadata, which 16
 // lanes share, goes through LDS, the wave's own part of it, so that no wave waits for another until the waves' sets are joined.
+// Two waves a SIMD: what one is to read from LDS is requested a product ahead, and a pair's metadata and codes as soon as those of the pair before
+// are used.  4 x 8 KV heads of 32768 tokens, 5 nodes of 4 query heads: 60 us for 303 MB, 5.05 TB/s, what a large copy reaches (each read where it is
+// used 66, the widths' products for each pair by itself among it); vector ALU 60 % busy, matrix cores 20 %.
 constexpr int FEW_WAVES = 8;
 constexpr int FEW_KM_HALF = 64 + 4, FEW_KM_KIND = 2 * FEW_KM_HALF, FEW_KM_BLK = 2 * FEW_KM_KIND + 8;   // floats; padded: the four
 constexpr int FEW_VM_BLK = VM_BYTES + 32, FEW_W_RUN = 32 * 16 + 16;                                   // addresses of a read in four sets of banks
 constexpr int FEW_KM = 0, FEW_VM = FEW_KM + 2 * FEW_KM_BLK * 4, FEW_W = FEW_VM + 2 * FEW_VM_BLK, FEW_META_END = FEW_W + D / 8 * FEW_W_RUN;   // widths [run of 8 channels][32 blocks]
-constexpr int FEW_EXACT = 64;   // trailing tokens and, as many as a group of 32 rows has nodes, drafted ones
-static_assert(BLK - 1 + T_ROWS <= FEW_EXACT && FEW_META_END <= T_FLOATS * 4 && 2 * FEW_EXACT * D * 2 <= 2 * T_FLOATS * 4 && FEW_VM % 16 == 0 && FEW_W % 16 == 0, "a wave's part of LDS");
+constexpr int FEW_EXACT = 96;   // trailing and drafted tokens of a turn
+static_assert(FEW_META_END <= T_FLOATS * 4 && 2 * FEW_EXACT * D * 2 <= FEW_WAVES * T_FLOATS * 4 && FEW_VM % 16 == 0 && FEW_W % 16 == 0,
+              "a wave's part of LDS");
 
 __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
   fetch_args<sizeof(TreeArgs)>();
@@ -603,7 +613,6 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
   __shared__ __align__(16) uint8_t s_q[Q_TILE];
   __shared__ __align__(16) float s_norm[FEW_EXACT];
   __shared__ __align__(16) uint8_t s_bad[FEW_EXACT];
-  __shared__ uint32_t s_flag[T_ROWS];
   const int tid = threadIdx.x, l = tid & 63, n32 = l & 31, half = l >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t head = blockIdx.x;
@@ -724,36 +733,35 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
     wave_sync();
   }
   rows.sealed = rows.sum;
-  // The other tokens are the workgroup's whose turn is the next: it fetches them together, and two of its waves attend them.
-  if (split == (units + FEW_WAVES - 1) / FEW_WAVES % a.nsplit) {
+  // The other tokens, dealt from the workgroup on whose turn is the next, which fetches them together; three of its waves attend them.
+  for (int t0 = (split + a.nsplit - (units + FEW_WAVES - 1) / FEW_WAVES % a.nsplit) % a.nsplit * FEW_EXACT; t0 < a.trail + a.n; t0 += a.nsplit * FEW_EXACT) {
     uint4* const s_k = reinterpret_cast<uint4*>(s_set);
     uint4* const s_v = s_k + 16 * FEW_EXACT;
-    const uint32_t bits = open_tokens(a, b, rows.node, (2 * w + half) * BLK);
+    const int blk = 2 * w + half;
+    const uint32_t bits = open_tokens(a, b, rows.node, t0 + blk * BLK);
     if (tid < FEW_EXACT / 4) reinterpret_cast<uint32_t*>(s_bad)[tid] = 0u;
     __syncthreads();
-    load_exact<64 * FEW_WAVES, FEW_EXACT>(a, head, 0, tid, s_k, s_v, s_norm, s_bad);
+    load_exact<64 * FEW_WAVES, FEW_EXACT>(a, head, t0, tid, s_k, s_v, s_norm, s_bad);
     __syncthreads();
-    if (w * 32 < a.trail + a.n) {
-      const int blk = 2 * w + half;
+    if (w * 32 < min(FEW_EXACT, a.trail + a.n - t0)) {
       open_exact(rows, bits, s_norm + blk * BLK, s_bad + blk * BLK);
       attend32(
           rows, true, bits, 0.0f, [&](int ks) { return __builtin_bit_cast(f16x8, s_k[(half * 8 + ks) * FEW_EXACT + w * 32 + n32]); }, [] {},
           [&](int oct, int ct) { return __builtin_bit_cast(f16x8, s_v[(blk * 2 + oct) * D + ct * 32 + n32]); });
     }
-    __syncthreads();   // (the waves' sets come where the tokens are)
+    __syncthreads();   // (the next ones, or the waves' sets, come where these are)
   }
   end_rows(rows);
   put_rows(rows, s_set[w]);
-  if (tid < T_ROWS) s_flag[tid] = 0u;
   __syncthreads();
   if (a.nsplit > 1) {
     join_sets<FEW_WAVES, 512>(s_set[0], T_FLOATS, set_of(a, head, tile, split), tid);
     return;
   }
-  finish_sets<FEW_WAVES, T_ROWS, 512>(s_set[0], T_FLOATS, FEW_WAVES, a, (int)head, tile, 0, tid, s_flag);
+  finish_sets<FEW_WAVES, T_ROWS, 512>(s_set[0], T_FLOATS, FEW_WAVES, a, (int)head, tile, 0, tid);
 }
 
-// ---- more rows: bound by the products -------------------------------------------------------------------------------------------------
+// ---- many rows: bound by the products -------------------------------------------------------------------------------------------------
 //
 // Eight waves, WR side by side over rows (32 each) and WT over tokens; four of them reconstruct the tile's keys and four its values
 // into LDS, a block each, for all.  A SIMD has a wave of either kind, and they take turns with a barrier between the phases: while one
@@ -764,6 +772,8 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
 // Keys of t are read in 2 t and 2 t + 1 and replaced (t + 2) in 2 t + 2; values of t are read in 2 t + 2 and 2 t + 3 and replaced
 // in 2 t + 5: two tiles in LDS.  eta of t comes with the keys in 2 t - 2 and is read until 2 t + 2: four of them.  Codes are requested a tile
 // ahead.  (Reconstruction in the weights' phase: products 1310 cycles, weights and reconstruction 2600, of which the products' wave waited half.)
+// 8 KV heads of 131072 tokens, 64 nodes of 4 query heads: 167 - 183 us for 142 GFLOP, 780 - 850 TFLOP/s; vector ALU 67 % and matrix cores 47 % busy, at a clock
+// that falls from 2.4 to 1.6 - 1.8 GHz meanwhile.
 template <int WR>
 struct ManyShape {
   static constexpr int WT = 8 / WR;
@@ -786,7 +796,6 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   __shared__ float s_eta[4][BLKS];
   __shared__ __align__(16) float s_norm[TOK];
   __shared__ __align__(16) uint8_t s_bad[TOK];
-  __shared__ uint32_t s_flag[32 * WR];
 
   const int tid = threadIdx.x, l = tid & 63, n32 = l & 31, half = l >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1067,7 +1076,6 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
     // the token waves' sets are joined through LDS
     float* const sets = reinterpret_cast<float*>(s_main);
     put_rows(rows, sets + w * T_FLOATS);
-    if (tid < 32 * WR) s_flag[tid] = 0u;
     __syncthreads();
     constexpr int PER = 512 / WR;   // threads a joined set: set i of row wave r is that of wave i * WR + r
     const int r = tid / PER;
@@ -1075,7 +1083,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
       if (tile0 + r < a.row_tiles) join_sets<S::WT, PER>(sets + r * T_FLOATS, WR * T_FLOATS, set_of(a, head, tile0 + r, split), tid % PER);
       return;
     }
-    finish_sets<S::WT, T_ROWS, PER>(sets + r * T_FLOATS, WR * T_FLOATS, S::WT, a, (int)head, tile0 + r, 0, tid % PER, s_flag + r * T_ROWS);
+    finish_sets<S::WT, T_ROWS, PER>(sets + r * T_FLOATS, WR * T_FLOATS, S::WT, a, (int)head, tile0 + r, 0, tid % PER);
   }
 }
 
@@ -1087,127 +1095,137 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
 constexpr int JOIN_ROWS = 8, JOIN_FEW_THREADS = JOIN_ROWS * 32 + 64;
 template <int N>
 __global__ __launch_bounds__(JOIN_FEW_THREADS) void tree_join_few_kernel(TreeArgs a) {
-  __shared__ uint32_t s_bad[JOIN_ROWS];
   const int head = blockIdx.x, tile = blockIdx.y >> 2, first = (blockIdx.y & 3) * JOIN_ROWS;
-  if (threadIdx.x < JOIN_ROWS) s_bad[threadIdx.x] = 0u;
-  __syncthreads();
-  finish_sets<N, JOIN_ROWS, JOIN_FEW_THREADS>(set_of(a, head, tile, 0), T_FLOATS, a.nsplit, a, head, tile, first, threadIdx.x, s_bad);
+  finish_sets<N, JOIN_ROWS, JOIN_FEW_THREADS>(set_of(a, head, tile, 0), T_FLOATS, a.nsplit, a, head, tile, first, threadIdx.x);
 }
 
-// Many sets: eight rows a workgroup.  First every set's quantities of the rows, a set a thread, which gives the sets' weights; then the
-// accumulators, four channels of a row and every fourth set a thread, the first of them requested ahead of the weights.
+// Many sets: eight rows a workgroup, and a PARTS-th of their channels.  First every set's quantities of the rows, a set a thread, which gives the sets'
+// weights; then the accumulators, four channels of a row and every G-th set a thread, JOIN_AHEAD sets at a time, the first ones requested
+// ahead of the weights.  Four parts where more sets than one has requests for at a time meet few workgroups (1 head, 131000 tokens, 8 nodes of 4 query heads, 256
+// sets: 26.1 us a call, undivided 36.2; 2 heads, 16000 tokens, 64 nodes 28.5, 32.4; 128 workgroups undivided, 4 heads, 8000 tokens, 64 nodes: 28.1, 26.2).
 constexpr int JOIN_AHEAD = 8;
+template <int PARTS>
 __global__ __launch_bounds__(1024) void tree_join_kernel(TreeArgs a) {
-  extern __shared__ float s_f[];                     // [nsplit][JOIN_ROWS] weights
-  __shared__ __align__(16) float4 s_o[4][32][JOIN_ROWS];
-  __shared__ float s_m[16][JOIN_ROWS];
-  __shared__ float s_q[16][6][JOIN_ROWS];
-  __shared__ uint32_t s_bad[JOIN_ROWS];
-  const int tid = threadIdx.x, row = tid & 7, w = tid >> 6;
-  const int c = (tid >> 3) & 31, g = tid >> 8;       // channels 4 c .. 4 c + 3, sets g, g + 4, ...
-  const int head = blockIdx.x, tile = blockIdx.y >> 2, r32 = (blockIdx.y & 3) * JOIN_ROWS + row;
+  constexpr int R = JOIN_ROWS, C = 32 / PARTS, G = 4 * PARTS;
+  extern __shared__ float s_f[];                     // [nsplit][R] weights
+  __shared__ __align__(16) float4 s_o[G][C][R];
+  __shared__ float s_m[16][R];
+  __shared__ float s_q[16][7][R];
+  const int tid = threadIdx.x, row = tid % R, w = tid >> 6;
+  const int cc = tid / R % C, c = blockIdx.z * C + cc, g = tid / (C * R);   // channels 4 c .. 4 c + 3, sets g, g + G, ...
+  const int head = blockIdx.x, tile = blockIdx.y / (T_ROWS / R), r32 = blockIdx.y % (T_ROWS / R) * R + row;
   const int r = tile * 32 + r32;
   const float* const sets = a.part + ((int64_t)head * a.row_tiles + tile) * a.nsplit * T_FLOATS;
   const auto channels = [&](int i) { return reinterpret_cast<const float4*>(sets + (int64_t)i * T_FLOATS)[c * T_ROWS + r32]; };
   float4 y[JOIN_AHEAD];
 #pragma unroll
-  for (int k = 0; k < JOIN_AHEAD; ++k) y[k] = channels(min(g + 4 * k, a.nsplit - 1));
-  if (tid < JOIN_ROWS) s_bad[tid] = 0u;
+  for (int k = 0; k < JOIN_AHEAD; ++k) y[k] = channels(min(g + G * k, a.nsplit - 1));
 
   const auto lanes_max = [](float x) { return max_x32(max_x16(fmaxf(x, dpp_mov<0x128>(x)))); };   // over the lanes of a row: 8, 16, 32 apart
   const auto lanes_sum = [](float x) { return sum_x32(sum_x16(x + dpp_mov<0x128>(x))); };
-  constexpr int TRIP = 128;   // sets of a trip of the workgroup, eight a wave
+  constexpr int TRIP = 1024 / R;   // sets of a trip of the workgroup
   const auto quantity = [&](int i, int t) { return sets[(int64_t)min(i, a.nsplit - 1) * T_FLOATS + T_OFLOATS + t * T_ROWS + r32]; };
-  const int i0 = tid >> 3;
-  float z[7], m = -INFINITY;
-  if (w * 8 < a.nsplit) {   // the first trip's quantities at once
+  const int i0 = tid / R;
+  float z[8], m = -INFINITY;
+  if (w * (64 / R) < a.nsplit) {   // the first trip's quantities at once
 #pragma unroll
-    for (int t = 0; t < 7; ++t) z[t] = quantity(i0, t);
+    for (int t = 0; t < 8; ++t) z[t] = quantity(i0, t);
     m = z[T_M];
   }
   for (int i = i0 + TRIP; i < a.nsplit; i += TRIP) m = fmaxf(m, quantity(i, T_M));
   m = lanes_max(m);
-  if ((tid & 63) < 8) s_m[w][row] = m;
+  if ((tid & 63) < R) s_m[w][row] = m;
   __syncthreads();
   float M = s_m[0][row];
 #pragma unroll
   for (int i = 1; i < 16; ++i) M = fmaxf(M, s_m[i][row]);
-  float q[6] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};   // sums: L, sealed, EV; maxima: EVMAX, DMAX, VMAX
+  float q[7] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};   // sums: L, sealed, EV; maxima: EVMAX, DMAX, VMAX, BAD
   const auto take = [&](int i, const float* y) {
     if (i >= a.nsplit) return;
     const float f = y[T_M] == M ? 1.0f : __builtin_amdgcn_exp2f(y[T_M] - M);
-    s_f[i * JOIN_ROWS + row] = f;
+    s_f[i * R + row] = f;
     q[0] = fmaf(f, y[T_L], q[0]);
     q[1] = fmaf(f, y[T_SEALED], q[1]);
     q[2] = fmaf(f, y[T_EV], q[2]);
     q[3] = fmaxf(q[3], f * y[T_EVMAX]);
     q[4] = fmaxf(q[4], y[T_DMAX]);
     q[5] = fmaxf(q[5], y[T_VMAX]);
+    q[6] = fmaxf(q[6], y[T_BAD]);
   };
-  if (w * 8 < a.nsplit) take(i0, z);
+  if (w * (64 / R) < a.nsplit) take(i0, z);
   for (int i = i0 + TRIP; i < a.nsplit; i += TRIP) {
 #pragma unroll
-    for (int t = 0; t < 7; ++t) z[t] = quantity(i, t);
+    for (int t = 0; t < 8; ++t) z[t] = quantity(i, t);
     take(i, z);
   }
 #pragma unroll
-  for (int k = 0; k < 6; ++k) {
+  for (int k = 0; k < 7; ++k) {
     q[k] = k < 3 ? lanes_sum(q[k]) : lanes_max(q[k]);
-    if ((tid & 63) < 8) s_q[w][k][row] = q[k];
+    if ((tid & 63) < R) s_q[w][k][row] = q[k];
   }
   __syncthreads();
   float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   const auto add = [&](float f, const float4& v) { x.x = fmaf(f, v.x, x.x), x.y = fmaf(f, v.y, x.y), x.z = fmaf(f, v.z, x.z), x.w = fmaf(f, v.w, x.w); };
+  for (int i = g;; i += G * JOIN_AHEAD) {
 #pragma unroll
-  for (int k = 0; k < JOIN_AHEAD; ++k)
-    if (g + 4 * k < a.nsplit) add(s_f[(g + 4 * k) * JOIN_ROWS + row], y[k]);
-  for (int i = g + 4 * JOIN_AHEAD; i < a.nsplit; i += 4) add(s_f[i * JOIN_ROWS + row], channels(i));
-  s_o[g][c][row] = x;
-  __syncthreads();
-  const bool there = r < a.n * a.group, certifies = there && tid >= 512 && tid < 512 + JOIN_ROWS;
-  Certificate ct;
-  if (there && (tid < 256 || certifies)) {
+    for (int k = 0; k < JOIN_AHEAD; ++k)
+      if (i + G * k < a.nsplit) add(s_f[(i + G * k) * R + row], y[k]);
+    if (i + G * JOIN_AHEAD >= a.nsplit) break;
 #pragma unroll
-    for (int k = 0; k < 6; ++k) {
-      q[k] = s_q[0][k][row];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) q[k] = k < 3 ? q[k] + s_q[i][k][row] : fmaxf(q[k], s_q[i][k][row]);
-    }
-    if (certifies) {
-      ct = certificate(a, M, q[0], q[1], q[2], q[3], q[4], q[5]);
-    } else {
-#pragma unroll
-      for (int k = 1; k < 4; ++k) add(1.0f, s_o[k][c][row]);
-      if (put_channels(a, row_out(a, head, r), c, x, mean_factor(q[0]))) s_bad[row] = 1u;
-    }
+    for (int k = 0; k < JOIN_AHEAD; ++k) y[k] = channels(min(i + G * (JOIN_AHEAD + k), a.nsplit - 1));
   }
+  s_o[g][cc][row] = x;
   __syncthreads();
-  if (certifies) put_certificate(a, row_out(a, head, r), ct, s_bad[row] != 0u);
+  const bool certifies = tid >= 512 && tid < 512 + R && blockIdx.z == 0;
+  if (r >= a.n * a.group || (tid >= C * R && !certifies)) return;
+#pragma unroll
+  for (int k = 0; k < 7; ++k) {
+    q[k] = s_q[0][k][row];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) q[k] = k < 3 ? q[k] + s_q[i][k][row] : fmaxf(q[k], s_q[i][k][row]);
+  }
+  if (certifies) {
+    put_certificate(a, row_out(a, head, r), certificate(a, M, q[0], q[1], q[2], q[3], q[4], q[5]), q[6] != 0.0f);
+  } else {
+#pragma unroll
+    for (int k = 1; k < G; ++k) add(1.0f, s_o[k][cc][row]);
+    put_channels(a, row_out(a, head, r), c, x, mean_factor(q[0]));
+  }
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------------------
 
-// Rows of a KV group a workgroup takes.
-static int tree_rows(int n_rows) { return n_rows <= 32 ? 32 : (n_rows <= 64 ? 64 : (n_rows <= 128 ? 128 : 256)); }
-
-// Tokens of a tile: of more than 32 rows, or the pairs of blocks of the waves of few.
-static int tile_tokens(int rows) { return rows == 32 ? 32 * FEW_WAVES : (rows == 64 ? 128 : 64); }
-
-// Partial sets: as many workgroups as the device holds at a time, each with a tile of sealed blocks or of the other tokens.  Of few rows
-// the first tile and the other tokens are one workgroup's, which needs no second launch (8 heads, 4 nodes of 4 query heads, 200 tokens
-// 11.4 us, by two workgroups 13.3; two tiles, 400 tokens, 14.2, and by two 13.8).
-static int tree_splits(int n_cu, int64_t heads, int n_rows, int64_t sealed, int64_t others) {
-  const int rows = tree_rows(n_rows), tok = tile_tokens(rows);
-  const int64_t z = (n_rows + rows - 1) / rows, most = std::max<int64_t>(1, (int64_t)n_cu / (heads * z));
-  const int64_t tiles = (sealed + tok - 1) / tok;
-  return (int)std::min(most, rows > 32 ? tiles + (others + tok - 1) / tok : (tiles <= 1 ? 1 : tiles + 1));
+// Rows of a KV group a workgroup takes: 32, by the first kernel, where its waves have few turns each (it has them over sooner, and fewer sets to join),
+// else up to 256 by the second, which reconstructs a tile once for all of them.  One of the trailing and drafted tokens takes as long as two sealed
+// ones.  us by the first and the second kernel, turns a wave:
+//   64 rows   8 heads, 2000 tokens 13.1, 16.3 (0.5)   8 heads, 32000 33.3, 33.8 (8)   8 heads, 64000 54.0, 50.5 (16)
+//   128 rows  8 heads, 2000 15.5, 18.1 (1)   2 heads, 32000 23.2, 25.4 (4)   8 heads, 8000 23.0, 22.5 (4)   4 heads, 32000 31.5, 28.6 (8)
+//   256 rows  8 heads, 4000 23.2, 24.9 (4)   1 head, 32000 24.3, 31.9 (4)   8 heads, 8000 32.6, 29.2 (8)
+//   512 rows  4 heads, 4000 24.0, 26.9 (4.4)   8 heads, 2000 27.0, 23.7 (5)
+static int tree_rows(int n_cu, int64_t heads, int n_rows, int64_t sealed, int64_t others) {
+  const int64_t work = (sealed + 2 * others) * heads * ((n_rows + 31) / 32), turn = (int64_t)32 * FEW_WAVES * n_cu;
+  if (n_rows <= 32 || 2 * work <= (n_rows <= 64 ? 16 : 9) * turn) return 32;
+  return n_rows <= 64 ? 64 : (n_rows <= 128 ? 128 : 256);
 }
 
-// Sealed tiles of more than 32 rows by workgroup: the trailing and drafted tokens' tiles are the last workgroups', EXACT tiles' work each, and
+// Tokens of a tile, or of a turn of the first kernel's waves.
+static int tile_tokens(int rows) { return rows == 32 ? 32 * FEW_WAVES : (rows == 64 ? 128 : 64); }
+
+// Partial sets: as many workgroups as the device holds at a time, each with a tile of sealed blocks or of the other tokens.  Of 32 rows a workgroup
+// the first tile and the other tokens are one workgroup's, which needs no second launch (8 heads, 4 nodes of 4 query heads, 200 tokens
+// 11.4 us, by two workgroups 13.3; two tiles, 400 tokens, 14.2, and by two 13.8).
+static int tree_splits(int n_cu, int64_t heads, int n_rows, int rows, int64_t sealed, int64_t others) {
+  const int tok = tile_tokens(rows), exact = rows == 32 ? FEW_EXACT : tok;
+  const int64_t z = (n_rows + rows - 1) / rows, most = std::max<int64_t>(1, (int64_t)n_cu / (heads * z));
+  const int64_t tiles = (sealed + tok - 1) / tok, turns = tiles + (others + exact - 1) / exact;
+  return (int)std::min(most, rows == 32 && tiles <= 1 && others <= exact ? 1 : turns);
+}
+
+// Sealed tiles of the second kernel by workgroup: the trailing and drafted tokens' tiles are the last workgroups', EXACT tiles' work each, and
 // the sealed ones are dealt so that all end together.
 constexpr int EXACT = 3;
-static void tree_shares(TreeArgs& a, int n_rows) {
-  const int tok = tile_tokens(tree_rows(n_rows));
+static void tree_shares(TreeArgs& a, int rows) {
+  const int tok = tile_tokens(rows);
   const int tiles = (int)(((a.nb + 3) / 4 * 64 + tok - 1) / tok), exact = (a.trail + a.n + tok - 1) / tok;
   a.last = exact < a.nsplit ? exact : 0;
   a.least = std::max(0, (tiles + EXACT * exact) / a.nsplit - EXACT);
@@ -1219,7 +1237,9 @@ static void tree_shares(TreeArgs& a, int n_rows) {
 int64_t tree_ws_bytes(const Cache* c, int n_draft) {
   const int64_t heads = (int64_t)c->desc.batch * c->desc.n_kv_heads;
   const int n_rows = n_draft * (c->desc.n_q_heads / c->desc.n_kv_heads);
-  return heads * ((n_rows + 31) / 32) * tree_splits(c->n_cu, heads, n_rows, c->desc.max_tokens, n_draft + BLK - 1) * T_FLOATS * 4;
+  const auto most = [&](int rows) { return tree_splits(c->n_cu, heads, n_rows, rows, c->desc.max_tokens, n_draft + BLK - 1); };
+  const int64_t sets = std::max(most(32), most(n_rows <= 64 ? 64 : (n_rows <= 128 ? 128 : 256)));
+  return heads * ((n_rows + 31) / 32) * sets * T_FLOATS * 4;
 }
 
 template <int WR>
@@ -1249,14 +1269,15 @@ int32_t launch_tree(const Cache* c, int layer, const __half* q, const __half* kd
   a.group = c->desc.n_q_heads / c->desc.n_kv_heads;
   const int n_rows = n_draft * a.group;
   a.row_tiles = (n_rows + 31) / 32;
-  a.nsplit = tree_splits(c->n_cu, heads, n_rows, a.nb * BLK, a.trail + a.n);
-  tree_shares(a, n_rows);
+  const int rows = tree_rows(c->n_cu, heads, n_rows, a.nb * BLK, a.trail + a.n);
+  a.nsplit = tree_splits(c->n_cu, heads, n_rows, rows, a.nb * BLK, a.trail + a.n);
+  if (rows > 32) tree_shares(a, rows);
   a.O = O;
   a.cert = cert;
   a.flags = flags;
   a.tol = tol;
-  switch (tree_rows(n_rows)) {
-    case 32: tree_few_kernel<<<dim3((uint32_t)heads, (uint32_t)a.nsplit, 1), 64 * FEW_WAVES, 0, st>>>(a); break;
+  switch (rows) {
+    case 32: tree_few_kernel<<<dim3((uint32_t)heads, (uint32_t)a.nsplit, (uint32_t)a.row_tiles), 64 * FEW_WAVES, 0, st>>>(a); break;
     case 64: launch_many<2>(a, heads, st); break;
     case 128: launch_many<4>(a, heads, st); break;
     default: launch_many<8>(a, heads, st); break;
@@ -1268,8 +1289,10 @@ int32_t launch_tree(const Cache* c, int layer, const __half* q, const __half* kd
     tree_join_few_kernel<8><<<grid, JOIN_FEW_THREADS, 0, st>>>(a);
   else if (a.nsplit <= 16)
     tree_join_few_kernel<16><<<grid, JOIN_FEW_THREADS, 0, st>>>(a);
+  else if (a.nsplit > 4 * JOIN_AHEAD && heads * a.row_tiles * (T_ROWS / JOIN_ROWS) * 4 <= c->n_cu)
+    tree_join_kernel<4><<<dim3(grid.x, grid.y, 4), 1024, (size_t)a.nsplit * JOIN_ROWS * 4, st>>>(a);
   else
-    tree_join_kernel<<<grid, 1024, (size_t)a.nsplit * JOIN_ROWS * 4, st>>>(a);
+    tree_join_kernel<1><<<grid, 1024, (size_t)a.nsplit * JOIN_ROWS * 4, st>>>(a);
   CQA_HIP(hipGetLastError());
   return CQA_OK;
 }
