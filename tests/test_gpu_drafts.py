@@ -316,6 +316,51 @@ def test_lengths_at_the_tiles_ends(g, n):
                 assert_nodes(ref, O, cert, flags, n_tokens)
 
 
+# caches that are long for the device, by many sequences or tokens: 33 .. 64, 65 .. 128, up to 256 rows and several tiles of 256; a sequence by one workgroup, by
+# some, and by more than 32; without sealed tokens
+WIDE = [(87, 3, 4, 1029, 16), (96, 1, 4, 2811, 13), (88, 3, 4, 300, 27), (48, 2, 4, 1029, 19), (88, 3, 4, 150, 40), (48, 1, 4, 1029, 50),
+        (44, 3, 2, 75, 130), (24, 1, 4, 603, 130), (24, 1, 4, 0, 256), (12, 2, 4, 5, 255), (4, 1, 4, 10029, 64), (4, 1, 1, 20007, 201), (4, 1, 4, 12001, 8),
+        (4, 1, 4, 20007, 32)]
+
+
+@pytest.mark.parametrize("bt,hkv,g,n_tokens,n", WIDE)
+def test_caches_that_are_long_for_the_device(bt, hkv, g, n_tokens, n):
+    """Four sequences over and over, behind a reset: one as it comes, one with drafts that are no finite numbers, one with nodes that attend no draft,
+    a chunk."""
+    print("tree of many rows", bt, hkv, g, n_tokens, n, flush=True)
+    rng = np.random.default_rng(50 + n)
+    k, v, q, kd, vd = make(rng, 4, hkv, g, n_tokens, n, keys="student" if n % 2 else "normal", peaked=n % 3 == 0)
+    seen = random_tree(rng, 4, n)
+    seen[2, [0, n // 3, n - 1]] = False
+    seen[3] = np.tril(np.ones((n, n), bool))
+    nodes = np.unique(np.concatenate([[0, n // 3, n - 1], rng.choice(n, 6)]))
+    oc = oracle.OracleLayerCache(4, hkv)
+    oc.append(k, v)
+    ref = drafts.tree_decode(oc, q[:, nodes], kd, vd, seen[:, nodes], oracle.Tolerances())
+    kd[1, :, 1, 9], vd[1, :, n - 2, 100] = np.nan, np.inf
+    hit = np.zeros((4, n), bool)
+    hit[1] = seen[1, :, 1] | seen[1, :, n - 2]
+    assert hit[1].any() and not hit[1].all()
+    times = (bt + 3) // 4
+    wide = lambda x: np.tile(x, (times,) + (1,) * (x.ndim - 1))[:bt]  # noqa: E731
+    with GpuLayerCache(bt, hkv * g, hkv, n_tokens + 64, tier2=False) as gc:
+        old = np.full((1, 1, n_tokens + 64, 128), 50.0, np.float16)
+        old[..., ::3] = -700.0
+        old[:, :, 1::2] *= -1
+        gc.append(*[np.broadcast_to(old, (bt, hkv) + old.shape[2:])] * 2)   # larger widths and values than any that follow
+        gc.cqa.cqa_cache_reset(gc.h, 0)
+        if n_tokens:
+            gc.append(wide(k), wide(v))
+        O, cert, flags = tree_call(gc, wide(q), wide(kd), wide(vd), drafts.mask_words(wide(seen)))
+    for at in range(4):
+        for y in (O, flags, *cert.values()):
+            assert all(np.array_equal(z, y[at], equal_nan=True) for z in y[at::4])
+        assert np.isnan(O[at, hit[at]]).all() and (flags[at, hit[at]] == oracle.FLAG_PRECOND).all()
+        keep = [i for i, node in enumerate(nodes) if not hit[at, node]]
+        which = nodes[keep]
+        assert_nodes([[ref[at][i] for i in keep]], O[at:at + 1, which], {f: y[at:at + 1, which] for f, y in cert.items()}, flags[at:at + 1, which], at)
+
+
 def test_a_cache_that_is_filled_again():
     """What an earlier, longer sequence left behind the last block of a record is not the new one's: neither widths nor errors."""
     print("tree after a reset", flush=True)
