@@ -1,8 +1,9 @@
 // Attention of drafted tokens (a tree, or a chunk of a prompt) over the quantized cache, with the certificate of every
 // (node, query head): split pass on the matrix cores and the joining of its partial sets.
 //
-// The rows of a KV group are its n_draft nodes times its G query heads, and all of them attend the same sealed blocks, so one
-// workgroup reconstructs a tile of keys and values once, in FP16, into LDS, and its waves multiply it with up to 256 rows.
+// The rows of a KV group are its n_draft nodes times its G query heads, and all of them attend the same sealed blocks.  Two kernels: 32 rows a workgroup, whose
+// waves reconstruct pairs of blocks in registers, each for itself; or up to 256 rows, for which a workgroup reconstructs a tile of keys and values
+// once, into LDS (tree_rows says when).
 //   k^ = FP16(code sigma + z),  v^ = FP16(code scale + offset)
 // FP16 operands, FP32 accumulation: with the two-term scaled queries of the single-token pass the operand forming would cost
 // 128 multiplications per (row, block), more than the products.  What the rounding of the reconstruction adds is in the certificate:
@@ -71,7 +72,7 @@ struct TreeArgs {
   int n_kv, group;
   int row_tiles;           // of 32 rows
   int nsplit;              // partial sets per row; 1: the split pass finishes the rows itself
-  int share, over, least, last;   // more rows: sealed tiles of a workgroup, how many have one more, those of the `last` workgroups
+  int share, over, least, last;   // many rows: sealed tiles of a workgroup, how many have one more, those of the `last` workgroups
   __half* O;               // [Bt][n][Hq][128]
   cqa_node_cert* cert;     // [Bt][n][Hq]
   uint32_t* flags;
@@ -390,12 +391,12 @@ __device__ __forceinline__ void put_rows(const TreeRows& w, float* to) {
       const int c = (r4 >> 1) * 16 + ct * 4 + (r4 & 1) * 2 + half;
       reinterpret_cast<float4*>(to)[c * T_ROWS + row] = make_float4(w.o[ct][4 * r4], w.o[ct][4 * r4 + 1], w.o[ct][4 * r4 + 2], w.o[ct][4 * r4 + 3]);
     }
-  float none = 0.0f;   // stays, unless a channel is no finite number
+  float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};   // stay, unless a channel is no finite number
 #pragma unroll
-  for (int ct = 0; ct < 4; ++ct)
+  for (int r = 0; r < 16; ++r)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) none = fmaf(0.0f, w.o[ct][r], none);
-  const float bad = max_x32(none == 0.0f ? 0.0f : 1.0f);
+    for (int ct = 0; ct < 4; ++ct) none[ct] = fmaf(0.0f, w.o[ct][r], none[ct]);
+  const float bad = max_x32(none[0] + none[1] + none[2] + none[3] == 0.0f ? 0.0f : 1.0f);
   if (half == 0) {
     float* const st = to + T_OFLOATS + row;
     st[T_BAD * T_ROWS] = bad;
@@ -603,16 +604,20 @@ constexpr int FEW_WAVES = 8;
 constexpr int FEW_KM_HALF = 64 + 4, FEW_KM_KIND = 2 * FEW_KM_HALF, FEW_KM_BLK = 2 * FEW_KM_KIND + 8;   // floats; padded: the four
 constexpr int FEW_VM_BLK = VM_BYTES + 32, FEW_W_RUN = 32 * 16 + 16;                                   // addresses of a read in four sets of banks
 constexpr int FEW_KM = 0, FEW_VM = FEW_KM + 2 * FEW_KM_BLK * 4, FEW_W = FEW_VM + 2 * FEW_VM_BLK, FEW_META_END = FEW_W + D / 8 * FEW_W_RUN;   // widths [run of 8 channels][32 blocks]
-constexpr int FEW_EXACT = 96;   // trailing and drafted tokens of a turn
+constexpr int FEW_EXACT = 96;   // trailing and drafted tokens of a turn, at most
 static_assert(FEW_META_END <= T_FLOATS * 4 && 2 * FEW_EXACT * D * 2 <= FEW_WAVES * T_FLOATS * 4 && FEW_VM % 16 == 0 && FEW_W % 16 == 0,
               "a wave's part of LDS");
 
+// EXACT: tokens of a turn of the trailing and drafted ones.  64 where they are no more, for each thread fetches its share of EXACT (1 KV head, 1029 tokens, 8 nodes
+// 12.0 us a call, with 96 12.5; 8 heads, 60 tokens, 12 nodes 10.2, 10.8), else 96 (64 nodes 11.0, by two turns of 64 12.3; 256 nodes, 500 tokens 22.4, 26.0).
+template <int EXACT>
 __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
+  static_assert(EXACT <= FEW_EXACT, "LDS");
   fetch_args<sizeof(TreeArgs)>();
   __shared__ __align__(16) float s_set[FEW_WAVES][T_FLOATS];
   __shared__ __align__(16) uint8_t s_q[Q_TILE];
-  __shared__ __align__(16) float s_norm[FEW_EXACT];
-  __shared__ __align__(16) uint8_t s_bad[FEW_EXACT];
+  __shared__ __align__(16) float s_norm[EXACT];
+  __shared__ __align__(16) uint8_t s_bad[EXACT];
   const int tid = threadIdx.x, l = tid & 63, n32 = l & 31, half = l >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t head = blockIdx.x;
@@ -733,20 +738,20 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
     wave_sync();
   }
   rows.sealed = rows.sum;
-  // The other tokens, dealt from the workgroup on whose turn is the next, which fetches them together; three of its waves attend them.
-  for (int t0 = (split + a.nsplit - (units + FEW_WAVES - 1) / FEW_WAVES % a.nsplit) % a.nsplit * FEW_EXACT; t0 < a.trail + a.n; t0 += a.nsplit * FEW_EXACT) {
+  // The other tokens, dealt from the workgroup on whose turn is the next, which fetches them together; as many of its waves as they have pairs of blocks attend them.
+  for (int t0 = (split + a.nsplit - (units + FEW_WAVES - 1) / FEW_WAVES % a.nsplit) % a.nsplit * EXACT; t0 < a.trail + a.n; t0 += a.nsplit * EXACT) {
     uint4* const s_k = reinterpret_cast<uint4*>(s_set);
-    uint4* const s_v = s_k + 16 * FEW_EXACT;
+    uint4* const s_v = s_k + 16 * EXACT;
     const int blk = 2 * w + half;
     const uint32_t bits = open_tokens(a, b, rows.node, t0 + blk * BLK);
-    if (tid < FEW_EXACT / 4) reinterpret_cast<uint32_t*>(s_bad)[tid] = 0u;
+    if (tid < EXACT / 4) reinterpret_cast<uint32_t*>(s_bad)[tid] = 0u;
     __syncthreads();
-    load_exact<64 * FEW_WAVES, FEW_EXACT>(a, head, t0, tid, s_k, s_v, s_norm, s_bad);
+    load_exact<64 * FEW_WAVES, EXACT>(a, head, t0, tid, s_k, s_v, s_norm, s_bad);
     __syncthreads();
-    if (w * 32 < min(FEW_EXACT, a.trail + a.n - t0)) {
+    if (w * 32 < min(EXACT, a.trail + a.n - t0)) {
       open_exact(rows, bits, s_norm + blk * BLK, s_bad + blk * BLK);
       attend32(
-          rows, true, bits, 0.0f, [&](int ks) { return __builtin_bit_cast(f16x8, s_k[(half * 8 + ks) * FEW_EXACT + w * 32 + n32]); }, [] {},
+          rows, true, bits, 0.0f, [&](int ks) { return __builtin_bit_cast(f16x8, s_k[(half * 8 + ks) * EXACT + w * 32 + n32]); }, [] {},
           [&](int oct, int ct) { return __builtin_bit_cast(f16x8, s_v[(blk * 2 + oct) * D + ct * 32 + n32]); });
     }
     __syncthreads();   // (the next ones, or the waves' sets, come where these are)
@@ -1215,7 +1220,7 @@ static int tile_tokens(int rows) { return rows == 32 ? 32 * FEW_WAVES : (rows ==
 // the first tile and the other tokens are one workgroup's, which needs no second launch (8 heads, 4 nodes of 4 query heads, 200 tokens
 // 11.4 us, by two workgroups 13.3; two tiles, 400 tokens, 14.2, and by two 13.8).
 static int tree_splits(int n_cu, int64_t heads, int n_rows, int rows, int64_t sealed, int64_t others) {
-  const int tok = tile_tokens(rows), exact = rows == 32 ? FEW_EXACT : tok;
+  const int tok = tile_tokens(rows), exact = rows == 32 ? FEW_EXACT : tok;   // (64 others at most are a turn as well)
   const int64_t z = (n_rows + rows - 1) / rows, most = std::max<int64_t>(1, (int64_t)n_cu / (heads * z));
   const int64_t tiles = (sealed + tok - 1) / tok, turns = tiles + (others + exact - 1) / exact;
   return (int)std::min(most, rows == 32 && tiles <= 1 && others <= exact ? 1 : turns);
@@ -1277,7 +1282,14 @@ int32_t launch_tree(const Cache* c, int layer, const __half* q, const __half* kd
   a.flags = flags;
   a.tol = tol;
   switch (rows) {
-    case 32: tree_few_kernel<<<dim3((uint32_t)heads, (uint32_t)a.nsplit, (uint32_t)a.row_tiles), 64 * FEW_WAVES, 0, st>>>(a); break;
+    case 32: {
+      const dim3 grid((uint32_t)heads, (uint32_t)a.nsplit, (uint32_t)a.row_tiles);
+      if (a.trail + a.n <= 64)
+        tree_few_kernel<64><<<grid, 64 * FEW_WAVES, 0, st>>>(a);
+      else
+        tree_few_kernel<FEW_EXACT><<<grid, 64 * FEW_WAVES, 0, st>>>(a);
+      break;
+    }
     case 64: launch_many<2>(a, heads, st); break;
     case 128: launch_many<4>(a, heads, st); break;
     default: launch_many<8>(a, heads, st); break;
