@@ -599,7 +599,7 @@ __device__ __forceinline__ float* set_of(const TreeArgs& a, int64_t head, int ti
 // lanes share, goes through LDS, the wave's own part of it, so that no wave waits for another until the waves' sets are joined.
 // Two waves a SIMD: what one is to read from LDS is requested a product ahead, and a pair's metadata and codes as soon as those of the pair before
 // are used.  4 x 8 KV heads of 32768 tokens, 5 nodes of 4 query heads: 60 us for 303 MB, 5.05 TB/s, what a large copy reaches (each read where it is
-// used 66, the widths' products for each pair by itself among it); vector ALU 60 % busy, matrix cores 20 %.
+// used 66, the widths' products for each pair by itself among it); vector ALU 70 % busy, matrix cores 15 %.
 constexpr int FEW_WAVES = 8;
 constexpr int FEW_KM_HALF = 64 + 4, FEW_KM_KIND = 2 * FEW_KM_HALF, FEW_KM_BLK = 2 * FEW_KM_KIND + 8;   // floats; padded: the four
 constexpr int FEW_VM_BLK = VM_BYTES + 32, FEW_W_RUN = 32 * 16 + 16;                                   // addresses of a read in four sets of banks
