@@ -1224,8 +1224,8 @@ int32_t cqa_cache_read(const cqa_cache* h, int32_t layer, int64_t first, int64_t
 
 static int32_t check_draft(const cqa_cache* h, int32_t n_draft) {
   if (h == nullptr || n_draft < 1) return CQA_ERR_INVALID_ARG;
-  // a workgroup column per KV group of the batch
-  if (n_draft > CQA_MAX_DRAFT || (int64_t)h->impl.desc.batch * h->impl.desc.n_kv_heads > 0xffffff) return CQA_ERR_UNSUPPORTED;
+  // a workgroup of up to 1024 threads per KV group of the batch side by side, 32 bits of threads
+  if (n_draft > CQA_MAX_DRAFT || (int64_t)h->impl.desc.batch * h->impl.desc.n_kv_heads > 0x3fffff) return CQA_ERR_UNSUPPORTED;
   return CQA_OK;
 }
 

@@ -1218,7 +1218,7 @@ static int tile_tokens(int rows) { return rows == 32 ? 32 * FEW_WAVES : (rows ==
 
 // Partial sets: as many workgroups as the device holds at a time, each with a tile of sealed blocks or of the other tokens.  Of 32 rows a workgroup
 // the first tile and the other tokens are one workgroup's, which needs no second launch (8 heads, 4 nodes of 4 query heads, 200 tokens
-// 11.4 us, by two workgroups 13.3; two tiles, 400 tokens, 14.2, and by two 13.8).
+// 11.4 us, by two workgroups 12.6; two tiles, 400 tokens, by one 13.8, by three 12.2).
 static int tree_splits(int n_cu, int64_t heads, int n_rows, int rows, int64_t sealed, int64_t others) {
   const int tok = tile_tokens(rows), exact = rows == 32 ? FEW_EXACT : tok;   // (64 others at most are a turn as well)
   const int64_t z = (n_rows + rows - 1) / rows, most = std::max<int64_t>(1, (int64_t)n_cu / (heads * z));
