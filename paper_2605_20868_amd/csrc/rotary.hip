@@ -64,7 +64,8 @@ __device__ __forceinline__ void sin_cos_of(uint64_t turn, int64_t p, float m, fl
   c *= m;
 }
 
-// P = 8: a thread has 8 pairs, where their channels come in whole runs of 8 (rot_dim a multiple of 16); P = 1: one pair, any rot_dim.
+// P = 8: a thread has 8 pairs, where their channels come in whole runs of 8 (rot_dim a multiple of 16); P = 1: one pair, any rot_dim (the two prompts
+// of the figures above by P = 1: 86 us for 35, 73 for 42).
 template <int TI, int TO, int P>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
   constexpr int UNITS = D / 2 / P;   // threads a row takes
@@ -160,7 +161,8 @@ int32_t launch_rotary(const Rotary& r, const int64_t* positions, int64_t pos_bat
   const int slots = wide ? 32 : 4;   // rows side by side in a workgroup
   a.tok_shift = 0;
   while ((1 << a.tok_shift) < slots && (1 << a.tok_shift) < n_tokens) ++a.tok_shift;
-  // As many heads a thread as leave the device's 256 compute units 8 workgroups each: the sines are shared by them.
+  // As many heads a thread as leave the device's 256 compute units 8 workgroups each: the sines are shared by them.  (4, 8, 16, 32 each: 8192 tokens x 40 heads,
+  // BF16 to FP16, 33.9, 35.3, 36.0, 39.8 us; 2 x 4099 x 24 in FP32 45.7, 42.4, 41.3, 41.3; a row requested ahead of the one before 36.3, 34.6 and 49.9, 45.1.)
   const int n_all = a.rows[0].n_heads + a.rows[1].n_heads;
   const int64_t tiles = ((n_tokens - 1) >> a.tok_shift) + 1;
   a.heads_per = slots >> a.tok_shift;
