@@ -844,7 +844,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   int u = from;
   load(u);
   {
-    static_assert(8 * Q_TILE <= S::WIDTH_AT, "the queries' way leads past the widths");
+    static_assert(8 * Q_TILE <= S::BYTES, "the queries on their way");
     uint8_t* const s_q = s_main + w * Q_TILE;
     uint4 x[8];
 #pragma unroll
@@ -854,7 +854,6 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
     wave_sync();
     start_rows(rows, a, tile0 + wr, s_q);
   }
-  for (int i = tid; i < 2 * 32 * D * 2 / 4; i += 512) reinterpret_cast<uint32_t*>(s_main + S::WIDTH_AT)[i] = 0u;
   int fresh = 0, ring = 0;   // blocks whose widths have come into the half `ring`
   int buf = 0;
   __syncthreads();
@@ -995,7 +994,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
         constexpr int I = i_.value;
         product(i_);
         if constexpr (I + AHEAD < PRODUCTS) operand(std::integral_constant<int, I + AHEAD>{});
-        // (keys, behind the last tile: of the head's first record, which nothing reads, and its widths, which are the head's)
+        // (keys, behind the last tile: of the head's first record, which nothing reads)
         if constexpr (I >= FROM)
           each<EACH>([&](auto k_) {
             constexpr int P = (I - FROM) * EACH + k_.value, QD = P / PIECES, J = P % PIECES;
@@ -1011,7 +1010,9 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
         __builtin_amdgcn_sched_barrier(0);
       });
       if (full || last) {
-        if (wt == 0) bound_scores(rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(width_at(ring, half * 8 + ks, n32)); });
+        // (up to the last block that has come: on the last tile, other waves write the first record's widths behind it meanwhile)
+        const int blk = min(n32, fresh - 1);
+        if (wt == 0) bound_scores(rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(width_at(ring, half * 8 + ks, blk)); });
       }
       ring = ring1;
       fresh = slot + BLKS;
