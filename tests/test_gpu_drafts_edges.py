@@ -1,5 +1,7 @@
 """Drafted tokens over the cache where attention and its certificate are most easily wrong: against oracle/drafts.py, with the tolerances of
 test_gpu_drafts.py."""
+import math
+
 import numpy as np
 import pytest
 
@@ -43,3 +45,64 @@ def test_widths_of_two_blocks_do_not_meet(n, n_tokens):
         for y in (O, flags, *cert.values()):
             assert all(np.array_equal(z, y[at]) for z in y[at::4])
         assert_nodes(ref[at:at + 1], O[at:at + 1, nodes], {f: y[at:at + 1, nodes] for f, y in cert.items()}, flags[at:at + 1, nodes], at)
+
+
+SCORE = 1.0 / math.sqrt(128.0)
+
+
+def determined(oc, q, kd, seen, scale):
+    """bool [Bt, n, Hq]: rows whose result FP32 sums of products determine.  A score of 128 products is off by at most 128 * 2^-23 sum |q k|;
+    the largest one has to be beyond twice that, and 30 (e^-30 = 1e-13) on top, of the next -- or to be the same number by its keys."""
+    k_all, _ = drafts.read_back(oc, 0, oc.length)
+    bt, n, hq, _ = q.shape
+    g = hq // oc.hkv
+    out = np.ones((bt, n, hq), bool)
+    for b, i, h in np.ndindex(bt, n, hq):
+        k = np.concatenate([drafts.to_fp16(k_all[b, h // g]), kd[b, h // g][seen[b, i]]]).astype(np.float64)
+        x = q[b, i, h].astype(np.float64)
+        s = (k @ x) * SCORE
+        if len(s) < 2 or np.abs(s).max() < 1000.0:
+            continue
+        off = 128 * 2.0 ** -23 * (np.abs(k) @ np.abs(x)).max() * SCORE
+        near = s >= s.max() - 2 * off - 30.0
+        out[b, i, h] = (k[near] == k[near][0]).all()
+    return out
+
+
+# few rows; 64, 128 and 256 rows by a workgroup; several tokens' turns; nothing sealed
+LARGE = [(1, 1, 6, 0), (2, 1, 6, 37), (1, 2, 27, 700), (1, 1, 4, 3001), (256, 1, 13, 1157), (160, 1, 27, 613), (160, 1, 64, 203)]
+
+
+@pytest.mark.parametrize("scale", [400.0, 2000.0, 8000.0, 50000.0, -2000.0, -50000.0])
+@pytest.mark.parametrize("bt,hkv,n,n_tokens", LARGE)
+def test_large_keys_meet_large_queries(bt, hkv, n, n_tokens, scale):
+    """Scores up to 2^35 of either sign: of FP32's spacing there, the largest weight must not be more than FP16 holds, nor nothing.  Every other
+    head has ordinary scores over the same keys."""
+    print("tree large scores", bt, hkv, n, n_tokens, scale, flush=True)
+    rng = np.random.default_rng(70 + n_tokens)
+    few, size = min(bt, 4), abs(scale)
+    u = rng.choice([-1.0, 1.0], 128)
+    around = lambda shape: 1.0 + 0.1 * rng.standard_normal(shape)  # noqa: E731
+    k, kd = (np.clip(u * size * around((few, hkv, m, 128)), -65504.0, 65504.0).astype(np.float16) for m in (n_tokens, n))
+    v, vd = (workloads.normal_f16(rng, (few, hkv, m, 128)) for m in (n_tokens, n))
+    q = np.clip(u * scale * around((few, n, hkv * 4, 128)), -65504.0, 65504.0)
+    q[:, :, 1::2] *= 20.0 / (128.0 * size * size) / SCORE
+    q = q.astype(np.float16)
+    seen = random_tree(rng, few, n)
+    nodes = np.unique([0, 1, n // 2, n - 1])
+    oc = oracle.OracleLayerCache(few, hkv)
+    oc.append(k, v)
+    tol = oracle.Tolerances(key_bound_mode=2)
+    ref = drafts.tree_decode(oc, q[:, nodes], kd, vd, seen[:, nodes], tol)
+    clear = determined(oc, q[:, nodes], kd, seen[:, nodes], scale)
+    assert clear.mean() > 0.9
+    with GpuLayerCache(bt, hkv * 4, hkv, max(n_tokens, 16), tier2=False) as gc:
+        if n_tokens:
+            gc.append(sequences(k, bt), sequences(v, bt))
+        O, cert, flags = tree_call(gc, sequences(q, bt), sequences(kd, bt), sequences(vd, bt), drafts.mask_words(sequences(seen, bt)),
+                                   gc.cqa.Tolerances(key_bound_mode=2))
+    assert np.isfinite(O).all() and all(np.isfinite(x).all() for x in cert.values()) and not (flags & oracle.FLAG_PRECOND).any()
+    for b, i, h in np.ndindex(few, len(nodes), hkv * 4):
+        if clear[b, i, h]:
+            at = (slice(b, b + 1), slice(nodes[i], nodes[i] + 1), slice(h, h + 1))
+            assert_nodes([[[ref[b][i][h]]]], O[at], {f: y[at] for f, y in cert.items()}, flags[at], (b, nodes[i], h))
