@@ -535,8 +535,8 @@ typedef struct cqa_node_cert {
  * flags: KEY, VAL, TOTAL, PRECOND by tol's thresholds, force_flags; they only REQUEST precision, there is no ladder for
  * nodes: a program accepts a path up to its first flagged node and has the token from there on served by a step of the
  * single-token calls.  A node that attends nothing (an empty cache and mask) returns O = 0, lse = -inf, zeros, and no
- * flag of its own.  One that attends a drafted key or value that is no finite number returns NaN and PRECOND; other
- * nodes are not touched by it.
+ * flag of its own.  One that attends a drafted key or value that is no finite number, or that attends anything by a query
+ * that is none, returns NaN and PRECOND; other nodes, and other heads of a query, are not touched by it.
  * The mask is read on the device: calls can be recorded into a HIP graph (the length of the cache is that at the recording).
  * The current device must be the cache's.  Asynchronous on `stream`; uses none of the handle's workspaces, so that calls with
  * workspaces of their own may overlap with each other and with decode calls.

@@ -376,9 +376,12 @@ __device__ __forceinline__ void open_exact(TreeRows& w, uint32_t bits, const flo
   if (bits & hit) w.sum = NAN;   // stays
 }
 
-// Joins the halves of the rows.
-__device__ __forceinline__ void end_rows(TreeRows& w) {
+// Joins the halves of the rows.  open: not 0 where the lane's row attends tokens that the wave has had.  Where these have left it no weight, all its scores are
+// -inf, as a query that is not finite has them: the sum is no number, and 0 is that of a row that attends nothing.
+__device__ __forceinline__ void end_rows(TreeRows& w, uint32_t open) {
   w.sum = sum_x32(w.sum);
+  const float any = max_x32(open != 0u ? 1.0f : 0.0f);
+  if (w.sum == 0.0f && any != 0.0f) w.sum = NAN;
   w.sealed = sum_x32(w.sealed);
   w.ev = sum_x32(w.ev);
   w.evmax = max_x32(w.evmax);
@@ -742,6 +745,7 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
     wave_sync();
   }
   rows.sealed = rows.sum;
+  uint32_t open = split * FEW_WAVES + w < units;
   // The other tokens, dealt from the workgroup on whose turn is the next, which fetches them together; as many of its waves as they have pairs of blocks attend them.
   for (int t0 = (split + a.nsplit - (units + FEW_WAVES - 1) / FEW_WAVES % a.nsplit) % a.nsplit * EXACT; t0 < a.trail + a.n; t0 += a.nsplit * EXACT) {
     uint4* const s_k = reinterpret_cast<uint4*>(s_set);
@@ -753,6 +757,7 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
     load_exact<64 * FEW_WAVES, EXACT>(a, head, t0, tid, s_k, s_v, s_norm, s_bad);
     __syncthreads();
     if (w * 32 < min(EXACT, a.trail + a.n - t0)) {
+      open |= bits;
       open_exact(rows, bits, s_norm + blk * BLK, s_bad + blk * BLK);
       attend32(
           rows, true, bits, 0.0f, [&](int ks) { return __builtin_bit_cast(f16x8, s_k[(half * 8 + ks) * EXACT + w * 32 + n32]); }, [] {},
@@ -760,7 +765,7 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
     }
     __syncthreads();   // (the next ones, or the waves' sets, come where these are)
   }
-  end_rows(rows);
+  end_rows(rows, open);
   put_rows(rows, s_set[w]);
   __syncthreads();
   if (a.nsplit > 1) {
@@ -1051,6 +1056,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
     add_values(buf ^ 1);
   }
   rows.sealed = rows.sum;
+  uint32_t open = from < units && (int64_t)from * BLKS + wt * MT * 2 < a.nb;
   // the other tokens' tiles: dealt to the workgroups from the last one down
   for (int t0 = (a.nsplit - 1 - split) * TOK; t0 < a.trail + a.n; t0 += a.nsplit * TOK, buf ^= 1) {
     uint4* const s_k = reinterpret_cast<uint4*>(s_main + buf * S::TILE);
@@ -1066,6 +1072,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const int unit = wt * MT + mt, blk = unit * 2 + half;
+      open |= bits[mt];
       open_exact(rows, bits[mt], s_norm + blk * BLK, s_bad + blk * BLK);
       attend32(
           rows, true, bits[mt], 0.0f, [&](int ks) { return key_of(s_k, unit, ks); }, [] {}, [&](int oct, int ct) { return value_of(s_v, blk, oct, ct); });
@@ -1075,7 +1082,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
   if (w < 4 && l == 0) s_norm[w] = nu;
   __syncthreads();
   rows.vmax = fmaxf(rows.vmax, fmaxf(fmaxf(s_norm[0], s_norm[1]), fmaxf(s_norm[2], s_norm[3])));
-  end_rows(rows);
+  end_rows(rows, open);
   if constexpr (S::WT == 1) {
     if (tile0 + wr >= a.row_tiles) return;
     if (a.nsplit > 1)

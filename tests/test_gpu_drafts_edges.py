@@ -106,3 +106,44 @@ def test_large_keys_meet_large_queries(bt, hkv, n, n_tokens, scale):
         if clear[b, i, h]:
             at = (slice(b, b + 1), slice(nodes[i], nodes[i] + 1), slice(h, h + 1))
             assert_nodes([[[ref[b][i][h]]]], O[at], {f: y[at] for f, y in cert.items()}, flags[at], (b, nodes[i], h))
+
+
+# nothing sealed; one workgroup, some, more than 16 and more than 32 of few rows; 64, 128 and 256 rows, by one workgroup and by some
+@pytest.mark.parametrize("bt,hkv,n,n_tokens", [(2, 1, 6, 0), (1, 2, 70, 0), (1, 1, 6, 5), (1, 1, 6, 200), (1, 1, 7, 2003), (1, 2, 30, 6000), (1, 1, 6, 12000),
+                                               (256, 1, 13, 1030), (96, 1, 27, 1001), (160, 1, 64, 203), (4, 1, 64, 10029)])
+def test_queries_that_are_not_finite(bt, hkv, n, n_tokens):
+    """All scores of such a row can be -inf, which leaves its weights nothing as an empty mask does: only the latter is an answer."""
+    print("tree queries not finite", bt, hkv, n, n_tokens, flush=True)
+    rng = np.random.default_rng(80 + n_tokens)
+    few = min(bt, 2)
+    k, kd = (workloads.normal_f16(rng, (few, hkv, m, 128)) for m in (n_tokens, n))
+    v, vd = (workloads.normal_f16(rng, (few, hkv, m, 128)) for m in (n_tokens, n))
+    k[..., 7], kd[..., 7] = np.float16(0.5), np.float16(0.5)
+    q = workloads.normal_f16(rng, (few, n, hkv * 4, 128))
+    seen = random_tree(rng, few, n)
+    seen[:, n // 2] = False
+    hit = np.zeros((few, n, hkv * 4), bool)
+    for i, x in ((0, -np.inf), (1, np.inf), (2, np.nan), (n - 1, -np.inf), (n // 2, -np.inf)):
+        q[:, i, 1, 7] = x
+        hit[:, i, 1] = True
+    if n_tokens == 0:   # this node attends nothing, whatever its query
+        hit[:, n // 2] = False
+    nodes = np.unique([0, 1, 2, n // 2, n - 1])
+    oc = oracle.OracleLayerCache(few, hkv)
+    oc.append(k, v)
+    plain = np.where(np.isfinite(q), q, np.float16(0.0))
+    ref = drafts.tree_decode(oc, plain[:, nodes], kd, vd, seen[:, nodes], oracle.Tolerances())
+    wide = lambda x: np.tile(x, ((bt + few - 1) // few,) + (1,) * (x.ndim - 1))[:bt]  # noqa: E731
+    with GpuLayerCache(bt, hkv * 4, hkv, max(n_tokens, 16), tier2=False) as gc:
+        if n_tokens:
+            gc.append(wide(k), wide(v))
+        O, cert, flags = tree_call(gc, wide(q), wide(kd), wide(vd), drafts.mask_words(wide(seen)))
+    for b, i, h in np.ndindex(few, len(nodes), hkv * 4):
+        at = (slice(b, b + 1), slice(nodes[i], nodes[i] + 1), slice(h, h + 1))
+        if hit[b, nodes[i], h]:
+            assert np.isnan(O[at]).all() and (flags[at] & oracle.FLAG_PRECOND).all(), at
+            assert np.isnan(cert["lse"][at]).all(), at
+        else:
+            assert_nodes([[[ref[b][i][h]]]], O[at], {f: y[at] for f, y in cert.items()}, flags[at], (b, nodes[i], h))
+    if n_tokens == 0:
+        assert (O[:, n // 2] == 0).all() and (cert["lse"][:, n // 2] == -math.inf).all() and (flags[:, n // 2] == 0).all()
