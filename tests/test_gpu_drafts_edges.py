@@ -1,5 +1,6 @@
 """Drafted tokens over the cache where attention and its certificate are most easily wrong: against oracle/drafts.py, with the tolerances of
 test_gpu_drafts.py."""
+import functools
 import math
 
 import numpy as np
@@ -8,15 +9,15 @@ import pytest
 import oracle
 import workloads
 from helpers import GpuLayerCache
-from oracle import drafts
+from oracle import drafts, quantizer
 from test_gpu_drafts import assert_nodes, random_tree, tree_call
 
 pytestmark = pytest.mark.gpu
 
 
 def sequences(x, bt):
-    """Four sequences over and over."""
-    return np.tile(x, ((bt + 3) // 4,) + (1,) * (x.ndim - 1))[:bt]
+    """Up to four sequences over and over."""
+    return np.tile(x, ((bt + len(x) - 1) // len(x),) + (1,) * (x.ndim - 1))[:bt]
 
 
 # 33 .. 64, 65 .. 128 and up to 256 rows; a workgroup has a sequence, more than 64 blocks of it and not a multiple of 32
@@ -133,11 +134,10 @@ def test_queries_that_are_not_finite(bt, hkv, n, n_tokens):
     oc.append(k, v)
     plain = np.where(np.isfinite(q), q, np.float16(0.0))
     ref = drafts.tree_decode(oc, plain[:, nodes], kd, vd, seen[:, nodes], oracle.Tolerances())
-    wide = lambda x: np.tile(x, ((bt + few - 1) // few,) + (1,) * (x.ndim - 1))[:bt]  # noqa: E731
     with GpuLayerCache(bt, hkv * 4, hkv, max(n_tokens, 16), tier2=False) as gc:
         if n_tokens:
-            gc.append(wide(k), wide(v))
-        O, cert, flags = tree_call(gc, wide(q), wide(kd), wide(vd), drafts.mask_words(wide(seen)))
+            gc.append(sequences(k, bt), sequences(v, bt))
+        O, cert, flags = tree_call(gc, sequences(q, bt), sequences(kd, bt), sequences(vd, bt), drafts.mask_words(sequences(seen, bt)))
     for b, i, h in np.ndindex(few, len(nodes), hkv * 4):
         at = (slice(b, b + 1), slice(nodes[i], nodes[i] + 1), slice(h, h + 1))
         if hit[b, nodes[i], h]:
@@ -147,3 +147,75 @@ def test_queries_that_are_not_finite(bt, hkv, n, n_tokens):
             assert_nodes([[[ref[b][i][h]]]], O[at], {f: y[at] for f, y in cert.items()}, flags[at], (b, nodes[i], h))
     if n_tokens == 0:
         assert (O[:, n // 2] == 0).all() and (cert["lse"][:, n // 2] == -math.inf).all() and (flags[:, n // 2] == 0).all()
+
+
+@pytest.mark.parametrize("bt,hkv,n,n_tokens", [(1, 4, 26, 2053), (256, 1, 13, 1157), (96, 1, 27, 1001), (160, 1, 64, 427)])
+def test_outlier_channels_and_peaked_queries(bt, hkv, n, n_tokens):
+    """Keys of 20 to 80 and queries of 3 to 9: one step of FP16 of one key is up to 4 % of its weight."""
+    print("tree outliers", bt, hkv, n, n_tokens, flush=True)
+    rng = np.random.default_rng(90 + n_tokens)
+    few = min(bt, 4)
+    k, kd = (rng.standard_normal((few, hkv, m, 128)) for m in (n_tokens, n))
+    k[..., 11::32] *= 20.0
+    kd[..., 11::32] *= 20.0
+    k, kd = k.astype(np.float16), kd.astype(np.float16)
+    v, vd = (workloads.normal_f16(rng, (few, hkv, m, 128)) for m in (n_tokens, n))
+    q = rng.standard_normal((few, n, hkv * 4, 128))
+    q[:, :, ::2] *= 3.0
+    q = q.astype(np.float16)
+    seen = random_tree(rng, few, n)
+    nodes = np.arange(n) if bt == 1 else np.unique([0, 1, n // 3, n // 2, n - 2, n - 1])
+    oc = oracle.OracleLayerCache(few, hkv)
+    oc.append(k, v)
+    ref = drafts.tree_decode(oc, q[:, nodes], kd, vd, seen[:, nodes], oracle.Tolerances())
+    with GpuLayerCache(bt, hkv * 4, hkv, n_tokens, tier2=False) as gc:
+        gc.append(sequences(k, bt), sequences(v, bt))
+        O, cert, flags = tree_call(gc, sequences(q, bt), sequences(kd, bt), sequences(vd, bt), drafts.mask_words(sequences(seen, bt)))
+    assert_nodes(ref, O[:few, nodes], {f: y[:few, nodes] for f, y in cert.items()}, flags[:few, nodes])
+
+
+@functools.lru_cache
+def columns_at_a_border(count):
+    """[16, count] FP16 keys of one channel and block, one of them, near the largest, reconstructed to another FP16 number where the product
+    code sigma is rounded before z is added: the definition rounds the sum once."""
+    found, rng = [], np.random.default_rng(101)
+    for _ in range(40):
+        k = (rng.standard_normal((100000, 16, 1)) * 20.0).astype(np.float16)
+        codes, sigma, z = quantizer.quantize_key_blocks(k)
+        once = quantizer.dequantize_keys(codes, sigma, z).astype(np.float32)[:, :, 0]
+        twice = (codes.astype(np.float32) * sigma[:, None] + z[:, None])[:, :, 0]
+        told = (once.astype(np.float16) != twice.astype(np.float16)) & (once >= 16.0) & (once >= once.max(1, keepdims=True) - 12.0)
+        found.append(k[told.any(1), :, 0].T)
+    found = np.concatenate(found, 1)
+    assert found.shape[1] >= count, found.shape
+    return found[:, :count]
+
+
+@pytest.mark.parametrize("bt,n_tokens", [(1, 16), (1, 100), (256, 1157)])
+def test_keys_are_rounded_once(bt, n_tokens):
+    """A key at a border of FP16 in each of 32 channels, rows that ask for one channel, and values that show every weight of the first block."""
+    print("tree rounding", bt, n_tokens, flush=True)
+    rng = np.random.default_rng(100)
+    n = 13
+    k, kd = (workloads.normal_f16(rng, (1, 1, m, 128)) for m in (n_tokens, n))
+    k[0, 0, :16, :32] = columns_at_a_border(32)
+    v, vd = np.zeros((1, 1, n_tokens, 128), np.float16), np.zeros((1, 1, n, 128), np.float16)
+    v[0, 0, np.arange(128) // 8, np.arange(128)] = 1.0
+    q = np.zeros((1, n, 4, 128), np.float16)
+    q.reshape(4 * n, 128)[np.arange(4 * n), np.arange(4 * n) % 32] = 3.0
+    seen = np.eye(n, dtype=bool)[None]
+    oc = oracle.OracleLayerCache(1, 1)
+    oc.append(k, v)
+    ref = drafts.tree_decode(oc, q, kd, vd, seen, oracle.Tolerances())
+    # with the other rounding, a step of FP16 from 2^-6 on, every row is further off than it may be
+    with pytest.MonkeyPatch.context() as m:
+        m.setattr(quantizer, "dequantize_keys", lambda codes, sigma, z: codes.astype(np.float32) * sigma[..., None, :] + z[..., None, :])
+        wrong = drafts.tree_decode(oc, q, kd, vd, seen, oracle.Tolerances())
+    for r, w in zip(sum(ref[0], []), sum(wrong[0], [])):
+        assert (np.abs(w["O"] - r["O"]) > 2.0 ** -11 * np.abs(r["O"]) + (2.0 ** -11 + 1e-4) * r["spread"] + 2.0 ** -25 * r["floor"]).any()
+    with GpuLayerCache(bt, 4, 1, n_tokens, tier2=False) as gc:
+        gc.append(sequences(k, bt), sequences(v, bt))
+        O, cert, flags = tree_call(gc, sequences(q, bt), sequences(kd, bt), sequences(vd, bt), drafts.mask_words(sequences(seen, bt)))
+    assert_nodes(ref, O[:1], {f: y[:1] for f, y in cert.items()}, flags[:1])
+    for y in (O, flags, *cert.values()):
+        assert all(np.array_equal(z, y[0]) for z in y)
