@@ -531,7 +531,8 @@ typedef struct cqa_node_cert {
  * the softmax's weights, times 2^14, enter the value product in FP16 (down to 2^-28 of the largest with 11 bits).  The
  * certificate is that of cqa_certified_decode with what the rounding to FP16 adds: sigma_c becomes the next FP16 number from
  *   sigma_c + 2 min(sigma_c / 2, 2^-11 max(|z_c - 128 sigma_c|, |z_c + 127 sigma_c|) + 2^-25)
- * upwards, eta_b becomes eta_b + min(eta_b, 2^-11 (nu_b + eta_b) + 2^-21); v_max ranges over the tokens the node attends.
+ * upwards, eta_b becomes eta_b + min(eta_b, 2^-11 (nu_b + eta_b) + 2^-21); v_max ranges over the tokens the node attends; and
+ * a sealed mass below 2^-110, which FP32 sums of weights may have lost, enters E_key as 2^-110 (alpha_tail_hat is what there is).
  * flags: KEY, VAL, TOTAL, PRECOND by tol's thresholds, force_flags; they only REQUEST precision, there is no ladder for
  * nodes: a program accepts a path up to its first flagged node and has the token from there on served by a step of the
  * single-token calls.  A node that attends nothing (an empty cache and mask) returns O = 0, lse = -inf, zeros, and no

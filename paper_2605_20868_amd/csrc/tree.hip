@@ -494,8 +494,9 @@ __device__ __forceinline__ Certificate certificate(const TreeArgs& a, float M, f
   ct.max_block_contrib = EM * inv;
   ct.reserved = 0.0f;
   float tail = 0.0f;
-  if (ct.alpha_tail_hat > 0.0f && DM != 0.0f)
-    tail = fminf(1.0f, expf((float)a.tol.mass_exp * DM) * ct.alpha_tail_hat) * expm1f(2.0f * DM);
+  // (Sealed weights below 2^-126 are lost, 2^30 of them at most beside a sum of 2^14: a mass of 2^-110, which e^(4 Delta) can make a certain one.)
+  if (a.nb > 0 && DM != 0.0f)
+    tail = fminf(1.0f, expf((float)a.tol.mass_exp * DM) * (ct.alpha_tail_hat < 0x1p-110f ? 0x1p-110f : ct.alpha_tail_hat)) * expm1f(2.0f * DM);
   const float full = tanhf(DM);
   ct.E_key = 2.0f * VM * (a.tol.key_bound_mode == 0 ? fminf(full, tail) : (a.tol.key_bound_mode == 1 ? tail : full));
   uint32_t fl = a.tol.force_flags;

@@ -219,3 +219,29 @@ def test_keys_are_rounded_once(bt, n_tokens):
     assert_nodes(ref, O[:1], {f: y[:1] for f, y in cert.items()}, flags[:1])
     for y in (O, flags, *cert.values()):
         assert all(np.array_equal(z, y[0]) for z in y)
+
+
+@pytest.mark.parametrize("n_tokens", [48, 704, 5008])
+def test_sealed_tokens_too_light_for_fp32_still_have_a_key_error(n_tokens):
+    """Each node's draft is 150 above all sealed scores, which are themselves off by up to Delta = 50 and more: their mass, e^-150, is nothing in
+    FP32, but e^(4 Delta) times that is not."""
+    print("tree light sealed tokens", n_tokens, flush=True)
+    rng = np.random.default_rng(110 + n_tokens)
+    n = 5
+    k, v = ((rng.standard_normal((1, 1, n_tokens, 128)) * s).astype(np.float16) for s in (32.0, 1.0))
+    q = (rng.standard_normal((1, n, 1, 128)) * 32.0).astype(np.float16)
+    oc = oracle.OracleLayerCache(1, 1)
+    oc.append(k, v)
+    sealed = drafts.read_back(oc, 0, n_tokens)[0][0, 0].astype(np.float64)
+    x = q[0, :, 0].astype(np.float64)
+    top = (x @ sealed.T).max(1) * SCORE
+    kd = (x * ((top + 150.0) / SCORE / (x * x).sum(1))[:, None]).astype(np.float16)[None, None]
+    vd = workloads.normal_f16(rng, (1, 1, n, 128))
+    seen = np.eye(n, dtype=bool)[None]
+    tol = oracle.Tolerances(eps_key=0.01)
+    ref = drafts.tree_decode(oc, q, kd, vd, seen, tol)
+    for r in ref[0]:
+        assert r[0]["delta_h"] > 45.0 and 1e-80 < r[0]["alpha_tail_hat"] < 1e-45 and r[0]["E_key"] == 2 * r[0]["v_max"] and r[0]["flags"] & oracle.FLAG_KEY
+    with GpuLayerCache(1, 1, 1, n_tokens, tier2=False) as gc:
+        gc.append(k, v)
+        assert_nodes(ref, *tree_call(gc, q, kd, vd, drafts.mask_words(seen), gc.cqa.Tolerances(eps_key=0.01)))
