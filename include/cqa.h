@@ -479,9 +479,10 @@ typedef struct cqa_rotary_rows {
 /* Turns the rows of n_rows (1 or 2) tensors, the queries and the keys of a projection, in one launch:
  * a pair (a, b) of the row of token t of sequence s becomes
  *   magnitude (a cos w - b sin w),  magnitude (a sin w + b cos w),  w = p f_i,
- * p = positions_dev[s * position_stride + t] (device int64, any value; position_stride 0: the sequences
- * share their positions), computed in FP32 (the angle exactly modulo a turn, however far the position)
- * and rounded once.  Negative positions turn back: with -p the call is the gradient of the call with p, and
+ * p = positions_dev[s * position_stride + t] (device int64; position_stride 0: the sequences share their
+ * positions), computed in FP32 and rounded once.  The angle is kept modulo a turn in 64 bits behind the
+ * point, off by |p| 2^-64 turns at most, 2^-24 turns at |p| = 2^40; positions further out than that are
+ * turned by an angle that grows as inexact.  Negative positions turn back: with -p the call is the gradient of the call with p, and
  * with -d it moves rows d positions towards the front.
  * in_type, out_type: CQA_TYPE_*; pointers aligned to their type.  A tensor may be turned in place (same address,
  * same strides, types of the same size); no other overlap is allowed.
@@ -529,7 +530,9 @@ typedef struct cqa_node_cert {
  *   workspace_dev            cqa_tree_workspace_bytes(c, n_draft) bytes; calls that share one must be ordered
  * Sealed tokens are attended as cqa_cache_read gives them in FP16, trailing and drafted ones exactly; FP32 accumulation;
  * the softmax's weights, times 2^14, enter the value product in FP16 (down to 2^-28 of the largest with 11 bits).  The
- * certificate is that of cqa_certified_decode with what the rounding to FP16 adds: sigma_c becomes the next FP16 number from
+ * certificate bounds how far attention over the numbers attended is from attention over the originals; the arithmetic's own
+ * roundings are not in it: O's to FP16 (2^-11 |O|) and the weights' (2^-11 of the mean of |v| under the weights, per channel).
+ * It is that of cqa_certified_decode with what the rounding to FP16 adds: sigma_c becomes the next FP16 number from
  *   sigma_c + 2 min(sigma_c / 2, 2^-11 max(|z_c - 128 sigma_c|, |z_c + 127 sigma_c|) + 2^-25)
  * upwards, eta_b becomes eta_b + min(eta_b, 2^-11 (nu_b + eta_b) + 2^-21); v_max ranges over the tokens the node attends; and
  * a sealed mass below 2^-110, which FP32 sums of weights may have lost, enters E_key as 2^-110 (alpha_tail_hat is what there is).

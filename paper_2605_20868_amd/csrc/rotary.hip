@@ -3,8 +3,9 @@
 // A pair of channels (a, b) of a row at position p turns by the angle p f_i:
 //   a' = m (a cos - b sin),   b' = m (a sin + b cos).
 // The angle is kept in turns as a 64-bit binary fraction: the host rounds f_i / 2 pi to 64 bits behind the point, p times that
-// modulo 2^64 is the fraction of a turn exactly (for negative p as well), so that no position is too far: what is left of an
-// angle has an error of |p| 2^-65 turns, and the sine and cosine of its upper 32 bits are within 2^-24 of a turn's.
+// modulo 2^64 is the fraction of a turn exactly (for negative p as well).  What is left of an angle has an error of
+// |p| 2^-64 turns (f_i's own rounding on the host and this one), below that of FP32 up to |p| = 2^40, and the sine and cosine of
+// its upper 32 bits are within 2^-24 of a turn's.
 //
 // What bounds it: bytes, each row is read and written once.  A thread owns 8 pairs (16 channels) of one token and walks over the
 // token's heads, so that the 8 sines and cosines are computed once for all of them.  Rows are written past the caches: a prompt of 8192

@@ -17,7 +17,8 @@
 //   S^T [32 tokens][32 rows] = K^ Q^T.  The tile's 32 token rows are dealt to two blocks so that a lane's 16 results are the 16 tokens of
 //     one block for one row: the block's sum S_b is an in-lane sum, and what the lane holds is, packed, the B operand of
 //   O^T [128 channels][32 rows] += V^T P^T, whose 8 consecutive tokens per lane are what one dword of value codes holds.
-// Softmax in FP32 (running maximum per row, FP32 sums); the weights enter the second product as FP16, off by 2^-12 of a weight at most.
+// Softmax in FP32 (running maximum per row, FP32 sums); the weights enter the second product as FP16, off by 2^-11 of a weight at most: two terms
+// of each would double the products with the values, and O is rounded to FP16 itself.
 //
 // Trailing FP16 tokens and drafted ones, which are exact, are attended behind the sealed ones, under the mask, by the workgroups that have
 // the fewest of those.
@@ -233,14 +234,13 @@ __device__ __forceinline__ void softmax32(TreeRows& w, f32x16 (&s)[MT], uint32_t
     w.evmax = fmaxf(w.evmax, e);
   }
 }
-// All of it; between(): what is to be done once the keys are.
-template <typename Key, typename Between, typename Value>
-__device__ __forceinline__ void attend32(TreeRows& w, bool masked, uint32_t bits, float eta, Key key, Between between, Value value) {
+// All of it, of exact tokens.
+template <typename Key, typename Value>
+__device__ __forceinline__ void attend32(TreeRows& w, uint32_t bits, Key key, Value value) {
   f32x16 s[1];
   uint32_t p[1][8];
   scores32(w, s[0], key);
-  between();
-  softmax32<1>(w, s, p, masked, [&](int) { return bits; }, [&](int) { return eta; });
+  softmax32<1>(w, s, p, true, [&](int) { return bits; }, [&](int) { return 0.0f; });
   values32(w, p[0], value);
 }
 
@@ -761,7 +761,7 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
       open |= bits;
       open_exact(rows, bits, s_norm + blk * BLK, s_bad + blk * BLK);
       attend32(
-          rows, true, bits, 0.0f, [&](int ks) { return __builtin_bit_cast(f16x8, s_k[(half * 8 + ks) * EXACT + w * 32 + n32]); }, [] {},
+          rows, bits, [&](int ks) { return __builtin_bit_cast(f16x8, s_k[(half * 8 + ks) * EXACT + w * 32 + n32]); },
           [&](int oct, int ct) { return __builtin_bit_cast(f16x8, s_v[(blk * 2 + oct) * D + ct * 32 + n32]); });
     }
     __syncthreads();   // (the next ones, or the waves' sets, come where these are)
@@ -1076,7 +1076,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
       open |= bits[mt];
       open_exact(rows, bits[mt], s_norm + blk * BLK, s_bad + blk * BLK);
       attend32(
-          rows, true, bits[mt], 0.0f, [&](int ks) { return key_of(s_k, unit, ks); }, [] {}, [&](int oct, int ct) { return value_of(s_v, blk, oct, ct); });
+          rows, bits[mt], [&](int ks) { return key_of(s_k, unit, ks); }, [&](int oct, int ct) { return value_of(s_v, blk, oct, ct); });
     }
   }
   __syncthreads();
