@@ -1057,7 +1057,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
     add_values(buf ^ 1);
   }
   rows.sealed = rows.sum;
-  uint32_t open = from < units && (int64_t)from * BLKS + wt * MT * 2 < a.nb;
+  uint32_t open = fresh != 0 && (S::WT == 1 || (int64_t)from * BLKS + wt * MT * 2 < a.nb);   // it has had tiles, and the wave a block of the first
   // the other tokens' tiles: dealt to the workgroups from the last one down
   for (int t0 = (a.nsplit - 1 - split) * TOK; t0 < a.trail + a.n; t0 += a.nsplit * TOK, buf ^= 1) {
     uint4* const s_k = reinterpret_cast<uint4*>(s_main + buf * S::TILE);
