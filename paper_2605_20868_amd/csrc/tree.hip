@@ -606,8 +606,8 @@ __device__ __forceinline__ float* set_of(const TreeArgs& a, int64_t head, int ti
 // channels of a token) is two operands' part of its lane, a dword of value codes (8 tokens of a channel) one.  Only the metadata, which 16
 // lanes share, goes through LDS, the wave's own part of it, so that no wave waits for another until the waves' sets are joined.
 // Two waves a SIMD: what one is to read from LDS is requested a product ahead, and a pair's metadata and codes as soon as those of the pair before
-// are used.  4 x 8 KV heads of 32768 tokens, 5 nodes of 4 query heads: 60 us for 303 MB, 5.05 TB/s, what a large copy reaches (each read where it is
-// used 66, the widths' products for each pair by itself among it); vector ALU 70 % busy, matrix cores 15 %.
+// are used.  4 x 8 KV heads of 32768 tokens, 5 nodes of 4 query heads: 60 - 64 us for 303 MB, 4.7 - 5.0 TB/s, about what a large copy reaches (each read
+// where it is used took a tenth more, the widths' products for each pair by itself among it); vector ALU 65 - 70 % busy, matrix cores 15 %.
 constexpr int FEW_WAVES = 8;
 constexpr int FEW_KM_HALF = 64 + 4, FEW_KM_KIND = 2 * FEW_KM_HALF, FEW_KM_BLK = 2 * FEW_KM_KIND + 8;   // floats; padded: the four
 constexpr int FEW_VM_BLK = VM_BYTES + 32, FEW_W_RUN = 32 * 16 + 16;                                   // addresses of a read in four sets of banks
@@ -617,7 +617,8 @@ static_assert(FEW_META_END <= T_FLOATS * 4 && 2 * FEW_EXACT * D * 2 <= FEW_WAVES
               "a wave's part of LDS");
 
 // EXACT: tokens of a turn of the trailing and drafted ones.  64 where they are no more, for each thread fetches its share of EXACT (1 KV head, 1029 tokens, 8 nodes
-// 12.0 us a call, with 96 12.5; 8 heads, 60 tokens, 12 nodes 10.2, 10.8), else 96 (64 nodes 11.0, by two turns of 64 12.3; 256 nodes, 500 tokens 22.4, 26.0).
+// of 4 query heads 10.7 us a call in a graph, with 96 11.3; 8 heads, 60 tokens, 12 nodes 9.9, 10.4), else 96 (64 nodes 10.6, by turns of 64 12.8; 256 nodes, 500
+// tokens 22.6, 26.1).
 template <int EXACT>
 __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
   static_assert(EXACT <= FEW_EXACT, "LDS");
@@ -787,8 +788,8 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(TreeArgs a) {
 // Keys of t are read in 2 t and 2 t + 1 and replaced (t + 2) in 2 t + 2; values of t are read in 2 t + 2 and 2 t + 3 and replaced
 // in 2 t + 5: two tiles in LDS.  eta of t comes with the keys in 2 t - 2 and is read until 2 t + 2: four of them.  Codes are requested a tile
 // ahead.  (Reconstruction in the weights' phase: products 1310 cycles, weights and reconstruction 2600, of which the products' wave waited half.)
-// 8 KV heads of 131072 tokens, 64 nodes of 4 query heads: 167 - 183 us for 142 GFLOP, 780 - 850 TFLOP/s; vector ALU 67 % and matrix cores 47 % busy, at a clock
-// that falls from 2.4 to 1.6 - 1.8 GHz meanwhile.
+// 8 KV heads of 131072 tokens, 64 nodes of 4 query heads: 173 - 208 us in a trace (178 of a call of 187) for 142 GFLOP, 680 - 820 TFLOP/s; vector ALU 71 % and matrix
+// cores 46 % busy, at a clock that falls from 2.4 to 1.6 - 1.8 GHz meanwhile.
 template <int WR>
 struct ManyShape {
   static constexpr int WT = 8 / WR;
@@ -1108,8 +1109,8 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(TreeArgs a) {
 // ---- joining the partial sets ---------------------------------------------------------------------------------------------------------
 
 // Up to N sets: eight rows a workgroup, four channels of one a thread, and a wave for the certificates.  Every thread requests N sets, so there
-// are two of these and the one for any number (8 heads, 500 tokens, 256 nodes of 4 query heads, 8 sets: 22.5 us with N = 8, 24.8 with 16; 2000
-// tokens, of 2 heads, 16 sets: 23.5 with 16, 27.0 by the one below; 8000 tokens, 4 nodes, 31 sets: 16.5 with 32, 16.0 below).
+// are two of these and the one for any number (us a call in a graph: 8 heads, 8229 tokens, 26 nodes of 4 query heads, 8 sets: 24.1 with N = 8, 25.0 with 16; 2000
+// tokens, 256 nodes of 2, 16 sets: 23.7 with 16, 27.7 by the one below; 8000 tokens, 4 nodes of 4, 31 sets: 16.7 with 32, 16.1 below).
 constexpr int JOIN_ROWS = 8, JOIN_FEW_THREADS = JOIN_ROWS * 32 + 64;
 template <int N>
 __global__ __launch_bounds__(JOIN_FEW_THREADS) void tree_join_few_kernel(TreeArgs a) {
@@ -1119,8 +1120,9 @@ __global__ __launch_bounds__(JOIN_FEW_THREADS) void tree_join_few_kernel(TreeArg
 
 // Many sets: eight rows a workgroup, and a PARTS-th of their channels.  First every set's quantities of the rows, a set a thread, which gives the sets'
 // weights; then the accumulators, four channels of a row and every G-th set a thread, JOIN_AHEAD sets at a time, the first ones requested
-// ahead of the weights.  Four parts where more sets than one has requests for at a time meet few workgroups (1 head, 131000 tokens, 8 nodes of 4 query heads, 256
-// sets: 26.1 us a call, undivided 36.2; 2 heads, 16000 tokens, 64 nodes 28.5, 32.4; 128 workgroups undivided, 4 heads, 8000 tokens, 64 nodes: 28.1, 26.2).
+// ahead of the weights.  Four parts where more sets than one has requests for at a time meet few workgroups (us a call in a graph, 4 query heads: 1 head, 131000
+// tokens, 8 nodes, 256 sets 25.6, undivided 35.1; 2 heads, 64000 tokens, 32 nodes, 128 sets 30.3, 35.3; 4 heads, 64 sets 41.1, 42.7; 64 nodes, 128 workgroups
+// undivided, 59.5, 58.0).
 constexpr int JOIN_AHEAD = 8;
 template <int PARTS>
 __global__ __launch_bounds__(1024) void tree_join_kernel(TreeArgs a) {
@@ -1215,11 +1217,11 @@ __global__ __launch_bounds__(1024) void tree_join_kernel(TreeArgs a) {
 
 // Rows of a KV group a workgroup takes: 32, by the first kernel, where its waves have few turns each (it has them over sooner, and fewer sets to join),
 // else up to 256 by the second, which reconstructs a tile once for all of them.  One of the trailing and drafted tokens takes as long as two sealed
-// ones.  us by the first and the second kernel, turns a wave:
-//   64 rows   8 heads, 2000 tokens 13.1, 16.3 (0.5)   8 heads, 32000 33.3, 33.8 (8)   8 heads, 64000 54.0, 50.5 (16)
-//   128 rows  8 heads, 2000 15.5, 18.1 (1)   2 heads, 32000 23.2, 25.4 (4)   8 heads, 8000 23.0, 22.5 (4)   4 heads, 32000 31.5, 28.6 (8)
-//   256 rows  8 heads, 4000 23.2, 24.9 (4)   1 head, 32000 24.3, 31.9 (4)   8 heads, 8000 32.6, 29.2 (8)
-//   512 rows  4 heads, 4000 24.0, 26.9 (4.4)   8 heads, 2000 27.0, 23.7 (5)
+// ones.  us a call in a graph by the first and the second kernel, turns a wave:
+//   64 rows   8 heads, 2000 tokens 12.2, 15.8 (0.5)   8 heads, 32000 35.8, 36.6 (8)   8 heads, 64000 54.6, 51.4 (16)
+//   128 rows  8 heads, 2000 14.1, 17.0 (1)   2 heads, 32000 22.8, 25.6 (4)   8 heads, 8000 22.1, 22.2 (4)   4 heads, 32000 31.8, 28.7 (8)
+//   256 rows  8 heads, 4000 22.2, 24.7 (4)   1 head, 32000 23.0, 31.7 (4)   8 heads, 8000 32.6, 29.6 (8)
+//   512 rows  4 heads, 4000 23.3, 27.0 (4.2)   8 heads, 2000 23.3, 22.9 (4.4)
 static int tree_rows(int n_cu, int64_t heads, int n_rows, int64_t sealed, int64_t others) {
   const int64_t work = (sealed + 2 * others) * heads * ((n_rows + 31) / 32), turn = (int64_t)32 * FEW_WAVES * n_cu;
   if (n_rows <= 32 || 2 * work <= (n_rows <= 64 ? 16 : 9) * turn) return 32;
@@ -1230,8 +1232,8 @@ static int tree_rows(int n_cu, int64_t heads, int n_rows, int64_t sealed, int64_
 static int tile_tokens(int rows) { return rows == 32 ? 32 * FEW_WAVES : (rows == 64 ? 128 : 64); }
 
 // Partial sets: as many workgroups as the device holds at a time, each with a tile of sealed blocks or of the other tokens.  Of 32 rows a workgroup
-// the first tile and the other tokens are one workgroup's, which needs no second launch (8 heads, 4 nodes of 4 query heads, 200 tokens
-// 11.4 us, by two workgroups 12.6; two tiles, 400 tokens, by one 13.8, by three 12.2).
+// the first tile and the other tokens are one workgroup's, which needs no second launch (us a call in a graph, 8 heads of 4 query heads: 12 nodes, 60 tokens 9.9, by
+// two workgroups 10.9; 4 nodes, 200 tokens 10.7, 10.6; two tiles, 4 nodes, 400 tokens, by one 13.4, by three 10.8).
 static int tree_splits(int n_cu, int64_t heads, int n_rows, int rows, int64_t sealed, int64_t others) {
   const int tok = tile_tokens(rows), exact = rows == 32 ? FEW_EXACT : tok;   // (64 others at most are a turn as well)
   const int64_t z = (n_rows + rows - 1) / rows, most = std::max<int64_t>(1, (int64_t)n_cu / (heads * z));
