@@ -121,7 +121,9 @@ class RotaryRows(C.Structure):
 
     # (made from packed bytes: setting ten fields one by one costs more than the call)
     def __new__(cls, in_dev, out_dev, n_heads, in_strides, out_strides):
-        return cls.from_buffer_copy(_pack_rows(_ptr(in_dev) or 0, _ptr(out_dev) or 0, n_heads, 0, *in_strides, *out_strides))
+        rows = cls.from_buffer_copy(_pack_rows(_ptr(in_dev) or 0, _ptr(out_dev) or 0, n_heads, 0, *in_strides, *out_strides))
+        rows.tensors = in_dev, out_dev   # (they live as long as their addresses here, also where the caller has no other name for them)
+        return rows
 
     def __init__(self, *_):
         pass
