@@ -554,6 +554,72 @@ int32_t cqa_tree_decode(const cqa_cache* c, int32_t layer, const void* q_fp16_de
 /* Holds for every length the cache can have.  Errors: INVALID_ARG, UNSUPPORTED (n_draft). */
 int32_t cqa_tree_workspace_bytes(const cqa_cache* c, int32_t n_draft, int64_t* bytes);
 
+/* ---- other scores, shared beginnings ----------------------------------------------------------------- */
+
+/* How tokens are scored, for models that do not score them by q . k / sqrt(128).  For node i at place p_i and token j at
+ * place p_j:
+ *   x = scale q . k,   y = cap tanh(x / cap)   (cap 0: y = x),   score = y - slope[query head] |p_i - p_j|
+ * over the tokens that the node attends: cached ones of its two spans, drafted ones of its mask.  The place of a cached token is
+ * its index (of a shared beginning's: from its first; the sequence's own: behind the beginning's last); a drafted token's is that of its
+ * node.
+ *   scale       0: 1 / sqrt(128); otherwise 2^-40 .. 2^40
+ *   cap         0: none; otherwise 2^-20 .. 2^60
+ *   slopes_dev  float [n_q_heads], or NULL: no bias.  Negative slopes are allowed; one that is no finite number makes its head's rows NaN
+ *               with PRECOND, as such queries do
+ *   places_dev  int64 [batch][n_nodes], or NULL: node i of drafted ones is at the number of cached tokens + i; without drafted tokens
+ *               the nodes are the last n_nodes cached tokens.  Used by the bias only.  Places count up to 2^30 tokens ahead of the first and behind
+ *               the last cached token: one beyond is taken for that
+ *   spans_dev   int64 [batch][n_nodes][4], or NULL: every cached token.  Node i attends the cached tokens j with s[0] <= j < s[1] or
+ *               s[2] <= j < s[3], each once where the spans overlap; a span may be empty (to <= from) or reach beyond the cached tokens.  Sliding
+ *               windows with the first tokens kept, left-padded batches and packed documents are such spans; what no node of a
+ *               sequence attends between its two spans, or around them, is not read.
+ * Slopes, places and spans are read on the device. */
+typedef struct cqa_scoring {
+  float scale;
+  float cap;
+  const float* slopes_dev;
+  const int64_t* places_dev;
+  const int64_t* spans_dev;
+} cqa_scoring;
+
+/* cqa_tree_decode with scores of the caller's, and without drafted tokens where there are none: n_nodes nodes per sequence (1 ..
+ * CQA_MAX_DRAFT) attend the cached tokens of their spans and, if k_draft_dev and v_draft_dev are given, the drafted tokens of their mask (NULL:
+ * j <= i).  Without drafted tokens (both NULL, and mask_dev) the nodes attend cached tokens only: a single token that has been
+ * appended already is n_nodes = 1.  Arguments, layouts, results and errors otherwise as cqa_tree_decode's; scoring: host pointer, copied, NULL: the
+ * plain scores of every cached token.
+ * The certificate is that of cqa_tree_decode for these scores: Delta_b = (scale / 2) sum_c |q_c| w_c over the blocks of which the node
+ * attends a token; with a cap, scores of keys that differ by up to Delta before it differ by up to 2 cap tanh(Delta / (2 cap)) behind it, which is
+ * the delta_h that is returned and used; the bias is the same for both.  v_max ranges over the tokens attended, by blocks where they are sealed.
+ * Errors besides: INVALID_ARG (scoring out of range; one of k_draft_dev and v_draft_dev; a mask without them), UNSUPPORTED (2^30 cached
+ * tokens or more). */
+int32_t cqa_scored_decode(const cqa_cache* c, int32_t layer, const void* q_fp16_dev, const void* k_draft_dev,
+                          const void* v_draft_dev, int32_t n_nodes, const uint64_t* mask_dev,
+                          const cqa_scoring* scoring, const cqa_tolerances* tol, void* O_dev,
+                          cqa_node_cert* cert_dev, uint32_t* flags_dev, void* workspace_dev, void* stream);
+/* Holds for every length the cache can have.  Errors: INVALID_ARG, UNSUPPORTED (n_nodes). */
+int32_t cqa_scored_workspace_bytes(const cqa_cache* c, int32_t n_nodes, int64_t* bytes);
+
+/* Nodes times query heads per KV head, over the sequences of one beginning. */
+#define CQA_MAX_SHARED_ROWS (1 << 18)
+
+/* cqa_scored_decode for sequences behind a beginning that is cached once: sequence s of c attends the cached tokens of
+ * sequence s / (batch of c / batch of shared) of `shared`, then its own in c, then drafted ones.  The beginning is read and reconstructed
+ * once for its sequences, up to 256 of their rows (nodes x query heads of a KV group) at a time.  The caches are two handles with the same query and
+ * KV heads, on the same device, the batch of c a multiple of shared's; either may be empty, and their lengths are their own.  Both are used at the
+ * same `layer`.
+ * Spans and places count through the beginning's tokens and the sequence's own.  A sequence that is idle attends nothing: empty
+ * spans and an empty mask.  The certificate is over the tokens of both, each with its own block's.
+ * Calls that append to either cache must be ordered with this one.
+ * Errors besides: INVALID_ARG (caches that do not fit), UNSUPPORTED (more than CQA_MAX_SHARED_ROWS rows behind a beginning; 2^30 cached tokens
+ * or more in both). */
+int32_t cqa_prefix_decode(const cqa_cache* shared, const cqa_cache* c, int32_t layer, const void* q_fp16_dev,
+                          const void* k_draft_dev, const void* v_draft_dev, int32_t n_nodes,
+                          const uint64_t* mask_dev, const cqa_scoring* scoring, const cqa_tolerances* tol,
+                          void* O_dev, cqa_node_cert* cert_dev, uint32_t* flags_dev, void* workspace_dev,
+                          void* stream);
+/* Holds for every length the caches can have. */
+int32_t cqa_prefix_workspace_bytes(const cqa_cache* shared, const cqa_cache* c, int32_t n_nodes, int64_t* bytes);
+
 /* ---- misc ------------------------------------------------------------------ */
 
 /* Split count the decode pass uses for the current length of `layer`

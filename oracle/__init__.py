@@ -10,8 +10,9 @@ from .cache import OracleLayerCache, ladder_decision
 from . import quantizer
 from . import adaptive
 from . import drafts
+from . import scored
 from .adaptive import SelectorParams
 
 __all__ = ["FLAG_ANY", "FLAG_KEY", "FLAG_PRECOND", "FLAG_RANK", "FLAG_TOTAL", "FLAG_VAL",
            "RUNG_SHIFT", "Tolerances", "certified_head", "key_term", "softmax_attention",
-           "OracleLayerCache", "ladder_decision", "quantizer", "adaptive", "drafts", "SelectorParams"]
+           "OracleLayerCache", "ladder_decision", "quantizer", "adaptive", "drafts", "scored", "SelectorParams"]

@@ -139,6 +139,15 @@ class NodeCert(C.Structure):
                 ("reserved", C.c_float)]
 
 
+class Scoring(C.Structure):
+    """How tokens are scored (cqa_scoring); scale 0: 1 / sqrt(128), cap 0: none, the pointers None: no bias, places by order, every token."""
+    _fields_ = [("scale", C.c_float), ("cap", C.c_float), ("slopes_dev", C.c_void_p), ("places_dev", C.c_void_p), ("spans_dev", C.c_void_p)]
+
+    def __init__(self, scale=0.0, cap=0.0, slopes_dev=None, places_dev=None, spans_dev=None):
+        super().__init__(scale, cap, _ptr(slopes_dev), _ptr(places_dev), _ptr(spans_dev))
+        self.tensors = slopes_dev, places_dev, spans_dev   # (they live as long as their addresses here)
+
+
 class CqaError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -194,6 +203,10 @@ def _load():
         "cqa_cache_read": (i32, [vp, i32, i64, i64, i32, vp, vp, C.POINTER(Strides), vp]),
         "cqa_tree_decode": (i32, [vp, i32, vp, vp, vp, i32, vp, C.POINTER(Tolerances), vp, vp, vp, vp, vp]),
         "cqa_tree_workspace_bytes": (i32, [vp, i32, C.POINTER(i64)]),
+        "cqa_scored_decode": (i32, [vp, i32, vp, vp, vp, i32, vp, C.POINTER(Scoring), C.POINTER(Tolerances), vp, vp, vp, vp, vp]),
+        "cqa_scored_workspace_bytes": (i32, [vp, i32, C.POINTER(i64)]),
+        "cqa_prefix_decode": (i32, [vp, vp, i32, vp, vp, vp, i32, vp, C.POINTER(Scoring), C.POINTER(Tolerances), vp, vp, vp, vp, vp]),
+        "cqa_prefix_workspace_bytes": (i32, [vp, vp, i32, C.POINTER(i64)]),
         "cqa_time_certified_decode": (i32, [vp, i32, vp, C.POINTER(Tolerances), vp, vp, vp, vp,
                                             i32, C.POINTER(C.c_float), vp]),
         "cqa_time_stream_read": (i32, [vp, i32, i32, C.POINTER(C.c_float), C.POINTER(i64), vp]),
@@ -475,6 +488,34 @@ def cqa_tree_decode(h, layer, q_dev, k_draft_dev, v_draft_dev, n_draft, mask_dev
     _check(_lib.cqa_tree_decode(h, layer, _ptr(q_dev), _ptr(k_draft_dev), _ptr(v_draft_dev), n_draft, _ptr(mask_dev),
                                 C.byref(tol), _ptr(O_dev), _ptr(cert_dev), _ptr(flags_dev), _ptr(workspace_dev),
                                 _ptr(stream)), "cqa_tree_decode")
+
+
+def cqa_scored_workspace_bytes(h, n_nodes) -> int:
+    n = C.c_int64(0)
+    _check(_lib.cqa_scored_workspace_bytes(h, n_nodes, C.byref(n)), "cqa_scored_workspace_bytes")
+    return n.value
+
+
+def cqa_scored_decode(h, layer, q_dev, k_draft_dev, v_draft_dev, n_nodes, mask_dev, scoring, tol: Tolerances, O_dev, cert_dev,
+                      flags_dev, workspace_dev, stream=None) -> None:
+    """scoring: a Scoring, or None for the plain scores; k_draft_dev, v_draft_dev None: no drafted tokens."""
+    _check(_lib.cqa_scored_decode(h, layer, _ptr(q_dev), _ptr(k_draft_dev), _ptr(v_draft_dev), n_nodes, _ptr(mask_dev),
+                                  None if scoring is None else C.byref(scoring), C.byref(tol), _ptr(O_dev), _ptr(cert_dev),
+                                  _ptr(flags_dev), _ptr(workspace_dev), _ptr(stream)), "cqa_scored_decode")
+
+
+def cqa_prefix_workspace_bytes(shared, h, n_nodes) -> int:
+    n = C.c_int64(0)
+    _check(_lib.cqa_prefix_workspace_bytes(shared, h, n_nodes, C.byref(n)), "cqa_prefix_workspace_bytes")
+    return n.value
+
+
+def cqa_prefix_decode(shared, h, layer, q_dev, k_draft_dev, v_draft_dev, n_nodes, mask_dev, scoring, tol: Tolerances, O_dev, cert_dev,
+                      flags_dev, workspace_dev, stream=None) -> None:
+    """cqa_scored_decode of sequences behind the cached tokens of `shared`."""
+    _check(_lib.cqa_prefix_decode(shared, h, layer, _ptr(q_dev), _ptr(k_draft_dev), _ptr(v_draft_dev), n_nodes, _ptr(mask_dev),
+                                  None if scoring is None else C.byref(scoring), C.byref(tol), _ptr(O_dev), _ptr(cert_dev),
+                                  _ptr(flags_dev), _ptr(workspace_dev), _ptr(stream)), "cqa_prefix_decode")
 
 
 def cqa_time_certified_decode(h, layer, q_dev, tol: Tolerances, O_dev, cert_dev, flags_dev,

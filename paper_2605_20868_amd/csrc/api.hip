@@ -1254,4 +1254,74 @@ int32_t cqa_tree_decode(const cqa_cache* h, int32_t layer, const void* q_fp16_de
                      (__half*)O_dev, cert_dev, flags_dev, (float*)workspace_dev, (hipStream_t)stream);
 }
 
+// shared: null = none
+static int32_t check_nodes(const cqa_cache* shared, const cqa_cache* h, int32_t n_nodes) {
+  if (h == nullptr || n_nodes < 1) return CQA_ERR_INVALID_ARG;
+  if (const int32_t rc = check_draft(h, n_nodes)) return rc;
+  if (shared == nullptr) return CQA_OK;
+  const cqa_cache_desc &s = shared->impl.desc, &d = h->impl.desc;
+  if (s.n_q_heads != d.n_q_heads || s.n_kv_heads != d.n_kv_heads || s.batch > d.batch || d.batch % s.batch != 0 ||
+      shared->impl.device != h->impl.device)
+    return CQA_ERR_INVALID_ARG;
+  // the rows of a beginning lie along one dimension of a launch, eight to a workgroup
+  if ((int64_t)(d.batch / s.batch) * n_nodes * (d.n_q_heads / d.n_kv_heads) > CQA_MAX_SHARED_ROWS) return CQA_ERR_UNSUPPORTED;
+  return CQA_OK;
+}
+
+static int32_t nodes_workspace(const cqa_cache* shared, const cqa_cache* h, int32_t n_nodes, int64_t* bytes) {
+  if (bytes == nullptr) return CQA_ERR_INVALID_ARG;
+  if (const int32_t rc = check_nodes(shared, h, n_nodes)) return rc;
+  *bytes = scored_ws_bytes(shared != nullptr ? &shared->impl : nullptr, &h->impl, n_nodes);
+  return CQA_OK;
+}
+
+static int32_t check_scoring(const cqa_scoring* s) {
+  if (s == nullptr) return CQA_OK;
+  const auto within = [](float x, float lo, float hi) { return x >= lo && x <= hi; };   // (false for a NaN)
+  if (!(s->scale == 0.0f || within(s->scale, 0x1p-40f, 0x1p40f)) || !(s->cap == 0.0f || within(s->cap, 0x1p-20f, 0x1p60f)) ||
+      !aligned(s->slopes_dev, 4) || !aligned(s->places_dev, 8) || !aligned(s->spans_dev, 8))
+    return CQA_ERR_INVALID_ARG;
+  return CQA_OK;
+}
+
+static int32_t nodes_decode(const cqa_cache* shared, const cqa_cache* h, int32_t layer, const void* q, const void* kd, const void* vd, int32_t n_nodes,
+                            const uint64_t* mask, const cqa_scoring* scoring, const cqa_tolerances* tol, void* O, cqa_node_cert* cert, uint32_t* flags,
+                            void* ws, void* stream) {
+  if (h == nullptr || layer < 0 || layer >= h->impl.desc.n_layers || (shared != nullptr && layer >= shared->impl.desc.n_layers) || q == nullptr ||
+      (kd == nullptr) != (vd == nullptr) || (kd == nullptr && mask != nullptr) || tol == nullptr || O == nullptr || cert == nullptr || flags == nullptr ||
+      ws == nullptr || !aligned(q, 2) || !aligned(kd, 2) || !aligned(vd, 2) || !aligned(mask, 8) || !aligned(O, 16) || !aligned(cert, 16) ||
+      !aligned(flags, 16) || !aligned(ws, 16))
+    return CQA_ERR_INVALID_ARG;
+  if (const int32_t rc = check_nodes(shared, h, n_nodes)) return rc;
+  if (const int32_t rc = check_scoring(scoring)) return rc;
+  if (const int32_t rc = check_tolerances(tol, 0)) return rc;
+  if (tol->int8_query != 0) return CQA_ERR_UNSUPPORTED;
+  const Cache* const c = &h->impl;
+  const Cache* const s = shared != nullptr ? &shared->impl : nullptr;
+  // places and spans count in 32 bits, with 2^30 of room to either side
+  if (c->length[layer] + (s != nullptr ? s->length[layer] : 0) >= (int64_t)1 << 30) return CQA_ERR_UNSUPPORTED;
+  if (const int32_t rc = check_device(c)) return rc;
+  const NodeCall x = {(const __half*)q, (const __half*)kd, (const __half*)vd, n_nodes, mask, scoring, tol, (__half*)O, cert, flags};
+  return launch_scored(s, c, layer, x, (float*)ws, (hipStream_t)stream);
+}
+
+int32_t cqa_scored_workspace_bytes(const cqa_cache* h, int32_t n_nodes, int64_t* bytes) { return nodes_workspace(nullptr, h, n_nodes, bytes); }
+
+int32_t cqa_scored_decode(const cqa_cache* h, int32_t layer, const void* q_fp16_dev, const void* k_draft_dev, const void* v_draft_dev, int32_t n_nodes,
+                          const uint64_t* mask_dev, const cqa_scoring* scoring, const cqa_tolerances* tol, void* O_dev, cqa_node_cert* cert_dev,
+                          uint32_t* flags_dev, void* workspace_dev, void* stream) {
+  return nodes_decode(nullptr, h, layer, q_fp16_dev, k_draft_dev, v_draft_dev, n_nodes, mask_dev, scoring, tol, O_dev, cert_dev, flags_dev, workspace_dev, stream);
+}
+
+int32_t cqa_prefix_workspace_bytes(const cqa_cache* shared, const cqa_cache* h, int32_t n_nodes, int64_t* bytes) {
+  return shared == nullptr ? CQA_ERR_INVALID_ARG : nodes_workspace(shared, h, n_nodes, bytes);
+}
+
+int32_t cqa_prefix_decode(const cqa_cache* shared, const cqa_cache* h, int32_t layer, const void* q_fp16_dev, const void* k_draft_dev,
+                          const void* v_draft_dev, int32_t n_nodes, const uint64_t* mask_dev, const cqa_scoring* scoring, const cqa_tolerances* tol,
+                          void* O_dev, cqa_node_cert* cert_dev, uint32_t* flags_dev, void* workspace_dev, void* stream) {
+  if (shared == nullptr) return CQA_ERR_INVALID_ARG;
+  return nodes_decode(shared, h, layer, q_fp16_dev, k_draft_dev, v_draft_dev, n_nodes, mask_dev, scoring, tol, O_dev, cert_dev, flags_dev, workspace_dev, stream);
+}
+
 }  // extern "C"

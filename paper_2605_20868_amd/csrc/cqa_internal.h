@@ -465,6 +465,19 @@ int32_t launch_read(const Cache* c, int layer, int64_t first, int64_t n, int typ
 int32_t launch_tree(const Cache* c, int layer, const __half* q, const __half* kd, const __half* vd, int n_draft, const uint64_t* mask,
                     const cqa_tolerances& tol, __half* O, cqa_node_cert* cert, uint32_t* flags, float* ws, hipStream_t st);
 int64_t tree_ws_bytes(const Cache* c, int n_draft);
+// Nodes with scores of the caller's, sequences behind a shared beginning (scored.hip); shared: null = none
+struct NodeCall {
+  const __half *q, *kd, *vd;      // kd, vd null: no drafted tokens
+  int n;
+  const uint64_t* mask;
+  const cqa_scoring* scoring;     // null: the plain scores
+  const cqa_tolerances* tol;
+  __half* O;
+  cqa_node_cert* cert;
+  uint32_t* flags;
+};
+int32_t launch_scored(const Cache* shared, const Cache* c, int layer, const NodeCall& x, float* ws, hipStream_t st);
+int64_t scored_ws_bytes(const Cache* shared, const Cache* c, int n);
 
 inline uint32_t* ladder_raised(Cache* c) { return c->ladder_counts + 2; }
 inline uint32_t next_ladder_tag(Cache* c) {
