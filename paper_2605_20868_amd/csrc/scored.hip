@@ -3,7 +3,7 @@
 //
 // A beginning's cached tokens are one sequence for all who share it: their nodes are its rows, so that it is read and reconstructed once for up to 256 of
 // them instead of once a sequence.  A pass over it and one over the sequences' own tokens leave partial sets, which one launch joins.
-#include "tree_inl.h"
+#include "light_inl.h"
 
 namespace cqa {
 
@@ -27,7 +27,7 @@ struct SetsOfTwo {
     return reinterpret_cast<const float4*>(p)[c * T_ROWS + r];
   }
 };
-template <bool SCORES>
+template <Scores SCORES>
 struct JoinArgs : SetArgs<SCORES> {
   const float* own;              // the sequences' own sets [Bt * Hkv][own_tiles][own_sets][T_FLOATS]
   int own_tiles, own_sets;
@@ -41,10 +41,38 @@ struct JoinArgs : SetArgs<SCORES> {
 };
 
 static int row_count(const Cache* c, int64_t nodes) { return (int)(nodes * (c->desc.n_q_heads / c->desc.n_kv_heads)); }
+// Rows of a KV group a workgroup takes, and the partial sets of a row.
+struct Shape {
+  int rows, nsplit;
+};
+static int light_splits(int n_cu, int64_t heads, int waves, int64_t sealed, int64_t others) {
+  const int64_t most = std::max<int64_t>(1, 12 / waves * (int64_t)n_cu / heads), tiles = (sealed + 32 * waves - 1) / (32 * waves);
+  return (int)std::min(most, tiles <= 1 && others <= L_EXACT ? 1 : tiles + (others + L_EXACT - 1) / L_EXACT);
+}
+static Shape shape_of(int n_cu, int64_t heads, int n_rows, int64_t sealed, int64_t others) {
+  if (n_rows <= L_ROWS) {
+    const int most = light_splits(n_cu, heads, 12, 1 << 30, 0);
+    const int waves = (sealed + 383) / 384 >= 3 * most ? 12 : 4;
+    return {waves == 4 ? L_ROWS : L_ROWS + 1, light_splits(n_cu, heads, waves, sealed, others)};
+  }
+  const int rows = tree_rows(n_cu, heads, n_rows, sealed, others);
+  return {rows, tree_splits(n_cu, heads, n_rows, rows, sealed, others)};
+}
+template <typename A>
+static int32_t launch_rows(const A& a, int64_t heads, int rows, int others, hipStream_t st) {
+  if (rows > L_ROWS + 1) return launch_pass(a, heads, rows, others, st);
+  if (rows == L_ROWS)
+    tree_light_kernel<4><<<dim3((uint32_t)heads, (uint32_t)a.nsplit), 256, 0, st>>>(a);
+  else
+    tree_light_kernel<12><<<dim3((uint32_t)heads, (uint32_t)a.nsplit), 768, 0, st>>>(a);
+  CQA_HIP(hipGetLastError());
+  return CQA_OK;
+}
 static int64_t set_floats(const Cache* c, int64_t nodes, int64_t others) {
   const int64_t heads = (int64_t)c->desc.batch * c->desc.n_kv_heads;
   const int n_rows = row_count(c, nodes);
   const auto most = [&](int rows) { return (int64_t)tree_splits(c->n_cu, heads, n_rows, rows, c->desc.max_tokens, others); };
+  if (n_rows <= L_ROWS) return heads * light_splits(c->n_cu, heads, 4, c->desc.max_tokens, others) * T_FLOATS;
   return heads * ((n_rows + 31) / 32) * std::max(most(32), most(n_rows <= 64 ? 64 : (n_rows <= 128 ? 128 : 256))) * T_FLOATS;
 }
 int64_t scored_ws_bytes(const Cache* shared, const Cache* c, int n) {
@@ -54,7 +82,7 @@ int64_t scored_ws_bytes(const Cache* shared, const Cache* c, int n) {
 }
 
 // What the pass over c's tokens takes, of `nodes` nodes of each of its sequences.  others: drafted tokens.
-template <bool SCORES>
+template <Scores SCORES>
 static int put_pass(SetArgs<SCORES>& a, const Cache* c, int layer, int nodes, int drafts, int first, float* part) {
   const int64_t head0 = head_index(c, layer, 0, 0), heads = (int64_t)c->desc.batch * c->desc.n_kv_heads;
   a.t1 = c->t1 + head0 * c->nq_cap * QUAD_BYTES;
@@ -69,13 +97,13 @@ static int put_pass(SetArgs<SCORES>& a, const Cache* c, int layer, int nodes, in
   a.part = part;
   const int n_rows = nodes * a.group, others = a.trail + drafts;
   a.row_tiles = (n_rows + 31) / 32;
-  const int rows = tree_rows(c->n_cu, heads, n_rows, a.nb * BLK, others);
-  a.nsplit = tree_splits(c->n_cu, heads, n_rows, rows, a.nb * BLK, others);
-  if (rows > 32) put_shares(a, rows, others);
-  return rows;
+  const Shape x = shape_of(c->n_cu, heads, n_rows, a.nb * BLK, others);
+  a.nsplit = x.nsplit;
+  if (x.rows > 32) put_shares(a, x.rows, others);
+  return x.rows;
 }
 
-template <bool SCORES>
+template <Scores SCORES>
 static int32_t run(const Cache* shared, const Cache* c, int layer, const NodeCall& x, float* ws, hipStream_t st) {
   SetArgs<SCORES> a = {};
   a.q = x.q;
@@ -93,14 +121,15 @@ static int32_t run(const Cache* shared, const Cache* c, int layer, const NodeCal
   a.each = x.n;
   a.cached = (int)(beginning + c->length[layer]);
   a.drafted = x.kd != nullptr;
-  if (SCORES) {
+  if (SCORES != PLAIN) {
     const cqa_scoring& s = *x.scoring;
-    constexpr float LOG2E = 1.4426950408889634f, LOW_CAPS = 256.0f;   // (CAP_LOW at 256: 3e-5 of a score)
+    constexpr float LOG2E = 1.4426950408889634f;
     a.scale = s.scale != 0.0f ? s.scale : 0.08838834764831845f;
     a.cap = s.cap;
     a.cap_kind = s.cap == 0.0f ? CAP_NONE : (s.cap <= LOW_CAPS ? CAP_LOW : CAP_HIGH);
     a.gain = a.cap_kind == CAP_NONE ? 0.0f : (a.cap_kind == CAP_LOW ? 2.0f * LOG2E : 1.0f) * (a.scale / s.cap);
     a.per_unit = LOG2E * (a.cap_kind == CAP_NONE ? a.scale : (a.cap_kind == CAP_LOW ? 2.0f * s.cap : s.cap));
+    a.level = a.cap_kind == CAP_NONE ? a.per_unit : 1.0f;
     a.offset = a.cap_kind == CAP_LOW ? s.cap : 0.0f;
     a.slopes = s.slopes_dev;
     a.places = s.places_dev;
@@ -110,7 +139,7 @@ static int32_t run(const Cache* shared, const Cache* c, int layer, const NodeCal
   const bool own = beginning == 0 || c->length[layer] + drafts > 0;
   if (beginning == 0) {
     const int rows = put_pass(a, c, layer, x.n, drafts, 0, ws);
-    if (const int32_t rc = launch_pass(a, heads, rows, a.trail + drafts, st)) return rc;
+    if (const int32_t rc = launch_rows(a, heads, rows, a.trail + drafts, st)) return rc;
     return a.nsplit == 1 ? CQA_OK : launch_join(a, heads, a.nsplit, c->n_cu, st);
   }
   const int64_t shared_heads = (int64_t)shared->desc.batch * shared->desc.n_kv_heads;
@@ -118,11 +147,11 @@ static int32_t run(const Cache* shared, const Cache* c, int layer, const NodeCal
   static_cast<SetArgs<SCORES>&>(j) = a;
   const int shared_rows = put_pass(static_cast<SetArgs<SCORES>&>(j), shared, layer, x.n * (c->desc.batch / shared->desc.batch), 0, 0, ws);
   j.row_sets = own;
-  if (const int32_t rc = launch_pass(static_cast<const SetArgs<SCORES>&>(j), shared_heads, shared_rows, j.trail, st)) return rc;
+  if (const int32_t rc = launch_rows(static_cast<const SetArgs<SCORES>&>(j), shared_heads, shared_rows, j.trail, st)) return rc;
   if (!own) return j.nsplit == 1 ? CQA_OK : launch_join(static_cast<const SetArgs<SCORES>&>(j), shared_heads, j.nsplit, c->n_cu, st);
   a.row_sets = 1;
   const int rows = put_pass(a, c, layer, x.n, drafts, (int)beginning, ws + shared_heads * j.row_tiles * j.nsplit * T_FLOATS);
-  if (const int32_t rc = launch_pass(a, heads, rows, a.trail + drafts, st)) return rc;
+  if (const int32_t rc = launch_rows(a, heads, rows, a.trail + drafts, st)) return rc;
   j.own = a.part;
   j.own_tiles = a.row_tiles;
   j.own_sets = a.nsplit;
@@ -131,8 +160,9 @@ static int32_t run(const Cache* shared, const Cache* c, int layer, const NodeCal
 
 int32_t launch_scored(const Cache* shared, const Cache* c, int layer, const NodeCall& x, float* ws, hipStream_t st) {
   const cqa_scoring* const s = x.scoring;
-  const bool plain = s == nullptr || ((s->scale == 0.0f || s->scale == 0.08838834764831845f) && s->cap == 0.0f && s->slopes_dev == nullptr && s->spans_dev == nullptr);
-  return plain ? run<false>(shared, c, layer, x, ws, st) : run<true>(shared, c, layer, x, ws, st);
+  if (s != nullptr && (s->slopes_dev != nullptr || s->spans_dev != nullptr)) return run<PLACED>(shared, c, layer, x, ws, st);
+  if (s != nullptr && ((s->scale != 0.0f && s->scale != 0.08838834764831845f) || s->cap != 0.0f)) return run<SCALED>(shared, c, layer, x, ws, st);
+  return run<PLAIN>(shared, c, layer, x, ws, st);
 }
 
 }  // namespace cqa

@@ -61,7 +61,7 @@ constexpr int T_FLOATS = T_OFLOATS + 8 * T_ROWS;
 
 struct SetsOf;
 struct TreeArgs {
-  static constexpr bool SETS = false, SCORED = false;   // (SetArgs)
+  static constexpr bool SETS = false, SCORED = false, PLACED = false;   // (SetArgs)
   const uint8_t* t1;       // layer base of the quad records
   const __half* trail_k;   // layer base [Bt * Hkv][16][128]
   const __half* trail_v;
@@ -84,6 +84,7 @@ struct TreeArgs {
   __device__ int drafts() const { return n; }
   __device__ SetsOf sets_of(const float* sets, int head, int r32, int r) const;
   __device__ float unit() const { return SCORE; }        // exponents of 2 that a unit of score is worth
+  __device__ float m_unit() const { return SCORE; }
   __device__ float half_scale() const { return HALF_SCORE; }
 };
 
@@ -97,9 +98,11 @@ struct TreeArgs {
 // and the bias counts from the distance `near` of the row's nearest attended token (the farthest, under a negative slope), so that the scores of a
 // row that attends far tokens only keep their bits.
 enum { CAP_NONE = 0, CAP_LOW, CAP_HIGH };
-template <bool SCORES>
+constexpr float LOW_CAPS = 256.0f;
+enum Scores { PLAIN = 0, SCALED, PLACED };   // q . k / sqrt(d) of every token; by scale and cap; by places and spans as well
+template <Scores SCORES>
 struct SetArgs : TreeArgs {
-  static constexpr bool SETS = true, SCORED = SCORES;
+  static constexpr bool SETS = true, SCORED = SCORES != cqa::PLAIN, PLACED = SCORES == cqa::PLACED;
   int nd;                  // drafted tokens of a sequence in this pass: its nodes, or none
   int row_sets;            // not 0: the sets are not all of a row's, they are left to be joined
   // scores
@@ -110,13 +113,16 @@ struct SetArgs : TreeArgs {
   int cap_kind;
   float gain;              // x / cap by q . k: CAP_LOW in exponents of 2, twice
   float per_unit, offset;  // offset: of the score, where the unit's zero is
+  float level;             // exponents of 2 by a row's m: 1 with a cap, per_unit without
   float cap, scale;
   const float* slopes;     // [Hq]
   const int64_t* places;   // [Bt][n]
   const int64_t* spans;    // [Bt][n][4]
   __device__ int drafts() const { return nd; }
-  __device__ float unit() const { return SCORES ? per_unit : SCORE; }
-  __device__ float half_scale() const { return SCORES ? 0.5f * scale : HALF_SCORE; }
+  __device__ float unit() const { return SCORED ? per_unit : SCORE; }
+  __device__ float m_unit() const { return SCORED ? level : SCORE; }
+  __device__ bool capped() const { return SCORED && cap_kind != CAP_NONE; }
+  __device__ float half_scale() const { return SCORED ? 0.5f * scale : HALF_SCORE; }
 };
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
@@ -179,13 +185,27 @@ struct TreeRows {
   float m, sum, sealed, ev, evmax, dmax, vmax;
   int node;
 };
-struct ScoredRows : TreeRows {
-  float slope;       // in units of score
-  int place, near;   // the node's place from the pass's first cached token
-  bool undefined;    // a number of the query is not finite: a cap would hide it
+// Of a pass of SetArgs.
+struct SetRows : TreeRows {
+  template <typename F>
+  __device__ __forceinline__ void each_sum(F f) {
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[ct][r] = f(o[ct][r]);
+  }
 };
+template <typename Rows>
+struct Scored : Rows {
+  bool undefined;            // a number of the query is not finite: a cap would hide it
+  // of PLACED ones
+  float slope = 0.0f;        // in units of score
+  int place = 0, near = 0;   // the node's place from the pass's first cached token
+  bool idle = false;         // attends no cached token of the pass
+};
+using ScoredRows = Scored<SetRows>;
 template <typename A>
-using RowsOf = std::conditional_t<A::SCORED, ScoredRows, TreeRows>;
+using RowsOf = std::conditional_t<A::SCORED, ScoredRows, std::conditional_t<A::SETS, SetRows, TreeRows>>;
 
 // ---- scores: spans and bias of a row ---------------------------------------------------------------------------------------------------
 
@@ -248,36 +268,46 @@ __device__ __forceinline__ RowBias row_bias(const A& a, int64_t node, int q_head
 template <typename A>
 __device__ __forceinline__ float row_offset(const A& a, int64_t node, int q_head) {
   if constexpr (A::SCORED) {
+    if constexpr (!A::PLACED) return a.offset;
     const RowBias x = row_bias(a, node, q_head);
     return a.slopes == nullptr ? a.offset : fmaf(-x.slope, (float)x.near, a.offset);
   }
   return 0.0f;
 }
-// A lane's products with 16 tokens become scores; `bias`: places are asked for.
-template <typename A, typename Far>
-__device__ __forceinline__ void score16(const A& a, const ScoredRows& w, f32x16& s, Far far) {
+// A lane's products with N tokens become scores.  far(r): |place - token| - near.
+// (tanh by a series of six coefficients where all of a wave's products are in its range, which is relatively exact at the small ones, is two operations a
+// score more: 8 heads, 131072 tokens, 64 nodes of 4 heads 293 us, so 241.)
+template <typename A>
+__device__ __forceinline__ float cap_low(const A& a, float s) { return __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s * a.gain)); }
+// low_done: CAP_LOW has been applied.
+template <int N, typename A, typename Rows, typename V, typename Far>
+__device__ __forceinline__ void score(const A& a, const Rows& w, V& s, Far far, bool low_done = false) {
   if (a.cap_kind == CAP_LOW) {
+    if (!low_done)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s[r] * a.gain));
+      for (int r = 0; r < N; ++r) s[r] = cap_low(a, s[r]);
   } else if (a.cap_kind == CAP_HIGH) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      // (tanh x = 1 - 2 / (1 + e^2x) loses its relative accuracy near zero, where five terms of the series have it)
+    for (int r = 0; r < N; ++r) {
+      // (1 - 2 / (1 + e^2x) loses its relative accuracy near zero, where five terms of the series have it)
       const float x = s[r] * a.gain, y = x * x;
       const float low = x * fmaf(y, fmaf(y, fmaf(y, fmaf(y, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
       const float high = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f / LN2))), 1.0f);
       s[r] = fabsf(x) < 0.25f ? low : high;
     }
   }
-  if (a.slopes != nullptr)
+  if constexpr (A::PLACED)
+    if (a.slopes != nullptr)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = fmaf(-w.slope, far(r), s[r]);
+      for (int r = 0; r < N; ++r) s[r] = fmaf(-w.slope, far(r), s[r]);
 }
-// |place - token| - near of 16 tokens from t on: |from - r| + rest, whether the place is ahead of them, behind them or among them.
-struct BlockFar {
+// |place - token| - near of N tokens from t on: |from - r| + rest, whether the place is ahead of them, behind them or among them.
+template <int N>
+struct RunFar {
   float from, rest;
-  __device__ __forceinline__ BlockFar(const ScoredRows& w, int t) {
-    const int d = w.place - t, b = min(max(d, 0), BLK - 1);
+  template <typename Rows>
+  __device__ __forceinline__ RunFar(const Rows& w, int t) {
+    const int d = w.place - t, b = min(max(d, 0), N - 1);
     from = (float)b;
     rest = (float)(abs(d - b) - w.near);
   }
@@ -302,6 +332,7 @@ __device__ __forceinline__ Hull hull_of(const Spans& s) {
   for (int i = 0; i < 2; ++i) {
     h.lo[i] = lo[i] < hi[i] ? lo[i] : NONE, h.hi[i] = lo[i] < hi[i] ? hi[i] : -1;
     h.in_lo[i] = lo[i], h.in_hi[i] = hi[i];
+    if (s.hi0 == 0 && s.hi1 == 0) h.in_lo[i] = 0, h.in_hi[i] = NONE;   // (an idle row: drop_idle)
   }
 #pragma unroll
   for (int k = 1; k < 64; k *= 2)
@@ -382,6 +413,7 @@ __device__ __forceinline__ void score_rows(ScoredRows& s, const A& a, int b, int
   s.place = x.place - a.first;
   s.near = x.near;
   mine = node_spans(a, node, a.first, count);
+  s.idle = a.spans != nullptr && mine.hi0 == 0 && mine.hi1 == 0;
   if (a.spans != nullptr && l < T_ROWS) at[l] = mine;
 }
 
@@ -404,7 +436,7 @@ __device__ __forceinline__ void values32(TreeRows& w, const uint32_t (&p)[8], Va
 }
 // What weights relative to a largest score m are worth beside a largest one M >= m (-inf: there are none).
 template <typename A>
-__device__ __forceinline__ float set_weight(const A& a, float m, float M) { return m == M ? 1.0f : __builtin_amdgcn_exp2f((m - M) * a.unit()); }
+__device__ __forceinline__ float set_weight(const A& a, float m, float M) { return m == M ? 1.0f : __builtin_amdgcn_exp2f((m - M) * a.m_unit()); }
 // Scores of MT times 32 tokens to weights, 2^MOST for a row's largest score so far, the row's m.  The weights enter
 // the product with the values as FP16: those down to 2^-28 of the largest keep 11 bits, and a million lighter ones are together off by 2^-19
 // of it.  (With 1 for the largest, tokens of 2^-25 of it vanished, and all of the result with them where the heavy ones' values are zero.)
@@ -458,14 +490,86 @@ __device__ __forceinline__ void softmax32(const A& a, TreeRows& w, f32x16 (&s)[M
     w.evmax = fmaxf(w.evmax, e);
   }
 }
+// The same in passes of SetArgs, for MT times N scores of a lane.  With a cap, which bounds them, a row's m is its largest score's exponent of 2, upwards, a
+// whole number: a weight's exponent is one multiply-add, and sets of different m join exactly.  largest(x): over the lanes of a row; block(x): the sum
+// over a block.
+template <int MT, int N, typename A, typename Rows, typename V, typename Bits, typename Eta, typename Largest, typename Block>
+__device__ __forceinline__ void softmax_sets(const A& a, Rows& w, V (&s)[MT], uint32_t (&p)[MT][N / 2], bool masked, Bits bits, Eta eta, Largest largest, Block block) {
+  if (masked) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const uint32_t x = bits(mt);
+#pragma unroll
+      for (int r = 0; r < N; ++r) s[mt][r] = x >> r & 1u ? s[mt][r] : -INFINITY;
+    }
+  }
+  float top = -INFINITY;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int r = 0; r < N; ++r) top = fmaxf(top, s[mt][r]);
+  top = largest(top);
+  top = a.capped() ? ceilf(top * a.unit()) : top;
+  if (__any(top > w.m)) {
+    const float mn = fmaxf(w.m, top);
+    const float f = set_weight(a, w.m, mn);
+    w.m = mn;
+    w.sum *= f;
+    w.sealed *= f;
+    w.ev *= f;
+    w.evmax *= f;
+    w.each_sum([&](float o) { return o * f; });
+  }
+  const float m = w.m == -INFINITY ? 0.0f : w.m;   // nothing attended yet: every weight is exp2(-inf) = 0
+  const float most = a.capped() ? MOST - m : MOST;
+  if (!a.capped())
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int r = 0; r < N; ++r) s[mt][r] -= m;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    float bs = 0.0f;
+#pragma unroll
+    for (int r = 0; r < N / 2; ++r) {
+      const int i = (r & 4) * 2 + (r & 3);   // tokens i and i + 4
+      const float x = __builtin_amdgcn_exp2f(fmaf(s[mt][i], a.unit(), most));
+      const float y = __builtin_amdgcn_exp2f(fmaf(s[mt][i + 4], a.unit(), most));
+      bs += x + y;
+      p[mt][r] = pack_f16(x, y);
+    }
+    w.sum += bs;
+    w.ev = fmaf(bs, eta(mt), w.ev);
+    w.evmax = fmaxf(w.evmax, block(bs) * eta(mt));
+  }
+}
+// ... of 32 rows
+template <int MT, typename A, typename Rows, typename Bits, typename Eta>
+__device__ __forceinline__ void weigh32(const A& a, Rows& w, f32x16 (&s)[MT], uint32_t (&p)[MT][8], bool masked, Bits bits, Eta eta) {
+  if constexpr (A::SETS)
+    softmax_sets<MT, 16>(a, w, s, p, masked, bits, eta, [](float x) { return max_x32(x); }, [](float x) { return x; });
+  else
+    softmax32<MT>(a, w, s, p, masked, bits, eta);
+}
+// What an idle row has had with the others, whose tokens are not looked at one by one where they are all the others', is dropped.
+template <typename Rows>
+__device__ __forceinline__ void drop_idle(Rows& w, uint32_t& open) {
+  if (!__any(w.idle)) return;
+  if (w.idle) {
+    w.m = -INFINITY;
+    w.sum = w.sealed = w.ev = w.evmax = w.dmax = w.vmax = 0.0f;
+    open = 0u;
+    w.each_sum([](float) { return 0.0f; });
+  }
+}
 // All of it, of exact tokens.
 template <typename A, typename Key, typename Value>
 __device__ __forceinline__ void attend32(const A& a, RowsOf<A>& w, uint32_t bits, const int* places, Key key, Value value) {
   f32x16 s[1];
   uint32_t p[1][8];
   scores32(w, s[0], key);
-  if constexpr (A::SCORED) score16(a, w, s[0], [&](int r) { return (float)(abs(w.place - places[r]) - w.near); });
-  softmax32<1>(a, w, s, p, true, [&](int) { return bits; }, [&](int) { return 0.0f; });
+  if constexpr (A::SCORED) score<16>(a, w, s[0], [&](int r) { return (float)(abs(w.place - places[r]) - w.near); });
+  weigh32<1>(a, w, s, p, true, [&](int) { return bits; }, [&](int) { return 0.0f; });
   values32(w, p[0], value);
 }
 
@@ -493,13 +597,18 @@ __device__ __forceinline__ void bound_scores(TreeRows& w, Width width, bool mask
 __device__ __forceinline__ int key_place(int blk, int t) { return (blk >> 1) * 32 + (t >> 2) * 8 + (blk & 1) * 4 + (t & 3); }
 // run of 8 tokens of channel c among the values of a tile: the A operand's rows are (c >> 6, c & 15), its tiles (c >> 4) & 3
 __device__ __forceinline__ int value_place(int oct, int c) { return oct * D + ((c >> 4) & 3) * 32 + (c >> 6) * 16 + (c & 15); }
+// The places of trailing and drafted tokens, for operands of 32 rows.
+struct Places32 {
+  static __device__ __forceinline__ int key(int t) { return key_place(t / BLK, t % BLK); }
+  static __device__ __forceinline__ int value(int oct, int c) { return value_place(oct, c); }
+};
 
 // Trailing and drafted tokens t0 .. t0 + TOK - 1 (of trail + n; zeros behind the last) by THREADS threads, thread `tid`.
 //   keys [16 runs of 8 channels][TOK], values [TOK / 8][128] by value_place, norms [TOK], bad [TOK]: 1 for a token with a number that
 //   is not finite (zeros before)
 // Such a number must not meet the zero weight of a row that does not attend its token: it is taken out, and the rows that do attend
 // the token get a sum that is no number.
-template <int THREADS, int TOK, typename A>
+template <int THREADS, int TOK, typename Places = Places32, typename A>
 __device__ __forceinline__ void load_exact(const A& a, int64_t head, int t0, int tid, uint4* keys, uint4* values, float* norms, uint8_t* bad) {
   const int total = a.trail + a.drafts();
   const auto finite = [](uint32_t x) { return finite2(x); };
@@ -535,7 +644,7 @@ __device__ __forceinline__ void load_exact(const A& a, int64_t head, int t0, int
     if (there & (ok ^ 1u)) bad[t] = 1;
     const uint32_t keep = 0u - (there & ok);
     x.x &= keep, x.y &= keep, x.z &= keep, x.w &= keep;
-    keys[(i & 15) * TOK + key_place(t / BLK, t % BLK)] = x;
+    keys[(i & 15) * TOK + Places::key(t)] = x;
   }
   // four channels of eight tokens
 #pragma unroll
@@ -567,7 +676,7 @@ __device__ __forceinline__ void load_exact(const A& a, int64_t head, int t0, int
       uint32_t h[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) h[j] = __builtin_amdgcn_perm(x[j + 4][e >> 1], x[j][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
-      values[value_place(oct, c + e)] = make_uint4(h[0], h[1], h[2], h[3]);
+      values[Places::value(oct, c + e)] = make_uint4(h[0], h[1], h[2], h[3]);
     }
   }
 }
@@ -756,7 +865,7 @@ __device__ __forceinline__ Certificate certificate(const A& a, float M, float L,
   ct.delta_h = DM;
   ct.v_max = VM;
   ct.alpha_tail_hat = sealed * inv;
-  ct.lse = empty ? -INFINITY : fmaf(M, a.unit() * LN2, logf(L) - MOST * LN2);
+  ct.lse = empty ? -INFINITY : fmaf(M, a.m_unit() * LN2, logf(L) - MOST * LN2);
   if constexpr (A::SCORED) ct.lse = empty ? ct.lse : ct.lse + offset;
   ct.max_block_contrib = EM * inv;
   ct.reserved = 0.0f;
@@ -906,8 +1015,8 @@ struct FewLds {
   uint8_t* q;               // [Q_TILE]
   float* norm;              // [EXACT]
   uint8_t* bad;             // [EXACT]
-  int* place;               // [EXACT], SCORED
-  Spans* span;              // [T_ROWS], SCORED
+  int* place;               // [EXACT], PLACED
+  Spans* span;              // [T_ROWS], PLACED
 };
 template <int EXACT, typename A>
 __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, int tile, const FewLds& lds) {
@@ -927,7 +1036,7 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
   Active active;
   Spans mine;
   bool spans = false;
-  if constexpr (A::SCORED) {
+  if constexpr (A::PLACED) {
     rows.node = min(tile * T_ROWS + n32, a.n * a.group - 1) / a.group;
     score_rows(rows, a, b, kvh, tile, (int)a.nb * BLK + a.trail, lds.span, mine);   // (every wave the same)
     spans = a.spans != nullptr;
@@ -937,7 +1046,7 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
     }
   }
   const auto pair_at = [&](int u) {
-    if constexpr (A::SCORED) return spans ? active.at(u) : u;
+    if constexpr (A::PLACED) return spans ? active.at(u) : u;
     return u;
   };
   const int step = FEW_WAVES * a.nsplit;
@@ -978,12 +1087,12 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
 
   const float* const sg = reinterpret_cast<const float*>(wave + FEW_KM) + bsel * FEW_KM_BLK + half * FEW_KM_HALF;
   const uint8_t* const sc = wave + FEW_VM + half * FEW_VM_BLK + (n32 >> 4) * 64;
-  uint32_t open = 0u;   // SCORED: tokens of sealed blocks that the lane's row has attended
+  uint32_t open = 0u;   // PLACED: tokens of sealed blocks that the lane's row has attended
   for (int turn = 0; u < units; u += step, ++turn) {
     const int pair = pair_at(u);
     uint32_t there = 0xffffu;
     bool masked = (int64_t)pair * 2 + 2 > a.nb;
-    if constexpr (A::SCORED) {
+    if constexpr (A::PLACED) {
       if (spans && !active.open(pair * 2 * BLK, (pair + 1) * 2 * BLK)) {
         masked = true;
         there = span_bits(lds.span[n32], (pair * 2 + half) * BLK);
@@ -998,7 +1107,7 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
     *reinterpret_cast<uint4*>(at + FEW_KM_BLK) = km1;
     *reinterpret_cast<uint4*>(wave + FEW_VM + half * FEW_VM_BLK + n32 * 16) = paired(vm);
     const float eta = value_error(an);
-    rows.vmax = fmaxf(rows.vmax, A::SCORED && there == 0u ? 0.0f : an.y);
+    rows.vmax = fmaxf(rows.vmax, A::PLACED && there == 0u ? 0.0f : an.y);
     load_meta(u + step);
     wave_sync();
     // Operands' metadata are read a product ahead of their use.
@@ -1051,9 +1160,9 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
           });
       wave_sync();
     }
-    if constexpr (A::SCORED) score16(a, rows, x[0], BlockFar(rows, (pair * 2 + half) * BLK));
-    softmax32<1>(
-        a, rows, x, p, masked, [&](int) { return A::SCORED ? there : ((int64_t)u * 2 + half < a.nb ? 0xffffu : 0u); }, [&](int) { return eta; });
+    if constexpr (A::SCORED) score<16>(a, rows, x[0], RunFar<BLK>(rows, (pair * 2 + half) * BLK));
+    weigh32<1>(
+        a, rows, x, p, masked, [&](int) { return A::PLACED ? there : ((int64_t)u * 2 + half < a.nb ? 0xffffu : 0u); }, [&](int) { return eta; });
     each<8>([&](auto i_) {
       constexpr int I = i_.value, ct = I & 3, oct = I >> 2;
       __builtin_amdgcn_sched_barrier(0);
@@ -1068,15 +1177,16 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
     load_values(u + step);
     wave_sync();
   }
+  if constexpr (A::PLACED) drop_idle(rows, open);
   rows.sealed = rows.sum;
-  if constexpr (!A::SCORED) open = split * FEW_WAVES + w < units;
+  if constexpr (!A::PLACED) open = split * FEW_WAVES + w < units;
   // The other tokens, dealt from the workgroup on whose turn is the next, which fetches them together; as many of its waves as they have pairs of blocks attend them.
   for (int t0 = (split + a.nsplit - (units + FEW_WAVES - 1) / FEW_WAVES % a.nsplit) % a.nsplit * EXACT; t0 < a.trail + a.drafts(); t0 += a.nsplit * EXACT) {
     uint4* const s_k = reinterpret_cast<uint4*>(s_set);
     uint4* const s_v = s_k + 16 * EXACT;
     const int blk = 2 * w + half;
     uint32_t bits = open_tokens(a, b, rows.node, t0 + blk * BLK);
-    if constexpr (A::SCORED) {
+    if constexpr (A::PLACED) {
       if (spans) bits &= span_bits(lds.span[n32], (int)a.nb * BLK + t0 + blk * BLK) | ~trailing_bits(a, t0 + blk * BLK);
       if (a.slopes != nullptr && tid < EXACT) lds.place[tid] = exact_place(a, b, t0 + tid);
     }
@@ -1088,7 +1198,7 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
       open |= bits;
       open_exact(rows, bits, s_norm + blk * BLK, s_bad + blk * BLK);
       attend32(
-          a, rows, bits, A::SCORED ? lds.place + blk * BLK : nullptr, [&](int ks) { return __builtin_bit_cast(f16x8, s_k[(half * 8 + ks) * EXACT + w * 32 + n32]); },
+          a, rows, bits, A::PLACED ? lds.place + blk * BLK : nullptr, [&](int ks) { return __builtin_bit_cast(f16x8, s_k[(half * 8 + ks) * EXACT + w * 32 + n32]); },
           [&](int oct, int ct) { return __builtin_bit_cast(f16x8, s_v[(blk * 2 + oct) * D + ct * 32 + n32]); });
     }
     __syncthreads();   // (the next ones, or the waves' sets, come where these are)
@@ -1109,7 +1219,7 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(A a) {
   __shared__ __align__(16) uint8_t s_q[Q_TILE];
   __shared__ __align__(16) float s_norm[EXACT];
   __shared__ __align__(16) uint8_t s_bad[EXACT];
-  if constexpr (A::SCORED) {
+  if constexpr (A::PLACED) {
     __shared__ __align__(16) int s_place[EXACT];
     __shared__ __align__(16) Spans s_span[T_ROWS];
     attend_few<EXACT>(a, blockIdx.x, blockIdx.y, blockIdx.z, FewLds{s_set, s_q, s_norm, s_bad, s_place, s_span});
@@ -1169,9 +1279,9 @@ struct ManyLds {
   float (*eta)[ManyShape<WR>::BLKS];            // [4]
   float* norm;                                  // [TOK]
   uint8_t* bad;                                 // [TOK]
-  float (*nu)[ManyShape<WR>::BLKS];             // [4], SCORED
-  int* place;                                   // [TOK], SCORED
-  Spans (*span)[T_ROWS];                        // [8], SCORED
+  float (*nu)[ManyShape<WR>::BLKS];             // [4], PLACED
+  int* place;                                   // [TOK], PLACED
+  Spans (*span)[T_ROWS];                        // [8], PLACED
 };
 template <int WR, typename A>
 __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split, int z, const ManyLds<WR>& lds) {
@@ -1197,7 +1307,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
   TileShares sh = {a.share, a.over, a.least, a.last};
   Active active;
   bool spans = false;
-  if constexpr (A::SCORED) {
+  if constexpr (A::PLACED) {
     rows.node = min((tile0 + wr) * T_ROWS + n32, a.n * a.group - 1) / a.group;
     Spans mine;
     score_rows(rows, a, b, kvh, tile0 + wr, (int)a.nb * BLK + a.trail, lds.span[w], mine);
@@ -1221,7 +1331,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
     }
   }
   const auto tile_at = [&](int u) {
-    if constexpr (A::SCORED) return spans ? active.at(u) : u;
+    if constexpr (A::PLACED) return spans ? active.at(u) : u;
     return u;
   };
   const int even = a.nsplit - sh.last, mid = min(split, even);
@@ -1264,7 +1374,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
   }
   int fresh = 0, ring = 0;   // blocks whose widths have come into the half `ring`
   int ring_from = from;      // ... from this tile on
-  uint32_t open = 0u;        // SCORED: tokens of sealed blocks that the lane's row has attended
+  uint32_t open = 0u;        // PLACED: tokens of sealed blocks that the lane's row has attended
   int buf = 0;
   __syncthreads();
 
@@ -1332,7 +1442,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
         *reinterpret_cast<uint32_t*>(width_at(ring, ch >> 3, slot + blk) + (ch & 7) * 2) = out4.x | key_width(w2[0].y, w2[1].y) << 16;
       } else if constexpr (R == 2) {
         s_eta[turn & 3][blk] = value_error(an[qd]);   // (every lane the same)
-        if constexpr (A::SCORED)
+        if constexpr (A::PLACED)
           lds.nu[turn & 3][blk] = an[qd].y;
         else
           nu = fmaxf(nu, an[qd].y);
@@ -1371,6 +1481,12 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
   // the compiler, which cannot tell the tiles apart, each operand was read when it was needed: 3310 cycles a phase.)
   constexpr int PRODUCTS = 16 * MT, AHEAD = 6, FROM = 2, EACH = QUADS == 2 ? 4 : 2, BEHIND = FROM + PIECES * QUADS / EACH;
   static_assert(PIECES * QUADS % EACH == 0 && BEHIND < PRODUCTS, "the pieces end ahead of the products");
+  // Products with keys: the accumulators take turns; where caps are applied, the first 32 tokens' come first, and their caps stand between the others',
+  // CAPS scores a product.
+  constexpr bool EARLY = A::SCORED && MT == 2;
+  constexpr int CAPS = 3, CAPS_FROM = PRODUCTS - 6;
+  const auto key_mt = [](int k) constexpr { return EARLY ? k / 8 : k % MT; };
+  const auto key_ks = [](int k) constexpr { return EARLY ? k % 8 : k / MT; };
   const auto sealed_tiles = [&](auto keys) {
     for (int turn = 0; u < units; ++u, buf ^= 1, ++turn) {
       const bool last = u + 1 >= units, full = fresh == 32;
@@ -1384,7 +1500,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
         if constexpr (K < 0)
           f[I % AHEAD] = value_of(s_v, (wt * MT + I / 8) * 2 + half, (I & 7) >> 2, I & 3);
         else
-          f[I % AHEAD] = key_of(s_k, wt * MT + K % MT, K / MT);
+          f[I % AHEAD] = key_of(s_k, wt * MT + key_mt(K), key_ks(K));
       };
       const auto product = [&](auto i_) {
         constexpr int I = i_.value, K = I - 8 * MT;
@@ -1392,10 +1508,11 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
           const uint32_t* const x = &p[I / 8][(I & 4)];
           rows.o[I & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[I % AHEAD], __builtin_bit_cast(f16x8, make_uint4(x[0], x[1], x[2], x[3])), rows.o[I & 3], 0, 0, 0);
         } else {
-          if constexpr (K < MT)
+          constexpr int mt = key_mt(K), ks = key_ks(K);
+          if constexpr (ks == 0)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sc[K][r] = 0.0f;
-          sc[K % MT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[I % AHEAD], rows.q[K / MT], sc[K % MT], 0, 0, 0);
+            for (int r = 0; r < 16; ++r) sc[mt][r] = 0.0f;
+          sc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[I % AHEAD], rows.q[ks], sc[mt], 0, 0, 0);
         }
       };
       __builtin_amdgcn_s_setprio(1);
@@ -1419,6 +1536,14 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
               reconstruct(keys, std::integral_constant<int, QD>{}, std::integral_constant<int, J>{}, keys.value ? buf ^ 1 : buf, ring1, slot, turn + 1);
             }
           });
+        if constexpr (EARLY) {
+          if constexpr (I >= CAPS_FROM)
+            if (a.cap_kind == CAP_LOW) {
+              constexpr int R = (I - CAPS_FROM) * CAPS;
+#pragma unroll
+              for (int r = R; r < R + CAPS && r < 16; ++r) sc[0][r] = cap_low(a, sc[0][r]);
+            }
+        }
         if constexpr (I == BEHIND) load(keys.value ? u + 2 : u + 1);
         __builtin_amdgcn_sched_barrier(0);
       });
@@ -1438,7 +1563,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
       fresh = slot + BLKS;
       __builtin_amdgcn_s_setprio(0);
       turn_over();
-      if constexpr (A::SCORED) {
+      if constexpr (A::PLACED) {
         const int tile = tile_at(u);
         uint32_t there[MT];
         bool masked = (int64_t)(tile + 1) * BLKS > a.nb;
@@ -1450,13 +1575,16 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
           if (blk >= a.nb) there[mt] = 0u;
           open |= there[mt];
           rows.vmax = fmaxf(rows.vmax, there[mt] == 0u ? 0.0f : lds.nu[turn & 3][in]);
-          score16(a, rows, sc[mt], BlockFar(rows, blk * BLK));
+          score<16>(a, rows, sc[mt], RunFar<BLK>(rows, blk * BLK), EARLY && mt == 0);
         }
         masked |= some;
-        softmax32<MT>(
+        weigh32<MT>(
             a, rows, sc, p, masked, [&](int mt) { return there[mt]; }, [&](int mt) { return s_eta[turn & 3][(wt * MT + mt) * 2 + half]; });
       } else {
-        softmax32<MT>(
+        if constexpr (A::SCORED)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) score<16>(a, rows, sc[mt], [](int) { return 0.0f; }, EARLY && mt == 0);
+        weigh32<MT>(
             a, rows, sc, p, (int64_t)(u + 1) * BLKS > a.nb, [&](int mt) { return (int64_t)u * BLKS + (wt * MT + mt) * 2 + half < a.nb ? 0xffffu : 0u; },
             [&](int mt) { return s_eta[turn & 3][(wt * MT + mt) * 2 + half]; });
       }
@@ -1485,8 +1613,9 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
     }
     add_values(buf ^ 1);
   }
+  if constexpr (A::PLACED) drop_idle(rows, open);
   rows.sealed = rows.sum;
-  if constexpr (!A::SCORED) open = fresh != 0 && (S::WT == 1 || (int64_t)from * BLKS + wt * MT * 2 < a.nb);   // it has had tiles, and the wave a block of the first
+  if constexpr (!A::PLACED) open = fresh != 0 && (S::WT == 1 || (int64_t)from * BLKS + wt * MT * 2 < a.nb);   // it has had tiles, and the wave a block of the first
   // the other tokens' tiles: dealt to the workgroups from the last one down
   for (int t0 = (a.nsplit - 1 - split) * TOK; t0 < a.trail + a.drafts(); t0 += a.nsplit * TOK, buf ^= 1) {
     uint4* const s_k = reinterpret_cast<uint4*>(s_main + buf * S::TILE);
@@ -1496,11 +1625,11 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
     for (int mt = 0; mt < MT; ++mt) {
       const int at = t0 + ((wt * MT + mt) * 2 + half) * BLK;
       bits[mt] = open_tokens(a, b, rows.node, at);
-      if constexpr (A::SCORED)
+      if constexpr (A::PLACED)
         if (spans) bits[mt] &= span_bits(lds.span[w][n32], (int)a.nb * BLK + at) | ~trailing_bits(a, at);
     }
     __syncthreads();   // norms and bad tokens of the last tile are done with
-    if constexpr (A::SCORED)
+    if constexpr (A::PLACED)
       if (a.slopes != nullptr && tid < TOK) lds.place[tid] = exact_place(a, b, t0 + tid);
     if (tid < TOK) s_bad[tid] = 0;
     __syncthreads();
@@ -1512,11 +1641,11 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
       open |= bits[mt];
       open_exact(rows, bits[mt], s_norm + blk * BLK, s_bad + blk * BLK);
       attend32(
-          a, rows, bits[mt], A::SCORED ? lds.place + blk * BLK : nullptr, [&](int ks) { return key_of(s_k, unit, ks); }, [&](int oct, int ct) { return value_of(s_v, blk, oct, ct); });
+          a, rows, bits[mt], A::PLACED ? lds.place + blk * BLK : nullptr, [&](int ks) { return key_of(s_k, unit, ks); }, [&](int oct, int ct) { return value_of(s_v, blk, oct, ct); });
     }
   }
   __syncthreads();
-  if constexpr (!A::SCORED) {
+  if constexpr (!A::PLACED) {
     if (w < 4 && l == 0) s_norm[w] = nu;
     __syncthreads();
     rows.vmax = fmaxf(rows.vmax, fmaxf(fmaxf(s_norm[0], s_norm[1]), fmaxf(s_norm[2], s_norm[3])));
@@ -1551,7 +1680,7 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(A a) {
   __shared__ float s_eta[4][S::BLKS];
   __shared__ __align__(16) float s_norm[S::TOK];
   __shared__ __align__(16) uint8_t s_bad[S::TOK];
-  if constexpr (A::SCORED) {
+  if constexpr (A::PLACED) {
     __shared__ float s_nu[4][S::BLKS];
     __shared__ __align__(16) int s_place[S::TOK];
     __shared__ __align__(16) Spans s_span[8][T_ROWS];
