@@ -27,6 +27,11 @@ constexpr int L_EXACT = 64;                                            // traili
 constexpr int L_Q = L_ROWS * Q_ROW;
 static_assert(L_META_END <= L_SET * 4 && 2 * L_EXACT * D * 2 <= 4 * L_SET * 4 && L_VM % 16 == 0 && L_W % 16 == 0, "a wave's part of LDS, of four waves'");
 
+// Pairs by workgroup: a turn of the trailing and drafted tokens takes as long as two of the sealed ones.
+__host__ __device__ inline TileShares light_shares(int pairs, int others, int nsplit, int waves) {
+  return tile_shares(pairs, (others + L_EXACT - 1) / L_EXACT, nsplit, 2 * waves);
+}
+
 struct LightRows {
   f16x8 q[4];      // channels (i >> 1) 64 + g 16 + (i & 1) 8 + 0 .. 7
   f32x4 o[8];      // channels ct 16 + g 4 + 0 .. 3
@@ -51,9 +56,9 @@ __device__ __forceinline__ float sum_over_groups(float x) { return sum_x32(sum_x
 
 // Scores of a lane's eight tokens, of its octet, to weights; p: the B operand.  bits, where masked: those its row attends.
 template <typename A, typename Rows>
-__device__ __forceinline__ void softmax8(const A& a, Rows& w, f32x8 (&s)[1], uint32_t (&p)[1][4], bool masked, uint32_t bits, float eta) {
+__device__ __forceinline__ void softmax8(const A& a, Rows& w, f32x8 (&s)[1], uint32_t (&p)[1][4], bool masked, uint32_t bits, float eta, bool silent = false) {
   // (the block's other octet is 16 lanes away)
-  softmax_sets<1, 8>(a, w, s, p, masked, [&](int) { return bits; }, [&](int) { return eta; }, [](float x) { return max_over_groups(x); }, [](float x) { return sum_x16(x); });
+  softmax_sets<1, 8>(a, w, s, p, masked, [&](int) { return bits; }, [&](int) { return eta; }, [](float x) { return max_over_groups(x); }, [](float x) { return sum_x16(x); }, silent);
 }
 __device__ __forceinline__ f32x8 both(f32x4 x, f32x4 y) { return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7); }
 __device__ __forceinline__ f32x4 product16(uint4 x, f16x8 y, f32x4 z) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), y, z, 0, 0, 0); }
@@ -160,6 +165,9 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
   std::conditional_t<A::SCORED, Scored<LightRows>, LightRows> rows;
   const int last_row = a.n * a.group - 1;
   rows.node = min(n16, last_row) / a.group;
+  // rows 4 w .. 4 w + 3 of the queries by each of four waves: 16 lanes a row
+  const int q_row = min(4 * (w & 3) + g, last_row), q_node = q_row / a.group;
+  const uint4 q_in = ld16_any(a.q + (((int64_t)b * a.n + q_node) * a.n_kv * a.group + kvh * a.group + (q_row - q_node * a.group)) * D + n16 * 8);
 
   const uint8_t* const base = a.t1 + head * a.nq_cap * QUAD_BYTES;
   int units = (int)((a.nb + 1) >> 1);                       // pairs of sealed blocks
@@ -177,7 +185,7 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
       const Spans mine = node_spans(a, node, a.first, (int)a.nb * BLK + a.trail);
       rows.idle = mine.hi0 == 0 && mine.hi1 == 0;
       if (l < L_ROWS) lds.span[l] = mine;                   // (every wave the same)
-      active = active_units(hull_of(mine), (int)a.nb * BLK, 2 * BLK);
+      active = active_units(hull_of<L_ROWS>(mine), (int)a.nb * BLK, 2 * BLK);
       units = active.units;
     }
   }
@@ -185,7 +193,11 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
     if constexpr (A::PLACED) return spans ? active.at(u) : u;
     return u;
   };
-  const int step = WAVES * a.nsplit;
+  // the workgroup's pairs: from .. units - 1
+  const TileShares sh = spans ? light_shares(units, a.trail + a.drafts(), a.nsplit, WAVES) : TileShares{a.share, a.over, a.least, a.last};
+  const int even = a.nsplit - sh.last, mid = min(split, even);
+  const int from = mid * sh.share + min(mid, sh.over) + (split - mid) * sh.least;
+  units = from + (split < even ? sh.share + (split < sh.over) : sh.least);
   const int kb = n16 >> 3, tok = ((n16 >> 2) & 1) * 8 + (n16 & 3);   // the keys' block of the pair, and the first tile's token of it
   const int vb = g >> 1;                                             // the octet's block
   uint4 k00, k01, k10, k11, km0, km1, vc0, vc1, vm;                  // keys (tile, half of the channels)
@@ -209,16 +221,11 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
     vc0 = *reinterpret_cast<const uint4*>(p);
     vc1 = *reinterpret_cast<const uint4*>(p + 256);
   };
-  int u = split * WAVES + w;
-  {
-    // rows 4 w .. 4 w + 3 of the queries by each of four waves: 16 lanes a row
-    const int r = min(4 * (w & 3) + g, last_row), node = r / a.group;
-    const uint4 x = ld16_any(a.q + (((int64_t)b * a.n + node) * a.n_kv * a.group + kvh * a.group + (r - node * a.group)) * D + n16 * 8);
-    load_meta(u);
-    load_keys(u);
-    load_values(u);
-    *reinterpret_cast<uint4*>(lds.q + (4 * (w & 3) + g) * Q_ROW + n16 * 16) = x;   // (the others the same)
-  }
+  int u = from + w;
+  load_meta(u);
+  load_keys(u);
+  load_values(u);
+  *reinterpret_cast<uint4*>(lds.q + (4 * (w & 3) + g) * Q_ROW + n16 * 16) = q_in;   // (of each four waves the same)
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 4; ++i) rows.q[i] = *reinterpret_cast<const f16x8*>(lds.q + n16 * Q_ROW + (i >> 1) * 128 + g * 32 + (i & 1) * 16);
@@ -236,18 +243,24 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
       bad |= !(finite2(x.x) & finite2(x.y) & finite2(x.z) & finite2(x.w));
     }
     rows.undefined = max_over_groups(bad ? 1.0f : 0.0f) != 0.0f;
+    zero_undefined(rows, rows.q);
   }
 
   uint32_t open = 0u;   // what the lane's row has attended
-  for (int turn = 0; u < units; u += step, ++turn) {
+  for (int turn = 0; u < units; u += WAVES, ++turn) {
     const int pair = pair_at(u);
     uint32_t there = (int64_t)pair * 2 + vb < a.nb ? 0xffu : 0u;
+    bool silent = false;
     bool masked = (int64_t)pair * 2 + 2 > a.nb;
     if constexpr (A::PLACED)
       if (spans && !active.open(pair * 2 * BLK, (pair + 1) * 2 * BLK)) {
         masked = true;
         there &= span_bits(lds.span[n16], (pair * 4 + g) * 8);
       }
+    if constexpr (A::PLACED) {
+      silent = rows.idle;
+      there = silent ? 0u : there;
+    }
     open |= there;
     // metadata
     reinterpret_cast<uint4*>(wave + L_KM)[l] = km0;
@@ -255,7 +268,7 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
     *reinterpret_cast<uint4*>(wave + L_VM + (l >> 5) * L_VM_BLK + (l & 31) * 16) = paired(vm);
     const float eta = value_error(an);
     rows.vmax = fmaxf(rows.vmax, A::PLACED && there == 0u ? 0.0f : an.y);
-    load_meta(u + step);
+    load_meta(u + WAVES);
     wave_sync();
     // widths: four channels a lane
     {
@@ -276,10 +289,10 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
       x0 = product16(i & 1 ? keys8(c0.z, c0.w, s0, s1, z0, z1) : keys8(c0.x, c0.y, s0, s1, z0, z1), rows.q[i], x0);
       x1 = product16(i & 1 ? keys8(c1.z, c1.w, s0, s1, z0, z1) : keys8(c1.x, c1.y, s0, s1, z0, z1), rows.q[i], x1);
     });
-    load_keys(u + step);
-    if ((turn & 7) == 7 || u + step >= units) {
+    load_keys(u + WAVES);
+    if ((turn & 7) == 7 || u + WAVES >= units) {
       wave_sync();
-      const int last = (turn & 7) * 2 + 1, slot = min(n16, last), first = u - (turn & 7) * step;
+      const int last = (turn & 7) * 2 + 1, slot = min(n16, last), first = u - (turn & 7) * WAVES;
       f32x4 d = {0.0f, 0.0f, 0.0f, 0.0f};
       uint32_t no_signs = 0x7fff7fffu;
       asm volatile("" : "+s"(no_signs));   // |q| is formed here, not kept
@@ -294,7 +307,7 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
         const int s = min(g * 4 + r, last);
         bool some = true;
         if constexpr (A::PLACED)
-          if (spans) some = span_bits(lds.span[n16], (pair_at(first + (s >> 1) * step) * 2 + (s & 1)) * BLK) != 0u;
+          if (spans) some = span_bits(lds.span[n16], (pair_at(first + (s >> 1) * WAVES) * 2 + (s & 1)) * BLK) != 0u;
         if (some) rows.dmax = fmaxf(rows.dmax, d[r]);
       }
       wave_sync();
@@ -302,7 +315,7 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
     f32x8 s[1] = {both(x0, x1)};
     uint32_t p[1][4];
     if constexpr (A::SCORED) score<8>(a, rows, s[0], RunFar<8>(rows, (pair * 4 + g) * 8));
-    softmax8(a, rows, s, p, masked, there, eta);
+    softmax8(a, rows, s, p, masked, there, eta, silent);
     const f16x8 weights = __builtin_bit_cast(f16x8, make_uint4(p[0][0], p[0][1], p[0][2], p[0][3]));
     const uint8_t* const sc = wave + L_VM + vb * L_VM_BLK + (g & 1) * 128;
     each<8>([&](auto i_) {
@@ -311,13 +324,12 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
       const uint32_t c = (ct & 3) == 0 ? v.x : ((ct & 3) == 1 ? v.y : ((ct & 3) == 2 ? v.z : v.w));
       rows.o[ct] = product16(values8(c, *reinterpret_cast<const uint4*>(sc + ct * 16), *reinterpret_cast<const uint4*>(sc + 256 + ct * 16)), weights, rows.o[ct]);
     });
-    load_values(u + step);
+    load_values(u + WAVES);
     wave_sync();
   }
-  if constexpr (A::PLACED) drop_idle(rows, open);
   rows.sealed = rows.sum;
-  // The other tokens, dealt from the workgroup on whose turn is the next, 32 to a wave.
-  for (int t0 = (split + a.nsplit - (units + WAVES - 1) / WAVES % a.nsplit) % a.nsplit * L_EXACT; t0 < a.trail + a.drafts(); t0 += a.nsplit * L_EXACT) {
+  // The other tokens, 32 to a wave: dealt to the workgroups from the last one down.
+  for (int t0 = (a.nsplit - 1 - split) * L_EXACT; t0 < a.trail + a.drafts(); t0 += a.nsplit * L_EXACT) {
     uint4* const s_k = reinterpret_cast<uint4*>(lds.set);
     uint4* const s_v = s_k + 16 * L_EXACT;
     const int at = t0 + w * 32 + g * 8;   // the lane's octet

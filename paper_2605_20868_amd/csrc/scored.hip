@@ -52,7 +52,7 @@ static int light_splits(int n_cu, int64_t heads, int waves, int64_t sealed, int6
 static Shape shape_of(int n_cu, int64_t heads, int n_rows, int64_t sealed, int64_t others) {
   if (n_rows <= L_ROWS) {
     const int most = light_splits(n_cu, heads, 12, 1 << 30, 0);
-    const int waves = (sealed + 383) / 384 >= 3 * most ? 12 : 4;
+    const int waves = heads <= n_cu && (sealed + 383) / 384 >= 3 * most ? 12 : 4;
     return {waves == 4 ? L_ROWS : L_ROWS + 1, light_splits(n_cu, heads, waves, sealed, others)};
   }
   const int rows = tree_rows(n_cu, heads, n_rows, sealed, others);
@@ -99,7 +99,12 @@ static int put_pass(SetArgs<SCORES>& a, const Cache* c, int layer, int nodes, in
   a.row_tiles = (n_rows + 31) / 32;
   const Shape x = shape_of(c->n_cu, heads, n_rows, a.nb * BLK, others);
   a.nsplit = x.nsplit;
-  if (x.rows > 32) put_shares(a, x.rows, others);
+  if (x.rows > 32) {
+    put_shares(a, x.rows, others);
+  } else if (x.rows <= L_ROWS + 1) {
+    const TileShares s = light_shares((int)((a.nb + 1) / 2), others, a.nsplit, x.rows == L_ROWS ? 4 : 12);
+    a.share = s.share, a.over = s.over, a.least = s.least, a.last = s.last;
+  }
   return x.rows;
 }
 

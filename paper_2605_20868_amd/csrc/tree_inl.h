@@ -324,6 +324,22 @@ struct Active {
 struct Hull {
   int lo[2], hi[2], in_lo[2], in_hi[2];   // of the spans, what they cover and what is in all of them
 };
+// f over ROWS lanes, 16 or 32, of which the others have the same.
+template <int ROWS, typename F>
+__device__ __forceinline__ int row_extreme(int x, F f) {
+  x = f(x, dpp_movi<0xB1>(x));
+  x = f(x, dpp_movi<0x4E>(x));
+  x = f(x, dpp_movi<0x141>(x));
+  x = f(x, dpp_movi<0x140>(x));
+  if constexpr (ROWS == 32) {
+    uint32_t even, odd;
+    swap16((uint32_t)x, even, odd);
+    x = f((int)even, (int)odd);
+  }
+  return x;
+}
+// of a wave's rows
+template <int ROWS>
 __device__ __forceinline__ Hull hull_of(const Spans& s) {
   constexpr int NONE = 0x7fffffff;
   Hull h;
@@ -332,15 +348,12 @@ __device__ __forceinline__ Hull hull_of(const Spans& s) {
   for (int i = 0; i < 2; ++i) {
     h.lo[i] = lo[i] < hi[i] ? lo[i] : NONE, h.hi[i] = lo[i] < hi[i] ? hi[i] : -1;
     h.in_lo[i] = lo[i], h.in_hi[i] = hi[i];
-    if (s.hi0 == 0 && s.hi1 == 0) h.in_lo[i] = 0, h.in_hi[i] = NONE;   // (an idle row: drop_idle)
+    if (s.hi0 == 0 && s.hi1 == 0) h.in_lo[i] = 0, h.in_hi[i] = NONE;   // (an idle row is silent)
   }
+  const auto least = [](int x) { return row_extreme<ROWS>(x, [](int y, int z) { return min(y, z); }); };
+  const auto most = [](int x) { return row_extreme<ROWS>(x, [](int y, int z) { return max(y, z); }); };
 #pragma unroll
-  for (int k = 1; k < 64; k *= 2)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      h.lo[i] = min(h.lo[i], __shfl_xor(h.lo[i], k)), h.hi[i] = max(h.hi[i], __shfl_xor(h.hi[i], k));
-      h.in_lo[i] = max(h.in_lo[i], __shfl_xor(h.in_lo[i], k)), h.in_hi[i] = min(h.in_hi[i], __shfl_xor(h.in_hi[i], k));
-    }
+  for (int i = 0; i < 2; ++i) h.lo[i] = least(h.lo[i]), h.hi[i] = most(h.hi[i]), h.in_lo[i] = most(h.in_lo[i]), h.in_hi[i] = least(h.in_hi[i]);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     h.lo[i] = __builtin_amdgcn_readfirstlane(h.lo[i]), h.hi[i] = __builtin_amdgcn_readfirstlane(h.hi[i]);
@@ -381,6 +394,19 @@ __device__ __forceinline__ void keep_rows(uint8_t* at, int row, uint4 x) {
   const int l = threadIdx.x & 63;
   *reinterpret_cast<uint4*>(at + (row + (l >> 4)) * Q_ROW + (l & 15) * 16) = x;
 }
+// A query or a slope that is not finite (a slope of more than 10^28 with it, for distances are numbers too): zeros, which nothing passes on; the row's
+// sum is no number at the end.
+template <typename Rows, int N>
+__device__ __forceinline__ void zero_undefined(Rows& w, f16x8 (&q)[N]) {
+  const bool steep = !(fabsf(w.slope) <= 1e28f);
+  w.undefined |= steep;
+  w.slope = steep ? 0.0f : w.slope;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint4 x = __builtin_bit_cast(uint4, q[i]);
+    q[i] = __builtin_bit_cast(f16x8, w.undefined ? make_uint4(0u, 0u, 0u, 0u) : x);
+  }
+}
 template <typename A>
 __device__ __forceinline__ void start_rows(RowsOf<A>& s, const A& a, int tile, const uint8_t* at) {
   const int l = threadIdx.x & 63;
@@ -400,7 +426,8 @@ __device__ __forceinline__ void start_rows(RowsOf<A>& s, const A& a, int tile, c
       const uint4 x = __builtin_bit_cast(uint4, s.q[ks]);
       bad |= !(finite2(x.x) & finite2(x.y) & finite2(x.z) & finite2(x.w));
     }
-    s.undefined = __shfl_xor((int)bad, 32) != 0 || bad;
+    s.undefined = max_x32(bad ? 1.0f : 0.0f) != 0.0f;
+    zero_undefined(s, s.q);
   }
 }
 // The bias and the spans of a wave's rows, of sequence or beginning b; sealed and trailing tokens: count.  The spans go to LDS, a row's 16 bytes.
@@ -493,8 +520,10 @@ __device__ __forceinline__ void softmax32(const A& a, TreeRows& w, f32x16 (&s)[M
 // The same in passes of SetArgs, for MT times N scores of a lane.  With a cap, which bounds them, a row's m is its largest score's exponent of 2, upwards, a
 // whole number: a weight's exponent is one multiply-add, and sets of different m join exactly.  largest(x): over the lanes of a row; block(x): the sum
 // over a block.
+// silent: a lane's row has no part in it (one that attends no cached token, among others whose tokens are not looked at one by one).
 template <int MT, int N, typename A, typename Rows, typename V, typename Bits, typename Eta, typename Largest, typename Block>
-__device__ __forceinline__ void softmax_sets(const A& a, Rows& w, V (&s)[MT], uint32_t (&p)[MT][N / 2], bool masked, Bits bits, Eta eta, Largest largest, Block block) {
+__device__ __forceinline__ void softmax_sets(const A& a, Rows& w, V (&s)[MT], uint32_t (&p)[MT][N / 2], bool masked, Bits bits, Eta eta, Largest largest, Block block,
+                                             bool silent = false) {
   if (masked) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -510,6 +539,7 @@ __device__ __forceinline__ void softmax_sets(const A& a, Rows& w, V (&s)[MT], ui
     for (int r = 0; r < N; ++r) top = fmaxf(top, s[mt][r]);
   top = largest(top);
   top = a.capped() ? ceilf(top * a.unit()) : top;
+  if constexpr (A::PLACED) top = silent ? -INFINITY : top;
   if (__any(top > w.m)) {
     const float mn = fmaxf(w.m, top);
     const float f = set_weight(a, w.m, mn);
@@ -521,7 +551,8 @@ __device__ __forceinline__ void softmax_sets(const A& a, Rows& w, V (&s)[MT], ui
     w.each_sum([&](float o) { return o * f; });
   }
   const float m = w.m == -INFINITY ? 0.0f : w.m;   // nothing attended yet: every weight is exp2(-inf) = 0
-  const float most = a.capped() ? MOST - m : MOST;
+  float most = a.capped() ? MOST - m : MOST;
+  if constexpr (A::PLACED) most = silent ? -INFINITY : most;
   if (!a.capped())
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
@@ -545,22 +576,16 @@ __device__ __forceinline__ void softmax_sets(const A& a, Rows& w, V (&s)[MT], ui
 }
 // ... of 32 rows
 template <int MT, typename A, typename Rows, typename Bits, typename Eta>
-__device__ __forceinline__ void weigh32(const A& a, Rows& w, f32x16 (&s)[MT], uint32_t (&p)[MT][8], bool masked, Bits bits, Eta eta) {
+__device__ __forceinline__ void weigh32(const A& a, Rows& w, f32x16 (&s)[MT], uint32_t (&p)[MT][8], bool masked, Bits bits, Eta eta, bool silent = false) {
   if constexpr (A::SETS)
-    softmax_sets<MT, 16>(a, w, s, p, masked, bits, eta, [](float x) { return max_x32(x); }, [](float x) { return x; });
+    softmax_sets<MT, 16>(a, w, s, p, masked, bits, eta, [](float x) { return max_x32(x); }, [](float x) { return x; }, silent);
   else
     softmax32<MT>(a, w, s, p, masked, bits, eta);
 }
-// What an idle row has had with the others, whose tokens are not looked at one by one where they are all the others', is dropped.
 template <typename Rows>
-__device__ __forceinline__ void drop_idle(Rows& w, uint32_t& open) {
-  if (!__any(w.idle)) return;
-  if (w.idle) {
-    w.m = -INFINITY;
-    w.sum = w.sealed = w.ev = w.evmax = w.dmax = w.vmax = 0.0f;
-    open = 0u;
-    w.each_sum([](float) { return 0.0f; });
-  }
+__device__ __forceinline__ bool silent_of(const Rows& w) {
+  if constexpr (std::is_base_of_v<Scored<SetRows>, Rows>) return w.idle;
+  return false;
 }
 // All of it, of exact tokens.
 template <typename A, typename Key, typename Value>
@@ -1041,7 +1066,7 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
     score_rows(rows, a, b, kvh, tile, (int)a.nb * BLK + a.trail, lds.span, mine);   // (every wave the same)
     spans = a.spans != nullptr;
     if (spans) {
-      active = active_units(hull_of(mine), (int)a.nb * BLK, 2 * BLK);
+      active = active_units(hull_of<T_ROWS>(mine), (int)a.nb * BLK, 2 * BLK);
       units = active.units;
     }
   }
@@ -1097,7 +1122,7 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
         masked = true;
         there = span_bits(lds.span[n32], (pair * 2 + half) * BLK);
       }
-      if ((int64_t)pair * 2 + half >= a.nb) there = 0u;
+      if ((int64_t)pair * 2 + half >= a.nb || rows.idle) there = 0u;
       open |= there;
     }
     // metadata: sigma and z by (block, kind, half of the channels), scales and offsets by block
@@ -1162,7 +1187,7 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
     }
     if constexpr (A::SCORED) score<16>(a, rows, x[0], RunFar<BLK>(rows, (pair * 2 + half) * BLK));
     weigh32<1>(
-        a, rows, x, p, masked, [&](int) { return A::PLACED ? there : ((int64_t)u * 2 + half < a.nb ? 0xffffu : 0u); }, [&](int) { return eta; });
+        a, rows, x, p, masked, [&](int) { return A::PLACED ? there : ((int64_t)u * 2 + half < a.nb ? 0xffffu : 0u); }, [&](int) { return eta; }, silent_of(rows));
     each<8>([&](auto i_) {
       constexpr int I = i_.value, ct = I & 3, oct = I >> 2;
       __builtin_amdgcn_sched_barrier(0);
@@ -1177,7 +1202,6 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
     load_values(u + step);
     wave_sync();
   }
-  if constexpr (A::PLACED) drop_idle(rows, open);
   rows.sealed = rows.sum;
   if constexpr (!A::PLACED) open = split * FEW_WAVES + w < units;
   // The other tokens, dealt from the workgroup on whose turn is the next, which fetches them together; as many of its waves as they have pairs of blocks attend them.
@@ -1262,10 +1286,10 @@ struct TileShares {
 constexpr int EXACT_TILES = 3;
 // Tiles by workgroup: the trailing and drafted tokens' tiles are the last workgroups', EXACT_TILES tiles' work each, and the sealed ones are dealt so
 // that all end together.
-__host__ __device__ inline TileShares tile_shares(int tiles, int exact, int nsplit) {
+__host__ __device__ inline TileShares tile_shares(int tiles, int exact, int nsplit, int exact_tiles = EXACT_TILES) {
   TileShares x;
   x.last = exact < nsplit ? exact : 0;
-  x.least = (tiles + EXACT_TILES * exact) / nsplit - EXACT_TILES;
+  x.least = (tiles + exact_tiles * exact) / nsplit - exact_tiles;
   if (x.least < 0) x.least = 0;
   const int rest = tiles - x.last * x.least, even = nsplit - x.last;
   x.share = rest / even;
@@ -1314,7 +1338,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
     spans = a.spans != nullptr;
     if (spans) {
       // the hull of the workgroup's rows, and what is open to all of the wave's
-      Hull h = hull_of(mine);
+      Hull h = hull_of<T_ROWS>(mine);
       int* const s_hull = reinterpret_cast<int*>(s_main);
       if (l < 4) s_hull[w * 4 + l] = l == 0 ? h.lo[0] : l == 1 ? h.hi[0] : l == 2 ? h.lo[1] : h.hi[1];
       __syncthreads();
@@ -1572,14 +1596,14 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
         for (int mt = 0; mt < MT; ++mt) {
           const int in = (wt * MT + mt) * 2 + half, blk = tile * BLKS + in;
           there[mt] = some ? span_bits(lds.span[w][n32], blk * BLK) : 0xffffu;
-          if (blk >= a.nb) there[mt] = 0u;
+          if (blk >= a.nb || rows.idle) there[mt] = 0u;
           open |= there[mt];
           rows.vmax = fmaxf(rows.vmax, there[mt] == 0u ? 0.0f : lds.nu[turn & 3][in]);
           score<16>(a, rows, sc[mt], RunFar<BLK>(rows, blk * BLK), EARLY && mt == 0);
         }
         masked |= some;
         weigh32<MT>(
-            a, rows, sc, p, masked, [&](int mt) { return there[mt]; }, [&](int mt) { return s_eta[turn & 3][(wt * MT + mt) * 2 + half]; });
+            a, rows, sc, p, masked, [&](int mt) { return there[mt]; }, [&](int mt) { return s_eta[turn & 3][(wt * MT + mt) * 2 + half]; }, rows.idle);
       } else {
         if constexpr (A::SCORED)
 #pragma unroll
@@ -1613,7 +1637,6 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
     }
     add_values(buf ^ 1);
   }
-  if constexpr (A::PLACED) drop_idle(rows, open);
   rows.sealed = rows.sum;
   if constexpr (!A::PLACED) open = fresh != 0 && (S::WT == 1 || (int64_t)from * BLKS + wt * MT * 2 < a.nb);   // it has had tiles, and the wave a block of the first
   // the other tokens' tiles: dealt to the workgroups from the last one down
