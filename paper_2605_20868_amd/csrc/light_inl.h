@@ -388,16 +388,37 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
   end_light<WAVES>(a, lds.set, (int)head, split, tid);
 }
 
-template <int WAVES, typename A>
-__global__ __launch_bounds__(64 * WAVES, 3) void tree_light_kernel(A a) {
-  fetch_args<sizeof(A)>();
+template <int WAVES, typename F>
+__device__ __forceinline__ void with_light_lds(F f) {
   __shared__ __align__(16) float s_set[WAVES][L_SET];
   __shared__ __align__(16) uint8_t s_q[L_Q];
   __shared__ __align__(16) float s_norm[L_EXACT];
   __shared__ __align__(16) uint8_t s_bad[L_EXACT];
   __shared__ __align__(16) int s_place[L_EXACT];
   __shared__ __align__(16) Spans s_span[L_ROWS];
-  attend_light<WAVES>(a, blockIdx.x, blockIdx.y, LightLds{s_set, s_q, s_norm, s_bad, s_place, s_span});
+  f(LightLds{s_set, s_q, s_norm, s_bad, s_place, s_span});
+}
+template <int WAVES, typename A>
+__global__ __launch_bounds__(64 * WAVES, 3) void tree_light_kernel(A a) {
+  fetch_args<sizeof(A)>();
+  with_light_lds<WAVES>([&](const LightLds& lds) { attend_light<WAVES>(a, blockIdx.x, blockIdx.y, lds); });
+}
+// Two passes in one launch, a's workgroups first.  (2 sequences behind 1029 tokens, 1 KV head: TWO_US.)
+template <typename A>
+struct TwoPasses {
+  A a, b;
+  int a_heads, a_groups, b_heads;   // KV groups, a's workgroups
+};
+template <int WAVES, typename A>
+__global__ __launch_bounds__(64 * WAVES, 3) void tree_light_two_kernel(TwoPasses<A> x) {
+  fetch_args<sizeof(TwoPasses<A>)>();
+  const int i = (int)blockIdx.x;
+  with_light_lds<WAVES>([&](const LightLds& lds) {
+    if (i < x.a_groups)
+      attend_light<WAVES>(x.a, i % x.a_heads, i / x.a_heads, lds);
+    else
+      attend_light<WAVES>(x.b, (i - x.a_groups) % x.b_heads, (i - x.a_groups) / x.b_heads, lds);
+  });
 }
 
 }  // namespace cqa

@@ -152,11 +152,21 @@ static int32_t run(const Cache* shared, const Cache* c, int layer, const NodeCal
   static_cast<SetArgs<SCORES>&>(j) = a;
   const int shared_rows = put_pass(static_cast<SetArgs<SCORES>&>(j), shared, layer, x.n * (c->desc.batch / shared->desc.batch), 0, 0, ws);
   j.row_sets = own;
-  if (const int32_t rc = launch_rows(static_cast<const SetArgs<SCORES>&>(j), shared_heads, shared_rows, j.trail, st)) return rc;
-  if (!own) return j.nsplit == 1 ? CQA_OK : launch_join(static_cast<const SetArgs<SCORES>&>(j), shared_heads, j.nsplit, c->n_cu, st);
+  const SetArgs<SCORES>& s = j;
+  if (!own) {
+    if (const int32_t rc = launch_rows(s, shared_heads, shared_rows, s.trail, st)) return rc;
+    return s.nsplit == 1 ? CQA_OK : launch_join(s, shared_heads, s.nsplit, c->n_cu, st);
+  }
   a.row_sets = 1;
-  const int rows = put_pass(a, c, layer, x.n, drafts, (int)beginning, ws + shared_heads * j.row_tiles * j.nsplit * T_FLOATS);
-  if (const int32_t rc = launch_rows(a, heads, rows, a.trail + drafts, st)) return rc;
+  const int rows = put_pass(a, c, layer, x.n, drafts, (int)beginning, ws + shared_heads * s.row_tiles * s.nsplit * T_FLOATS);
+  if (shared_rows == L_ROWS && rows == L_ROWS && shared_heads * s.nsplit + heads * a.nsplit <= 3 * (int64_t)c->n_cu) {
+    const TwoPasses<SetArgs<SCORES>> two = {s, a, (int)shared_heads, (int)shared_heads * s.nsplit, (int)heads};
+    tree_light_two_kernel<4><<<dim3((uint32_t)(two.a_groups + heads * a.nsplit)), 256, 0, st>>>(two);
+    CQA_HIP(hipGetLastError());
+  } else {
+    if (const int32_t rc = launch_rows(s, shared_heads, shared_rows, s.trail, st)) return rc;
+    if (const int32_t rc = launch_rows(a, heads, rows, a.trail + drafts, st)) return rc;
+  }
   j.own = a.part;
   j.own_tiles = a.row_tiles;
   j.own_sets = a.nsplit;
