@@ -403,7 +403,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void tree_light_kernel(A a) {
   fetch_args<sizeof(A)>();
   with_light_lds<WAVES>([&](const LightLds& lds) { attend_light<WAVES>(a, blockIdx.x, blockIdx.y, lds); });
 }
-// Two passes in one launch, a's workgroups first.  (2 sequences behind 1029 tokens, 1 KV head: TWO_US.)
+// Two passes in one launch, a's workgroups first. 
 template <typename A>
 struct TwoPasses {
   A a, b;

@@ -40,39 +40,35 @@ struct JoinArgs : SetArgs<SCORES> {
   }
 };
 
-static int row_count(const Cache* c, int64_t nodes) { return (int)(nodes * (c->desc.n_q_heads / c->desc.n_kv_heads)); }
-// Rows of a KV group a workgroup takes, and the partial sets of a row.
+// ---- what a call launches --------------------------------------------------------------------------------------------------------------
+
+// Rows of a KV group a workgroup takes, its waves, and the partial sets of a row.
 struct Shape {
-  int rows, nsplit;
+  int rows, waves, nsplit;
 };
 static int light_splits(int n_cu, int64_t heads, int waves, int64_t sealed, int64_t others) {
   const int64_t most = std::max<int64_t>(1, 12 / waves * (int64_t)n_cu / heads), tiles = (sealed + 32 * waves - 1) / (32 * waves);
   return (int)std::min(most, tiles <= 1 && others <= L_EXACT ? 1 : tiles + (others + L_EXACT - 1) / L_EXACT);
 }
+// Up to 16 rows go by the light kernel: twelve waves a workgroup, one of which a compute unit holds, where these have three turns and more, for there are
+// fewer sets to join; else four waves (us a call in a graph with twelve and with four: 8 heads, 131072 tokens 64.1, 67.8; 4 x 8 heads, windows of 4096 in
+// 32768 23.6, 24.4; 8 heads, 8000 tokens 14.4, 12.6; 64 x 8 heads, 1029 tokens 44.3, 33.6; 200 x 4 heads, 263 tokens 47.4, 26.1).  More rows: tree_rows.
 static Shape shape_of(int n_cu, int64_t heads, int n_rows, int64_t sealed, int64_t others) {
   if (n_rows <= L_ROWS) {
-    const int most = light_splits(n_cu, heads, 12, 1 << 30, 0);
-    const int waves = heads <= n_cu && (sealed + 383) / 384 >= 3 * most ? 12 : 4;
-    return {waves == 4 ? L_ROWS : L_ROWS + 1, light_splits(n_cu, heads, waves, sealed, others)};
+    const int waves = heads <= n_cu && (sealed + 383) / 384 >= 3 * (n_cu / heads) ? 12 : 4;
+    return {L_ROWS, waves, light_splits(n_cu, heads, waves, sealed, others)};
   }
   const int rows = tree_rows(n_cu, heads, n_rows, sealed, others);
-  return {rows, tree_splits(n_cu, heads, n_rows, rows, sealed, others)};
+  return {rows, 8, tree_splits(n_cu, heads, n_rows, rows, sealed, others)};
 }
-template <typename A>
-static int32_t launch_rows(const A& a, int64_t heads, int rows, int others, hipStream_t st) {
-  if (rows > L_ROWS + 1) return launch_pass(a, heads, rows, others, st);
-  if (rows == L_ROWS)
-    tree_light_kernel<4><<<dim3((uint32_t)heads, (uint32_t)a.nsplit), 256, 0, st>>>(a);
-  else
-    tree_light_kernel<12><<<dim3((uint32_t)heads, (uint32_t)a.nsplit), 768, 0, st>>>(a);
-  CQA_HIP(hipGetLastError());
-  return CQA_OK;
-}
+
+static int row_count(const Cache* c, int64_t nodes) { return (int)(nodes * (c->desc.n_q_heads / c->desc.n_kv_heads)); }
+static int64_t kv_groups(const Cache* c) { return (int64_t)c->desc.batch * c->desc.n_kv_heads; }
 static int64_t set_floats(const Cache* c, int64_t nodes, int64_t others) {
-  const int64_t heads = (int64_t)c->desc.batch * c->desc.n_kv_heads;
+  const int64_t heads = kv_groups(c);
   const int n_rows = row_count(c, nodes);
-  const auto most = [&](int rows) { return (int64_t)tree_splits(c->n_cu, heads, n_rows, rows, c->desc.max_tokens, others); };
   if (n_rows <= L_ROWS) return heads * light_splits(c->n_cu, heads, 4, c->desc.max_tokens, others) * T_FLOATS;
+  const auto most = [&](int rows) { return (int64_t)tree_splits(c->n_cu, heads, n_rows, rows, c->desc.max_tokens, others); };
   return heads * ((n_rows + 31) / 32) * std::max(most(32), most(n_rows <= 64 ? 64 : (n_rows <= 128 ? 128 : 256))) * T_FLOATS;
 }
 int64_t scored_ws_bytes(const Cache* shared, const Cache* c, int n) {
@@ -81,10 +77,16 @@ int64_t scored_ws_bytes(const Cache* shared, const Cache* c, int n) {
   return floats * 4;
 }
 
-// What the pass over c's tokens takes, of `nodes` nodes of each of its sequences.  others: drafted tokens.
+// The pass over c's tokens of `nodes` nodes of each of its sequences.
+struct Pass {
+  int64_t heads;
+  Shape shape;
+  int others;      // trailing and drafted tokens
+  int64_t floats;  // of its sets
+};
 template <Scores SCORES>
-static int put_pass(SetArgs<SCORES>& a, const Cache* c, int layer, int nodes, int drafts, int first, float* part) {
-  const int64_t head0 = head_index(c, layer, 0, 0), heads = (int64_t)c->desc.batch * c->desc.n_kv_heads;
+static Pass put_pass(SetArgs<SCORES>& a, const Cache* c, int layer, int nodes, int drafts, int first) {
+  const int64_t head0 = head_index(c, layer, 0, 0);
   a.t1 = c->t1 + head0 * c->nq_cap * QUAD_BYTES;
   a.trail_k = c->trail_k + head0 * BLK * D;
   a.trail_v = c->trail_v + head0 * BLK * D;
@@ -94,90 +96,109 @@ static int put_pass(SetArgs<SCORES>& a, const Cache* c, int layer, int nodes, in
   a.n = nodes;
   a.nd = drafts;
   a.first = first;
-  a.part = part;
-  const int n_rows = nodes * a.group, others = a.trail + drafts;
+  const int n_rows = nodes * a.group;
   a.row_tiles = (n_rows + 31) / 32;
-  const Shape x = shape_of(c->n_cu, heads, n_rows, a.nb * BLK, others);
-  a.nsplit = x.nsplit;
-  if (x.rows > 32) {
-    put_shares(a, x.rows, others);
-  } else if (x.rows <= L_ROWS + 1) {
-    const TileShares s = light_shares((int)((a.nb + 1) / 2), others, a.nsplit, x.rows == L_ROWS ? 4 : 12);
+  Pass x;
+  x.heads = kv_groups(c);
+  x.others = a.trail + drafts;
+  x.shape = shape_of(c->n_cu, x.heads, n_rows, a.nb * BLK, x.others);
+  a.nsplit = x.shape.nsplit;
+  if (x.shape.rows > 32) put_shares(a, x.shape.rows, x.others);
+  if (x.shape.rows == L_ROWS) {
+    const TileShares s = light_shares((int)((a.nb + 1) / 2), x.others, a.nsplit, x.shape.waves);
     a.share = s.share, a.over = s.over, a.least = s.least, a.last = s.last;
   }
-  return x.rows;
+  x.floats = x.heads * a.row_tiles * a.nsplit * T_FLOATS;
+  return x;
+}
+template <Scores SCORES>
+static void put_scores(SetArgs<SCORES>& a, const cqa_scoring& s, bool many) {
+  constexpr float LOG2E = 1.4426950408889634f;
+  a.scale = s.scale != 0.0f ? s.scale : PLAIN_SCALE;
+  a.cap = s.cap;
+  a.cap_kind = s.cap == 0.0f ? CAP_NONE : (many && s.cap <= LOW_CAPS ? CAP_LOW : CAP_HIGH);
+  a.gain = a.cap_kind == CAP_NONE ? 0.0f : (a.cap_kind == CAP_LOW ? 2.0f * LOG2E : 1.0f) * (a.scale / s.cap);
+  a.per_unit = LOG2E * (a.cap_kind == CAP_NONE ? a.scale : (a.cap_kind == CAP_LOW ? 2.0f * s.cap : s.cap));
+  a.offset = a.cap_kind == CAP_LOW ? s.cap : 0.0f;
+  a.slopes = s.slopes_dev;
+  a.places = s.places_dev;
+  a.spans = s.spans_dev;
+}
+template <typename A>
+static int32_t launch_rows(const A& a, const Pass& x, hipStream_t st) {
+  if (x.shape.rows != L_ROWS) return launch_pass(a, x.heads, x.shape.rows, x.others, st);
+  const dim3 grid((uint32_t)x.heads, (uint32_t)a.nsplit);
+  if (x.shape.waves == 4)
+    tree_light_kernel<4><<<grid, 256, 0, st>>>(a);
+  else
+    tree_light_kernel<12><<<grid, 768, 0, st>>>(a);
+  CQA_HIP(hipGetLastError());
+  return CQA_OK;
+}
+// A pass that is all of its rows'.
+template <typename A>
+static int32_t launch_alone(const A& a, const Pass& x, int n_cu, hipStream_t st) {
+  if (const int32_t rc = launch_rows(a, x, st)) return rc;
+  return a.nsplit == 1 ? CQA_OK : launch_join(a, x.heads, a.nsplit, n_cu, st);
 }
 
 template <Scores SCORES>
-static int32_t run(const Cache* shared, const Cache* c, int layer, const NodeCall& x, float* ws, hipStream_t st) {
+static int32_t run(const Cache* shared, const Cache* c, int layer, const NodeCall& call, float* ws, hipStream_t st) {
   SetArgs<SCORES> a = {};
-  a.q = x.q;
-  a.kd = x.kd;
-  a.vd = x.vd;
-  a.mask = x.mask;
-  a.words = (x.n + 63) / 64;
+  a.q = call.q;
+  a.kd = call.kd;
+  a.vd = call.vd;
+  a.mask = call.mask;
+  a.words = (call.n + 63) / 64;
   a.n_kv = c->desc.n_kv_heads;
   a.group = c->desc.n_q_heads / c->desc.n_kv_heads;
-  a.O = x.O;
-  a.cert = x.cert;
-  a.flags = x.flags;
-  a.tol = *x.tol;
-  const int64_t beginning = shared != nullptr ? shared->length[layer] : 0, heads = (int64_t)c->desc.batch * c->desc.n_kv_heads;
-  a.each = x.n;
+  a.O = call.O;
+  a.cert = call.cert;
+  a.flags = call.flags;
+  a.tol = *call.tol;
+  a.part = ws;
+  const int64_t beginning = shared != nullptr ? shared->length[layer] : 0;
+  const int drafts = call.kd != nullptr ? call.n : 0;
+  a.each = call.n;
   a.cached = (int)(beginning + c->length[layer]);
-  a.drafted = x.kd != nullptr;
-  if (SCORES != PLAIN) {
-    const cqa_scoring& s = *x.scoring;
-    constexpr float LOG2E = 1.4426950408889634f;
-    a.scale = s.scale != 0.0f ? s.scale : 0.08838834764831845f;
-    a.cap = s.cap;
-    a.cap_kind = s.cap == 0.0f ? CAP_NONE : (s.cap <= LOW_CAPS ? CAP_LOW : CAP_HIGH);
-    a.gain = a.cap_kind == CAP_NONE ? 0.0f : (a.cap_kind == CAP_LOW ? 2.0f * LOG2E : 1.0f) * (a.scale / s.cap);
-    a.per_unit = LOG2E * (a.cap_kind == CAP_NONE ? a.scale : (a.cap_kind == CAP_LOW ? 2.0f * s.cap : s.cap));
-    a.level = a.cap_kind == CAP_NONE ? a.per_unit : 1.0f;
-    a.offset = a.cap_kind == CAP_LOW ? s.cap : 0.0f;
-    a.slopes = s.slopes_dev;
-    a.places = s.places_dev;
-    a.spans = s.spans_dev;
+  a.drafted = drafts != 0;
+  // The sequences' own tokens and the beginning's, a pass each where there are any; the first also where there are none at all.
+  JoinArgs<SCORES> both = {};
+  SetArgs<SCORES>& b = both;
+  b = a;
+  const bool has_own = beginning == 0 || c->length[layer] + drafts > 0, has_shared = beginning != 0;
+  const Pass own = put_pass(a, c, layer, call.n, drafts, (int)beginning);
+  const Pass theirs = has_shared ? put_pass(b, shared, layer, call.n * (c->desc.batch / shared->desc.batch), 0, 0) : Pass{};
+  if constexpr (SCORES != PLAIN) {
+    const bool many = (has_own && own.shape.rows > 32) || (has_shared && theirs.shape.rows > 32);
+    put_scores(a, *call.scoring, many);
+    put_scores(b, *call.scoring, many);
   }
-  const int drafts = a.drafted ? x.n : 0;
-  const bool own = beginning == 0 || c->length[layer] + drafts > 0;
-  if (beginning == 0) {
-    const int rows = put_pass(a, c, layer, x.n, drafts, 0, ws);
-    if (const int32_t rc = launch_rows(a, heads, rows, a.trail + drafts, st)) return rc;
-    return a.nsplit == 1 ? CQA_OK : launch_join(a, heads, a.nsplit, c->n_cu, st);
-  }
-  const int64_t shared_heads = (int64_t)shared->desc.batch * shared->desc.n_kv_heads;
-  JoinArgs<SCORES> j = {};
-  static_cast<SetArgs<SCORES>&>(j) = a;
-  const int shared_rows = put_pass(static_cast<SetArgs<SCORES>&>(j), shared, layer, x.n * (c->desc.batch / shared->desc.batch), 0, 0, ws);
-  j.row_sets = own;
-  const SetArgs<SCORES>& s = j;
-  if (!own) {
-    if (const int32_t rc = launch_rows(s, shared_heads, shared_rows, s.trail, st)) return rc;
-    return s.nsplit == 1 ? CQA_OK : launch_join(s, shared_heads, s.nsplit, c->n_cu, st);
-  }
-  a.row_sets = 1;
-  const int rows = put_pass(a, c, layer, x.n, drafts, (int)beginning, ws + shared_heads * s.row_tiles * s.nsplit * T_FLOATS);
-  if (shared_rows == L_ROWS && rows == L_ROWS && shared_heads * s.nsplit + heads * a.nsplit <= 3 * (int64_t)c->n_cu) {
-    const TwoPasses<SetArgs<SCORES>> two = {s, a, (int)shared_heads, (int)shared_heads * s.nsplit, (int)heads};
-    tree_light_two_kernel<4><<<dim3((uint32_t)(two.a_groups + heads * a.nsplit)), 256, 0, st>>>(two);
+  if (!has_shared) return launch_alone(a, own, c->n_cu, st);
+  if (!has_own) return launch_alone(b, theirs, c->n_cu, st);
+  a.row_sets = b.row_sets = 1;
+  a.part = ws + theirs.floats;
+  const int64_t groups = theirs.heads * b.nsplit + own.heads * a.nsplit;
+  if (theirs.shape.rows == L_ROWS && own.shape.rows == L_ROWS && theirs.shape.waves == 4 && own.shape.waves == 4 && groups <= 3 * (int64_t)c->n_cu) {
+    // (as many as the device holds at a time: 2 sequences behind 1029 tokens, 1 KV head 13.0 us, by two launches 18.7)
+    const TwoPasses<SetArgs<SCORES>> two = {b, a, (int)theirs.heads, (int)(theirs.heads * b.nsplit), (int)own.heads};
+    tree_light_two_kernel<4><<<dim3((uint32_t)groups), 256, 0, st>>>(two);
     CQA_HIP(hipGetLastError());
   } else {
-    if (const int32_t rc = launch_rows(s, shared_heads, shared_rows, s.trail, st)) return rc;
-    if (const int32_t rc = launch_rows(a, heads, rows, a.trail + drafts, st)) return rc;
+    if (const int32_t rc = launch_rows(b, theirs, st)) return rc;
+    if (const int32_t rc = launch_rows(a, own, st)) return rc;
   }
-  j.own = a.part;
-  j.own_tiles = a.row_tiles;
-  j.own_sets = a.nsplit;
-  return launch_join(j, shared_heads, j.nsplit + a.nsplit, c->n_cu, st);
+  both.own = a.part;
+  both.own_tiles = a.row_tiles;
+  both.own_sets = a.nsplit;
+  return launch_join(both, theirs.heads, both.nsplit + a.nsplit, c->n_cu, st);
 }
 
-int32_t launch_scored(const Cache* shared, const Cache* c, int layer, const NodeCall& x, float* ws, hipStream_t st) {
-  const cqa_scoring* const s = x.scoring;
-  if (s != nullptr && (s->slopes_dev != nullptr || s->spans_dev != nullptr)) return run<PLACED>(shared, c, layer, x, ws, st);
-  if (s != nullptr && ((s->scale != 0.0f && s->scale != 0.08838834764831845f) || s->cap != 0.0f)) return run<SCALED>(shared, c, layer, x, ws, st);
-  return run<PLAIN>(shared, c, layer, x, ws, st);
+int32_t launch_scored(const Cache* shared, const Cache* c, int layer, const NodeCall& call, float* ws, hipStream_t st) {
+  const cqa_scoring* const s = call.scoring;
+  if (s != nullptr && (s->slopes_dev != nullptr || s->spans_dev != nullptr)) return run<PLACED>(shared, c, layer, call, ws, st);
+  if (s != nullptr && ((s->scale != 0.0f && s->scale != PLAIN_SCALE) || s->cap != 0.0f)) return run<SCALED>(shared, c, layer, call, ws, st);
+  return run<PLAIN>(shared, c, layer, call, ws, st);
 }
 
 }  // namespace cqa

@@ -37,6 +37,7 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+constexpr float PLAIN_SCALE = 0.08838834764831845f;
 constexpr float SCORE = 0.08838834764831845f * 1.4426950408889634f;   // 1 / sqrt(d), in the exponent's base 2
 constexpr float HALF_SCORE = 0.5f * 0.08838834764831845f;
 constexpr float F16_MAX = 65504.0f;
@@ -84,7 +85,6 @@ struct TreeArgs {
   __device__ int drafts() const { return n; }
   __device__ SetsOf sets_of(const float* sets, int head, int r32, int r) const;
   __device__ float unit() const { return SCORE; }        // exponents of 2 that a unit of score is worth
-  __device__ float m_unit() const { return SCORE; }
   __device__ float half_scale() const { return HALF_SCORE; }
 };
 
@@ -92,9 +92,10 @@ struct TreeArgs {
 // joined with another pass's; SCORES: with scores of the caller's.  x = scale q . k,  y = cap tanh(x / cap),  score = y - slope |p - j|.
 //   What the softmax works on is the score in units of its own, `per_unit` exponents of 2 each, and less a constant of the row:
 //   CAP_NONE   q . k
-//   CAP_LOW    -1 / (1 + e^(2 x / cap)) = (tanh(x / cap) - 1) / 2: an exponential and a reciprocal; off by 2^-24 of a unit, 2 cap, which is why it is
-//              only for caps up to LOW_CAPS
-//   CAP_HIGH   tanh(x / cap), relatively exact
+//   CAP_LOW    -1 / (1 + e^(2 x / cap)) = (tanh(x / cap) - 1) / 2, an exponential and a reciprocal: off by 2^-24 of a unit, 2 cap
+//   CAP_HIGH   tanh(x / cap), relatively exact, for some eight operations more
+// LOW where a pass reconstructs for many rows at once, which the scores' operations bound, and the cap is at most LOW_CAPS.  (8 heads, 131072 tokens, 64 nodes
+// of 4 heads: LOW 222 us, HIGH 287; one token: 66.5, HIGH_US.)
 // and the bias counts from the distance `near` of the row's nearest attended token (the farthest, under a negative slope), so that the scores of a
 // row that attends far tokens only keep their bits.
 enum { CAP_NONE = 0, CAP_LOW, CAP_HIGH };
@@ -113,15 +114,12 @@ struct SetArgs : TreeArgs {
   int cap_kind;
   float gain;              // x / cap by q . k: CAP_LOW in exponents of 2, twice
   float per_unit, offset;  // offset: of the score, where the unit's zero is
-  float level;             // exponents of 2 by a row's m: 1 with a cap, per_unit without
   float cap, scale;
   const float* slopes;     // [Hq]
   const int64_t* places;   // [Bt][n]
   const int64_t* spans;    // [Bt][n][4]
   __device__ int drafts() const { return nd; }
   __device__ float unit() const { return SCORED ? per_unit : SCORE; }
-  __device__ float m_unit() const { return SCORED ? level : SCORE; }
-  __device__ bool capped() const { return SCORED && cap_kind != CAP_NONE; }
   __device__ float half_scale() const { return SCORED ? 0.5f * scale : HALF_SCORE; }
 };
 
@@ -463,7 +461,7 @@ __device__ __forceinline__ void values32(TreeRows& w, const uint32_t (&p)[8], Va
 }
 // What weights relative to a largest score m are worth beside a largest one M >= m (-inf: there are none).
 template <typename A>
-__device__ __forceinline__ float set_weight(const A& a, float m, float M) { return m == M ? 1.0f : __builtin_amdgcn_exp2f((m - M) * a.m_unit()); }
+__device__ __forceinline__ float set_weight(const A& a, float m, float M) { return m == M ? 1.0f : __builtin_amdgcn_exp2f((m - M) * a.unit()); }
 // Scores of MT times 32 tokens to weights, 2^MOST for a row's largest score so far, the row's m.  The weights enter
 // the product with the values as FP16: those down to 2^-28 of the largest keep 11 bits, and a million lighter ones are together off by 2^-19
 // of it.  (With 1 for the largest, tokens of 2^-25 of it vanished, and all of the result with them where the heavy ones' values are zero.)
@@ -517,9 +515,14 @@ __device__ __forceinline__ void softmax32(const A& a, TreeRows& w, f32x16 (&s)[M
     w.evmax = fmaxf(w.evmax, e);
   }
 }
-// The same in passes of SetArgs, for MT times N scores of a lane.  With a cap, which bounds them, a row's m is its largest score's exponent of 2, upwards, a
-// whole number: a weight's exponent is one multiply-add, and sets of different m join exactly.  largest(x): over the lanes of a row; block(x): the sum
-// over a block.
+template <typename A>
+__device__ __forceinline__ bool low_cap(const A& a) {
+  if constexpr (A::SCORED) return a.cap_kind == CAP_LOW;
+  return false;
+}
+// The same in passes of SetArgs, for MT times N scores of a lane.  Under CAP_LOW, whose scores are within 2 cap of each other, m is taken off in the
+// multiply-add that scales them: one rounding, 2^-18 of an exponent, that all weights by this m share (8 heads, 131072 tokens, 64 nodes of 4 heads 245, 229
+// us).  largest(x): over the lanes of a row; block(x): the sum over a block.
 // silent: a lane's row has no part in it (one that attends no cached token, among others whose tokens are not looked at one by one).
 template <int MT, int N, typename A, typename Rows, typename V, typename Bits, typename Eta, typename Largest, typename Block>
 __device__ __forceinline__ void softmax_sets(const A& a, Rows& w, V (&s)[MT], uint32_t (&p)[MT][N / 2], bool masked, Bits bits, Eta eta, Largest largest, Block block,
@@ -538,7 +541,6 @@ __device__ __forceinline__ void softmax_sets(const A& a, Rows& w, V (&s)[MT], ui
 #pragma unroll
     for (int r = 0; r < N; ++r) top = fmaxf(top, s[mt][r]);
   top = largest(top);
-  top = a.capped() ? ceilf(top * a.unit()) : top;
   if constexpr (A::PLACED) top = silent ? -INFINITY : top;
   if (__any(top > w.m)) {
     const float mn = fmaxf(w.m, top);
@@ -551,13 +553,15 @@ __device__ __forceinline__ void softmax_sets(const A& a, Rows& w, V (&s)[MT], ui
     w.each_sum([&](float o) { return o * f; });
   }
   const float m = w.m == -INFINITY ? 0.0f : w.m;   // nothing attended yet: every weight is exp2(-inf) = 0
-  float most = a.capped() ? MOST - m : MOST;
-  if constexpr (A::PLACED) most = silent ? -INFINITY : most;
-  if (!a.capped())
+  float most = MOST;
+  if (low_cap(a))
+    most = fmaf(-m, a.unit(), MOST);
+  else
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int r = 0; r < N; ++r) s[mt][r] -= m;
+  if constexpr (A::PLACED) most = silent ? -INFINITY : most;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     float bs = 0.0f;
@@ -890,7 +894,7 @@ __device__ __forceinline__ Certificate certificate(const A& a, float M, float L,
   ct.delta_h = DM;
   ct.v_max = VM;
   ct.alpha_tail_hat = sealed * inv;
-  ct.lse = empty ? -INFINITY : fmaf(M, a.m_unit() * LN2, logf(L) - MOST * LN2);
+  ct.lse = empty ? -INFINITY : fmaf(M, a.unit() * LN2, logf(L) - MOST * LN2);
   if constexpr (A::SCORED) ct.lse = empty ? ct.lse : ct.lse + offset;
   ct.max_block_contrib = EM * inv;
   ct.reserved = 0.0f;

@@ -321,9 +321,9 @@ def again(x, bt):
     return None if x is None else np.tile(x, ((bt + len(x) - 1) // len(x),) + (1,) * (x.ndim - 1))[:bt]
 
 
-# 33 .. 64, 65 .. 128, up to 256 rows, all of a workgroup that reconstructs once for them: caches that are long for the device
+# caches that are long for the device: up to 16 rows by twelve waves; 33 .. 64, 65 .. 128, up to 256 rows by a workgroup that reconstructs once for all
 @pytest.mark.parametrize("n,tokens,cap,bias,spans", [
-    (13, 1157, 5.0, 1, "sorted"), (13, 1293, 0.0, -1, "window"), (13, 1290, 50.0, 0, "any"), (27, 1093, 3.0, 1, "padded"), (27, 1347, 1e3, 1, "sorted"),
+    (1, 1157, 30.0, 0, "all"), (1, 2053, 0.0, 1, "window"), (4, 1293, 5.0, 1, "sorted"), (4, 1029, 0.0, 0, "any"), (2, 1290, 500.0, -1, "padded"), (13, 1157, 5.0, 1, "sorted"), (13, 1293, 0.0, -1, "window"), (13, 1290, 50.0, 0, "any"), (27, 1093, 3.0, 1, "padded"), (27, 1347, 1e3, 1, "sorted"),
     (27, 1100, 0.0, 0, "window"), (64, 1093, 30.0, 0, "sorted"), (64, 1285, 2.0, 1, "window"), (64, 1029, 0.0, 1, "any"), (64, 1290, 9.0, 0, "all")])
 @pytest.mark.parametrize("beginnings", [False, True])
 def test_many_rows_of_many_sequences(n, tokens, cap, bias, spans, beginnings):
@@ -337,7 +337,7 @@ def test_many_rows_of_many_sequences(n, tokens, cap, bias, spans, beginnings):
     seen = random_tree(rng, 4, n)
     places = total + seen.sum(-1) - 1
     sp, slopes = make_spans(rng, spans, 4, n, total, places), slopes_of(4, bias)
-    some = np.unique([0, 1, n // 2, n - 1])
+    some = np.unique([0, min(1, n - 1), n // 2, n - 1])
     with Caches(x, 4) as c:
         # (the definition's rows are some of the nodes: drafted tokens are all there, with the masks and places of all)
         keep = dict(cap=cap, slopes=slopes, spans=None if sp is None else sp[:, some])
@@ -501,6 +501,42 @@ def test_more_sequences_than_compute_units_and_more_than_256_rows():
             assert_nodes(ref, O[:4], {f: y[:4] for f, y in cert.items()}, flags[:4], bt)
             assert all(np.array_equal(O[i], O[i % 4]) and np.array_equal(cert["E_key"][i], cert["E_key"][i % 4]) for i in range(bt))
             gc.close()
+
+
+@pytest.mark.parametrize("hkv,g,beginning,bt,n,cap", [(4, 4, 20016, 32, 1, 0.0), (4, 4, 20005, 16, 1, 40.0), (2, 4, 33003, 12, 6, 0.0), (8, 2, 5001, 160, 1, 20.0)])
+def test_many_sequences_behind_a_long_beginning(hkv, g, beginning, bt, n, cap):
+    """33 and more rows of several sequences by a workgroup that reconstructs once for all."""
+    print("prefix long", hkv, g, beginning, bt, n, flush=True)
+    rng = np.random.default_rng(bt)
+    x = make(rng, 4, hkv, g, 35, n, n > 1, "student", 2.0, 1, beginning)
+    seen = random_tree(rng, 4, n) if n > 1 else None
+    some = np.unique([0, n - 1])
+    with Caches(x, g) as c:
+        gc = GpuLayerCache(bt, hkv * g, hkv, 64, tier2=False)
+        gc.append(again(x["k"], bt), again(x["v"], bt))
+        O, cert, flags = call(c.shared, gc, again(x["q"], bt), again(x["kd"], bt), again(x["vd"], bt), None if seen is None else drafts.mask_words(again(seen, bt)), cap=cap)
+        places = scored.default_places(4, n, beginning + 35, n > 1)
+        if n > 1:
+            ref = some_nodes(c, x, seen, places, some, cap=cap)
+        else:
+            ref = scored.decode(c.shared_oc, c.oc, x["q"], None, None, None, oracle.Tolerances(), cap=cap)
+        gc.close()
+    assert_nodes(ref, O[:4, some], {f: y[:4, some] for f, y in cert.items()}, flags[:4, some], bt)
+    for y in (O, flags, *cert.values()):
+        assert all(np.array_equal(y[i], y[i % 4]) for i in range(bt))
+
+
+def test_nothing_at_all_is_attended():
+    """Empty caches and no drafted tokens, and an empty mask."""
+    print("scored empty", flush=True)
+    rng = np.random.default_rng(2)
+    for n in (1, 9, 70):
+        x = make(rng, 2, 1, 4, 0, n, True, shared=1, beginning=0)
+        with Caches(x, 4) as c:
+            for shared in (None, c.shared):
+                for got in (call(shared, c.gc, x["q"], cap=3.0), call(shared, c.gc, x["q"], x["kd"], x["vd"], np.zeros((2, n, (n + 63) // 64), np.uint64))):
+                    assert (got[0] == 0).all() and (got[2] == 0).all()
+                    assert all((y == (-np.inf if f == "lse" else 0)).all() for f, y in got[1].items())
 
 
 def test_the_calls_refuse_what_they_do_not_do():
