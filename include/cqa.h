@@ -564,10 +564,10 @@ int32_t cqa_tree_workspace_bytes(const cqa_cache* c, int32_t n_draft, int64_t* b
  * node.
  *   scale       0: 1 / sqrt(128); otherwise 2^-40 .. 2^40
  *   cap         0: none; otherwise 2^-20 .. 2^60
- *   slopes_dev  float [n_q_heads], or NULL: no bias.  Negative slopes are allowed; one that is no finite number makes its head's rows NaN
- *               with PRECOND, as such queries do
+ *   slopes_dev  float [n_q_heads], or NULL: no bias.  Negative slopes are allowed; one that is no finite number, or beyond 10^28 scale (10^28
+ *               cap, with a cap), makes its head's rows NaN with PRECOND, as such queries do
  *   places_dev  int64 [batch][n_nodes], or NULL: node i of drafted ones is at the number of cached tokens + i; without drafted tokens
- *               the nodes are the last n_nodes cached tokens.  Used by the bias only.  Places count up to 2^30 tokens ahead of the first and behind
+ *               the nodes are the last n_nodes cached tokens.  Used by the bias only.  Places count up to 2^29 tokens ahead of the first and behind
  *               the last cached token: one beyond is taken for that
  *   spans_dev   int64 [batch][n_nodes][4], or NULL: every cached token.  Node i attends the cached tokens j with s[0] <= j < s[1] or
  *               s[2] <= j < s[3], each once where the spans overlap; a span may be empty (to <= from) or reach beyond the cached tokens.  Sliding

@@ -1298,7 +1298,7 @@ static int32_t nodes_decode(const cqa_cache* shared, const cqa_cache* h, int32_t
   if (tol->int8_query != 0) return CQA_ERR_UNSUPPORTED;
   const Cache* const c = &h->impl;
   const Cache* const s = shared != nullptr ? &shared->impl : nullptr;
-  // places and spans count in 32 bits, with 2^30 of room to either side
+  // places and spans count in 32 bits
   if (c->length[layer] + (s != nullptr ? s->length[layer] : 0) >= (int64_t)1 << 30) return CQA_ERR_UNSUPPORTED;
   if (const int32_t rc = check_device(c)) return rc;
   const NodeCall x = {(const __half*)q, (const __half*)kd, (const __half*)vd, n_nodes, mask, scoring, tol, (__half*)O, cert, flags};

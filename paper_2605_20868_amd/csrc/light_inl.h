@@ -142,7 +142,7 @@ __device__ __forceinline__ void end_light(const A& a, const float (*sets)[L_SET]
     bad = fmaxf(bad, st[T_BAD * L_ROWS]);
   }
   if (!leaves) {
-    put_certificate(a, out, certificate(a, M, L, SL, E, EM, DM, VM, out_offset(a, out)), bad != 0.0f);
+    put_certificate(a, out, certificate(a, M, L, SL, E, EM, DM, VM, out_offset(a, head, row)), bad != 0.0f);
     return;
   }
   float* const st = to + T_OFLOATS + row;
@@ -175,14 +175,15 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
   bool spans = false;
   if constexpr (A::PLACED) {
     const int64_t node = (int64_t)b * a.n + rows.node;
-    const RowBias x = row_bias(a, node, kvh * a.group + (min(n16, last_row) - rows.node * a.group));
+    const SpansGiven given = spans_given(a, node);
+    const RowBias x = row_bias(a, node, kvh * a.group + (min(n16, last_row) - rows.node * a.group), given);
     rows.slope = x.slope * (1.0f / (a.per_unit * LN2));
     rows.place = x.place - a.first;
     rows.near = x.near;
     spans = a.spans != nullptr;
     rows.idle = false;
     if (spans) {
-      const Spans mine = node_spans(a, node, a.first, (int)a.nb * BLK + a.trail);
+      const Spans mine = spans_among(given, a.first, (int)a.nb * BLK + a.trail);
       rows.idle = mine.hi0 == 0 && mine.hi1 == 0;
       if (l < L_ROWS) lds.span[l] = mine;                   // (every wave the same)
       active = active_units(hull_of<L_ROWS>(mine), (int)a.nb * BLK, 2 * BLK);

@@ -95,7 +95,7 @@ struct TreeArgs {
 //   CAP_LOW    -1 / (1 + e^(2 x / cap)) = (tanh(x / cap) - 1) / 2, an exponential and a reciprocal: off by 2^-24 of a unit, 2 cap
 //   CAP_HIGH   tanh(x / cap), relatively exact, for some eight operations more
 // LOW where a pass reconstructs for many rows at once, which the scores' operations bound, and the cap is at most LOW_CAPS.  (8 heads, 131072 tokens, 64 nodes
-// of 4 heads: LOW 222 us, HIGH 287; one token: 66.5, HIGH_US.)
+// of 4 heads: LOW 222 us, HIGH 287; one token: 66.5, 68.0.)
 // and the bias counts from the distance `near` of the row's nearest attended token (the farthest, under a negative slope), so that the scores of a
 // row that attends far tokens only keep their bits.
 enum { CAP_NONE = 0, CAP_LOW, CAP_HIGH };
@@ -211,14 +211,22 @@ using RowsOf = std::conditional_t<A::SCORED, ScoredRows, std::conditional_t<A::S
 struct Spans {
   int lo0, hi0, lo1, hi1;
 };
-// A node's spans among the tokens first .. first + count - 1, from there on; empty ones are 0 .. 0.
+// A node's spans as they are given; without any, the cached tokens.
+struct SpansGiven {
+  int64_t at[4];
+};
 template <typename A>
-__device__ __forceinline__ Spans node_spans(const A& a, int64_t node, int first, int count) {
-  Spans s = {0, count, 0, 0};
-  if (a.spans == nullptr) return s;
+__device__ __forceinline__ SpansGiven spans_given(const A& a, int64_t node) {
+  SpansGiven s = {{0, a.cached, 0, 0}};
+  if (a.spans != nullptr)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s.at[i] = a.spans[node * 4 + i];
+  return s;
+}
+// ... among the tokens first .. first + count - 1, from there on; empty ones are 0 .. 0.
+__device__ __forceinline__ Spans spans_among(const SpansGiven& x, int first, int count) {
   const auto clip = [&](int64_t x) { return (int)(x < first ? 0 : (x - first > count ? count : x - first)); };
-  const int64_t* const p = a.spans + node * 4;
-  s.lo0 = clip(p[0]), s.hi0 = clip(p[1]), s.lo1 = clip(p[2]), s.hi1 = clip(p[3]);
+  Spans s = {clip(x.at[0]), clip(x.at[1]), clip(x.at[2]), clip(x.at[3])};
   if (s.lo0 >= s.hi0) s.lo0 = s.hi0 = 0;
   if (s.lo1 >= s.hi1) s.lo1 = s.hi1 = 0;
   return s;
@@ -228,38 +236,55 @@ __device__ __forceinline__ uint32_t span_bits(const Spans& s, int t) {
   const auto below = [&](int x) { return (1u << min(max(x - t, 0), BLK)) - 1u; };   // tokens ahead of x
   return (below(s.hi0) & ~below(s.lo0)) | (below(s.hi1) & ~below(s.lo1));
 }
-// Places count 2^30 tokens around the cached ones, and end there.
+// Places count 2^29 tokens around the cached ones, fewer than 2^30, and end there: distances are within 32 bits.
 template <typename A>
-__device__ __forceinline__ int node_place(const A& a, int64_t node, int in_sequence) {
-  if (a.places == nullptr) return a.cached - (a.drafted ? 0 : a.each) + in_sequence;
-  const int64_t p = a.places[node];
-  constexpr int64_t FAR = 1 << 30;
+__device__ __forceinline__ int64_t place_given(const A& a, int64_t node, int in_sequence) {
+  return a.places == nullptr ? a.cached - (a.drafted ? 0 : a.each) + in_sequence : a.places[node];
+}
+template <typename A>
+__device__ __forceinline__ int held_place(const A& a, int64_t p) {
+  constexpr int64_t FAR = 1 << 29;
   return (int)(p > a.cached + FAR ? a.cached + FAR : (p < -FAR ? -FAR : p));
 }
+template <typename A>
+__device__ __forceinline__ int node_place(const A& a, int64_t node, int in_sequence) { return held_place(a, place_given(a, node, in_sequence)); }
 struct RowBias {
   float slope;
   int place, near;
 };
-// Of all passes alike: places from the first cached token of all.
+// Of all passes alike: places from the first cached token of all.  (What is given is asked for at once.)
 template <typename A>
-__device__ __forceinline__ RowBias row_bias(const A& a, int64_t node, int q_head) {
+__device__ __forceinline__ RowBias row_bias(const A& a, int64_t node, int q_head, const SpansGiven& given) {
   RowBias x = {0.0f, 0, 0};
   if (a.slopes == nullptr) return x;
+  const int i = (int)((uint32_t)node % (uint32_t)a.each);
+  const auto bits = [&](int word) { return a.mask[node * a.words + word]; };
   x.slope = a.slopes[q_head];
-  x.place = node_place(a, node, (int)(node % a.each));
-  const Spans s = node_spans(a, node, 0, a.cached);
+  const int64_t place = place_given(a, node, i);
+  const uint64_t own = a.mask == nullptr ? ~0ull : bits(i >> 6);
+  x.place = held_place(a, place);
+  const Spans s = spans_among(given, 0, a.cached);
+  const bool near = x.slope >= 0.0f;
   const auto to = [&](int t) { return abs(x.place - t); };
-  if (x.slope >= 0.0f) {
-    bool own = a.drafted && a.mask == nullptr;
-    if (a.drafted && a.mask != nullptr)
-      for (int i = 0; i < a.words; ++i) own |= a.mask[node * a.words + i] != 0;
-    const auto nearest = [&](int lo, int hi) { return lo == hi ? 0x7fffffff : (x.place < lo ? lo - x.place : max(x.place - hi + 1, 0)); };
-    const int d = min(nearest(s.lo0, s.hi0), nearest(s.lo1, s.hi1));
-    x.near = own || d == 0x7fffffff ? 0 : d;
-  } else {
-    if (s.lo0 < s.hi0) x.near = max(to(s.lo0), to(s.hi0 - 1));
-    if (s.lo1 < s.hi1) x.near = max(x.near, max(to(s.lo1), to(s.hi1 - 1)));
+  int least = 0x7fffffff, most = 0;   // distances of the attended
+  const auto span = [&](int lo, int hi) {
+    if (lo == hi) return;
+    least = min(least, x.place < lo ? lo - x.place : max(x.place - hi + 1, 0));
+    most = max(most, max(to(lo), to(hi - 1)));
+  };
+  span(s.lo0, s.hi0);
+  span(s.lo1, s.hi1);
+  if (a.drafted && near && (own >> (i & 63) & 1u) != 0u) {
+    least = 0;   // itself
+  } else if (a.drafted) {
+    for (int j = 0; j < a.each; ++j) {
+      if (a.mask == nullptr ? j > i : (bits(j >> 6) >> (j & 63) & 1u) == 0u) continue;
+      const int d = to(node_place(a, node - i + j, j));
+      least = min(least, d);
+      most = max(most, d);
+    }
   }
+  x.near = near ? (least == 0x7fffffff ? 0 : least) : most;
   return x;
 }
 // What the row's scores are more than those worked on, in natural units.
@@ -267,14 +292,15 @@ template <typename A>
 __device__ __forceinline__ float row_offset(const A& a, int64_t node, int q_head) {
   if constexpr (A::SCORED) {
     if constexpr (!A::PLACED) return a.offset;
-    const RowBias x = row_bias(a, node, q_head);
-    return a.slopes == nullptr ? a.offset : fmaf(-x.slope, (float)x.near, a.offset);
+    if (a.slopes == nullptr) return a.offset;
+    const RowBias x = row_bias(a, node, q_head, spans_given(a, node));
+    return fmaf(-x.slope, (float)x.near, a.offset);
   }
   return 0.0f;
 }
 // A lane's products with N tokens become scores.  far(r): |place - token| - near.
-// (tanh by a series of six coefficients where all of a wave's products are in its range, which is relatively exact at the small ones, is two operations a
-// score more: 8 heads, 131072 tokens, 64 nodes of 4 heads 293 us, so 241.)
+// (A series of six coefficients where all of a wave's products are in its range, which is relatively exact at the small ones, is two operations a
+// score more than CAP_LOW: 8 heads, 131072 tokens, 64 nodes of 4 heads 293 us, 241.)
 template <typename A>
 __device__ __forceinline__ float cap_low(const A& a, float s) { return __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s * a.gain)); }
 // low_done: CAP_LOW has been applied.
@@ -433,11 +459,12 @@ template <typename A>
 __device__ __forceinline__ void score_rows(ScoredRows& s, const A& a, int b, int kvh, int tile, int count, Spans* at, Spans& mine) {
   const int l = threadIdx.x & 63, r = min(tile * T_ROWS + (l & 31), a.n * a.group - 1);
   const int64_t node = (int64_t)b * a.n + s.node;
-  const RowBias x = row_bias(a, node, kvh * a.group + (r - s.node * a.group));
+  const SpansGiven given = spans_given(a, node);
+  const RowBias x = row_bias(a, node, kvh * a.group + (r - s.node * a.group), given);
   s.slope = x.slope * (1.0f / (a.per_unit * LN2));
   s.place = x.place - a.first;
   s.near = x.near;
-  mine = node_spans(a, node, a.first, count);
+  mine = spans_among(given, a.first, count);
   s.idle = a.spans != nullptr && mine.hi0 == 0 && mine.hi1 == 0;
   if (a.spans != nullptr && l < T_ROWS) at[l] = mine;
 }
@@ -858,12 +885,11 @@ __device__ __forceinline__ int64_t row_out(const A& a, int head, int r) {
   const int b = head / a.n_kv, kvh = head - b * a.n_kv, node = r / a.group;
   return ((int64_t)b * a.n + node) * a.n_kv * a.group + kvh * a.group + (r - node * a.group);
 }
-// Its node and query head, for row_offset.
 template <typename A>
-__device__ __forceinline__ float out_offset(const A& a, int64_t out) {
+__device__ __forceinline__ float out_offset(const A& a, int head, int r) {
   if constexpr (A::SCORED) {
-    const int hq = a.n_kv * a.group;
-    return row_offset(a, out / hq, (int)(out % hq));
+    const int b = head / a.n_kv, kvh = head - b * a.n_kv, node = r / a.group;
+    return row_offset(a, (int64_t)b * a.n + node, kvh * a.group + (r - node * a.group));
   }
   return 0.0f;
 }
@@ -931,7 +957,7 @@ __device__ __forceinline__ void finish_rows(const TreeRows& w, const A& a, int h
     for (int r4 = 0; r4 < 4; ++r4)
       bad |= put_channels(a, out, (r4 >> 1) * 16 + ct * 4 + (r4 & 1) * 2 + half, make_float4(w.o[ct][4 * r4], w.o[ct][4 * r4 + 1], w.o[ct][4 * r4 + 2], w.o[ct][4 * r4 + 3]), inv);
   bad = __shfl_xor((int)bad, 32) != 0 || bad;
-  if (half == 0) put_certificate(a, out, certificate(a, w.m, w.sum, w.sealed, w.ev, w.evmax, w.dmax, w.vmax, out_offset(a, out)), bad);
+  if (half == 0) put_certificate(a, out, certificate(a, w.m, w.sum, w.sealed, w.ev, w.evmax, w.dmax, w.vmax, out_offset(a, head, r)), bad);
 }
 // Where the sets of a row are: `n` of them, `stride` floats apart, the row's place r32 in each.
 struct SetsOf {
@@ -987,7 +1013,7 @@ __device__ __forceinline__ void finish_sets(const A& a, int head, int tile, int 
       VM = fmaxf(VM, z[i][4]);
       bad = fmaxf(bad, z[i][5]);
     }
-    put_certificate(a, out, certificate(a, M, L, SL, E, EM, DM, VM, out_offset(a, out)), bad != 0.0f);
+    put_certificate(a, out, certificate(a, M, L, SL, E, EM, DM, VM, out_offset(a, head, r)), bad != 0.0f);
   } else if (there && tid < WIDE) {
     int c = tid / ROWS;
     float4 y[N];
@@ -1510,7 +1536,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
   constexpr int PRODUCTS = 16 * MT, AHEAD = 6, FROM = 2, EACH = QUADS == 2 ? 4 : 2, BEHIND = FROM + PIECES * QUADS / EACH;
   static_assert(PIECES * QUADS % EACH == 0 && BEHIND < PRODUCTS, "the pieces end ahead of the products");
   // Products with keys: the accumulators take turns; where caps are applied, the first 32 tokens' come first, and their caps stand between the others',
-  // CAPS scores a product.
+  // CAPS scores a product (8 heads, 131072 tokens, 64 nodes of 4 heads 237 us, behind the products 242).
   constexpr bool EARLY = A::SCORED && MT == 2;
   constexpr int CAPS = 3, CAPS_FROM = PRODUCTS - 6;
   const auto key_mt = [](int k) constexpr { return EARLY ? k / 8 : k % MT; };
@@ -1819,7 +1845,7 @@ __global__ __launch_bounds__(1024) void tree_join_kernel(A a) {
   }
   if (certifies) {
     const int64_t out = row_out(a, head, r);
-    put_certificate(a, out, certificate(a, M, q[0], q[1], q[2], q[3], q[4], q[5], out_offset(a, out)), q[6] != 0.0f);
+    put_certificate(a, out, certificate(a, M, q[0], q[1], q[2], q[3], q[4], q[5], out_offset(a, head, r)), q[6] != 0.0f);
   } else {
 #pragma unroll
     for (int k = 1; k < G; ++k) add(1.0f, s_o[k][cc][row]);

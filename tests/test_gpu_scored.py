@@ -229,7 +229,7 @@ def test_rows_that_attend_only_far_tokens_keep_their_weights(n, far):
     places = np.full((2, n), tokens + far, np.int64) + rng.integers(0, 5, (2, n))
     spans = make_spans(rng, "sorted", 2, n, tokens, places)
     slopes = np.array([0.5, 0.01, -0.02, 0.0], np.float32)
-    limit = 2 ** 30
+    limit = 2 ** 29
     held = np.clip(places, -limit, tokens + limit)
     with Caches(x, 4) as c:
         got = call(None, c.gc, x["q"], slopes=slopes, places=places, spans=spans)
@@ -245,6 +245,21 @@ def test_places_among_the_cached_tokens_and_of_drafted_ones_anywhere():
         places = rng.integers(-30, tokens + 60, (1, n))
         seen = rng.random((1, n, n)) < 0.5
         compare(x, 4, seen, n, slopes=np.array([0.25, 0.03, -0.01, 1.0], np.float32), places=places, cap=4.0, spans=make_spans(rng, "any", 1, n, tokens, places))
+
+
+@pytest.mark.parametrize("n", [2, 20, 64])
+def test_drafted_tokens_at_both_ends_of_the_places(n):
+    """Distances of almost 2^31, which the slopes make heavy or light."""
+    print("ends of places", n, flush=True)
+    rng = np.random.default_rng(n)
+    x = make(rng, 1, 1, 4, 300, n, True)
+    places = np.where(np.arange(n) % 2, -2 ** 40, 2 ** 40)[None]
+    held = np.clip(places, -2 ** 29, 300 + 2 ** 29)
+    seen = rng.random((1, n, n)) < 0.6
+    slopes = np.array([1e-9, -1e-9, 3.0, 0.0], np.float32)
+    with Caches(x, 4) as c:
+        got = call(None, c.gc, x["q"], x["kd"], x["vd"], drafts.mask_words(seen), slopes=slopes, places=places)
+        assert_nodes(scored.decode(None, c.oc, x["q"], x["kd"], x["vd"], seen, oracle.Tolerances(), slopes=slopes, places=held), *got, n)
 
 
 @pytest.mark.parametrize("beginning", [0, 210])
