@@ -247,7 +247,8 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
     zero_undefined(rows, rows.q);
   }
 
-  uint32_t open = 0u;   // what the lane's row has attended
+  uint32_t open = 0u;     // what the lane's row has attended
+  bool partial = false;   // PLACED: some row does not attend all of the blocks whose widths have come
   for (int turn = 0; u < units; u += WAVES, ++turn) {
     const int pair = pair_at(u);
     uint32_t there = (int64_t)pair * 2 + vb < a.nb ? 0xffu : 0u;
@@ -255,7 +256,7 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
     bool masked = (int64_t)pair * 2 + 2 > a.nb;
     if constexpr (A::PLACED)
       if (spans && !active.open(pair * 2 * BLK, (pair + 1) * 2 * BLK)) {
-        masked = true;
+        masked = partial = true;
         there &= span_bits(lds.span[n16], (pair * 4 + g) * 8);
       }
     if constexpr (A::PLACED) {
@@ -306,11 +307,12 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int s = min(g * 4 + r, last);
-        bool some = true;
+        float x = d[r];
         if constexpr (A::PLACED)
-          if (spans) some = span_bits(lds.span[n16], (pair_at(first + (s >> 1) * WAVES) * 2 + (s & 1)) * BLK) != 0u;
-        if (some) rows.dmax = fmaxf(rows.dmax, d[r]);
+          if (partial) x = some_of(lds.span[n16], pair_at(first + (s >> 1) * WAVES) * 2 + (s & 1)) ? x : 0.0f;
+        rows.dmax = fmaxf(rows.dmax, x);
       }
+      partial = false;
       wave_sync();
     }
     f32x8 s[1] = {both(x0, x1)};
@@ -328,6 +330,7 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
     load_values(u + WAVES);
     wave_sync();
   }
+  if constexpr (A::PLACED) rows.dmax = rows.idle ? 0.0f : rows.dmax;
   rows.sealed = rows.sum;
   // The other tokens, 32 to a wave: dealt to the workgroups from the last one down.
   for (int t0 = (a.nsplit - 1 - split) * L_EXACT; t0 < a.trail + a.drafts(); t0 += a.nsplit * L_EXACT) {

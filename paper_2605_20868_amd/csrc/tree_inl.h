@@ -231,6 +231,10 @@ __device__ __forceinline__ Spans spans_among(const SpansGiven& x, int first, int
   if (s.lo1 >= s.hi1) s.lo1 = s.hi1 = 0;
   return s;
 }
+// Whether a token of block k is in them.
+__device__ __forceinline__ bool some_of(const Spans& s, int k) {
+  return (k >= s.lo0 / BLK && k < (s.hi0 + BLK - 1) / BLK) || (k >= s.lo1 / BLK && k < (s.hi1 + BLK - 1) / BLK);
+}
 // The open ones of the 16 tokens from t on.
 __device__ __forceinline__ uint32_t span_bits(const Spans& s, int t) {
   const auto below = [&](int x) { return (1u << min(max(x - t, 0), BLK)) - 1u; };   // tokens ahead of x
@@ -630,9 +634,9 @@ __device__ __forceinline__ void attend32(const A& a, RowsOf<A>& w, uint32_t bits
 }
 
 // Delta of 32 blocks (or of fewer, repeated); width(ks): the A operand
-// open(slot): whether the lane's row attends a token of the block in that place
-template <typename Width, typename Open>
-__device__ __forceinline__ void bound_scores(TreeRows& w, Width width, bool masked, Open open) {
+// spans, where not null: only blocks of which the lane's row attends a token; block_of(slot): the block in that place
+template <typename Width, typename BlockOf>
+__device__ __forceinline__ void bound_scores(TreeRows& w, Width width, const Spans* spans, BlockOf block_of) {
   f32x16 d;
 #pragma unroll
   for (int r = 0; r < 16; ++r) d[r] = 0.0f;
@@ -645,8 +649,11 @@ __device__ __forceinline__ void bound_scores(TreeRows& w, Width width, bool mask
     d = __builtin_amdgcn_mfma_f32_32x32x16_f16(width(ks), __builtin_bit_cast(f16x8, y), d, 0, 0, 0);
   }
 #pragma unroll
-  for (int r = 0; r < 16; ++r)
-    if (!masked || open((r & 3) + 8 * (r >> 2) + 4 * (int)((threadIdx.x >> 5) & 1))) w.dmax = fmaxf(w.dmax, d[r]);
+  for (int r = 0; r < 16; ++r) {
+    float x = d[r];
+    if (spans != nullptr) x = some_of(*spans, block_of((r & 3) + 8 * (r >> 2) + 4 * (int)((threadIdx.x >> 5) & 1))) ? x : 0.0f;
+    w.dmax = fmaxf(w.dmax, x);
+  }
 }
 
 // place of token t of block `blk` among the keys of a tile: the A operand's rows are dealt to two blocks
@@ -1142,14 +1149,15 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
 
   const float* const sg = reinterpret_cast<const float*>(wave + FEW_KM) + bsel * FEW_KM_BLK + half * FEW_KM_HALF;
   const uint8_t* const sc = wave + FEW_VM + half * FEW_VM_BLK + (n32 >> 4) * 64;
-  uint32_t open = 0u;   // PLACED: tokens of sealed blocks that the lane's row has attended
+  uint32_t open = 0u;       // PLACED: tokens of sealed blocks that the lane's row has attended
+  bool partial = false;     // PLACED: some row does not attend all of the blocks whose widths have come
   for (int turn = 0; u < units; u += step, ++turn) {
     const int pair = pair_at(u);
     uint32_t there = 0xffffu;
     bool masked = (int64_t)pair * 2 + 2 > a.nb;
     if constexpr (A::PLACED) {
       if (spans && !active.open(pair * 2 * BLK, (pair + 1) * 2 * BLK)) {
-        masked = true;
+        masked = partial = true;
         there = span_bits(lds.span[n32], (pair * 2 + half) * BLK);
       }
       if ((int64_t)pair * 2 + half >= a.nb || rows.idle) there = 0u;
@@ -1207,12 +1215,18 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
       wave_sync();
       const int blk = min(n32, (turn & 15) * 2 + 1);
       const int first = u - (turn & 15) * step, last = (turn & 15) * 2 + 1;
-      bound_scores(
-          rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(wave + FEW_W + (half * 8 + ks) * FEW_W_RUN + blk * 16); }, spans,
-          [&](int slot) {
-            slot = min(slot, last);
-            return span_bits(lds.span[n32], (pair_at(first + (slot >> 1) * step) * 2 + (slot & 1)) * BLK) != 0u;
-          });
+      const auto width = [&](int ks) { return *reinterpret_cast<const f16x8*>(wave + FEW_W + (half * 8 + ks) * FEW_W_RUN + blk * 16); };
+      const auto block_of = [&](int slot) {
+        slot = min(slot, last);
+        return pair_at(first + (slot >> 1) * step) * 2 + (slot & 1);
+      };
+      if (partial) {
+        const Spans s = lds.span[n32];
+        bound_scores(rows, width, &s, block_of);
+      } else {
+        bound_scores(rows, width, nullptr, block_of);
+      }
+      partial = false;
       wave_sync();
     }
     if constexpr (A::SCORED) score<16>(a, rows, x[0], RunFar<BLK>(rows, (pair * 2 + half) * BLK));
@@ -1232,6 +1246,7 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
     load_values(u + step);
     wave_sync();
   }
+  if constexpr (A::PLACED) rows.dmax = rows.idle ? 0.0f : rows.dmax;
   rows.sealed = rows.sum;
   if constexpr (!A::PLACED) open = split * FEW_WAVES + w < units;
   // The other tokens, dealt from the workgroup on whose turn is the next, which fetches them together; as many of its waves as they have pairs of blocks attend them.
@@ -1428,6 +1443,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
   }
   int fresh = 0, ring = 0;   // blocks whose widths have come into the half `ring`
   int ring_from = from;      // ... from this tile on
+  bool partial = false;      // PLACED: some row of the wave does not attend all of them
   uint32_t open = 0u;        // PLACED: tokens of sealed blocks that the lane's row has attended
   int buf = 0;
   __syncthreads();
@@ -1544,6 +1560,11 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
   const auto sealed_tiles = [&](auto keys) {
     for (int turn = 0; u < units; ++u, buf ^= 1, ++turn) {
       const bool last = u + 1 >= units, full = fresh == 32;
+      bool some = false;   // PLACED: a row of the wave does not attend all of the tile
+      if constexpr (A::PLACED) {
+        some = spans && !active.open(tile_at(u) * TOK, (tile_at(u) + 1) * TOK);
+        partial |= some;
+      }
       const int ring1 = full ? ring ^ 1 : ring, slot = full ? 0 : fresh;   // where the next tile's widths go
       const uint4* const s_k = reinterpret_cast<const uint4*>(s_main + buf * S::TILE);
       const uint4* const s_v = reinterpret_cast<const uint4*>(s_main + (buf ^ 1) * S::TILE) + 16 * TOK;
@@ -1604,13 +1625,20 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
       if (full || last) {
         // (up to the last block that has come: on the last tile, other waves write the first record's widths behind it meanwhile)
         const int blk = min(n32, fresh - 1);
-        if (wt == 0)
-          bound_scores(
-              rows, [&](int ks) { return *reinterpret_cast<const f16x8*>(width_at(ring, half * 8 + ks, blk)); }, spans,
-              [&](int slot) {
-                slot = min(slot, fresh - 1);
-                return span_bits(lds.span[w][n32], (tile_at(ring_from + slot / BLKS) * BLKS + slot % BLKS) * BLK) != 0u;
-              });
+        const auto width = [&](int ks) { return *reinterpret_cast<const f16x8*>(width_at(ring, half * 8 + ks, blk)); };
+        const auto block_of = [&](int slot) {
+          slot = min(slot, fresh - 1);
+          return tile_at(ring_from + slot / BLKS) * BLKS + slot % BLKS;
+        };
+        if (wt == 0) {
+          if (partial) {
+            const Spans s = lds.span[w][n32];
+            bound_scores(rows, width, &s, block_of);
+          } else {
+            bound_scores(rows, width, nullptr, block_of);
+          }
+        }
+        partial = false;
       }
       if (full) ring_from = u + 1;
       ring = ring1;
@@ -1621,7 +1649,6 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
         const int tile = tile_at(u);
         uint32_t there[MT];
         bool masked = (int64_t)(tile + 1) * BLKS > a.nb;
-        const bool some = spans && !active.open(tile * TOK, (tile + 1) * TOK);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
           const int in = (wt * MT + mt) * 2 + half, blk = tile * BLKS + in;
@@ -1667,6 +1694,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
     }
     add_values(buf ^ 1);
   }
+  if constexpr (A::PLACED) rows.dmax = rows.idle ? 0.0f : rows.dmax;
   rows.sealed = rows.sum;
   if constexpr (!A::PLACED) open = fresh != 0 && (S::WT == 1 || (int64_t)from * BLKS + wt * MT * 2 < a.nb);   // it has had tiles, and the wave a block of the first
   // the other tokens' tiles: dealt to the workgroups from the last one down
