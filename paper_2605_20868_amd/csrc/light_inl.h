@@ -164,9 +164,9 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
   uint8_t* const wave = reinterpret_cast<uint8_t*>(lds.set[w]);
   std::conditional_t<A::SCORED, Scored<LightRows>, LightRows> rows;
   const int last_row = a.n * a.group - 1;
-  rows.node = min(n16, last_row) / a.group;
+  rows.node = a.node_of(min(n16, last_row));
   // rows 4 w .. 4 w + 3 of the queries by each of four waves: 16 lanes a row
-  const int q_row = min(4 * (w & 3) + g, last_row), q_node = q_row / a.group;
+  const int q_row = min(4 * (w & 3) + g, last_row), q_node = a.node_of(q_row);
   const uint4 q_in = ld16_any(a.q + (((int64_t)b * a.n + q_node) * a.n_kv * a.group + kvh * a.group + (q_row - q_node * a.group)) * D + n16 * 8);
 
   const uint8_t* const base = a.t1 + head * a.nq_cap * QUAD_BYTES;

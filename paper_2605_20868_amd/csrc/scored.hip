@@ -34,7 +34,7 @@ struct JoinArgs : SetArgs<SCORES> {
   __device__ SetsOfTwo sets_of(const float* sets, int head, int r32, int r) const {
     r = min(r, this->n * this->group - 1);
     const int b = head / this->n_kv, kvh = head - b * this->n_kv;
-    const int node = r / this->group, seq = node / this->each, row = (node - seq * this->each) * this->group + (r - node * this->group);
+    const int node = this->node_of(r), seq = node / this->each, row = (node - seq * this->each) * this->group + (r - node * this->group);
     const int64_t own_head = ((int64_t)b * (this->n / this->each) + seq) * this->n_kv + kvh;
     return {SetsOf{sets, T_FLOATS, this->nsplit, r32}, SetsOf{own + (own_head * own_tiles + row / T_ROWS) * own_sets * T_FLOATS, T_FLOATS, own_sets, row % T_ROWS}};
   }

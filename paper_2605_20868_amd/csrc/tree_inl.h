@@ -83,6 +83,7 @@ struct TreeArgs {
   uint32_t* flags;
   cqa_tolerances tol;
   __device__ int drafts() const { return n; }
+  __device__ int node_of(int row) const { return row / group; }
   __device__ SetsOf sets_of(const float* sets, int head, int r32, int r) const;
   __device__ float unit() const { return SCORE; }        // exponents of 2 that a unit of score is worth
   __device__ float half_scale() const { return HALF_SCORE; }
@@ -119,6 +120,7 @@ struct SetArgs : TreeArgs {
   const int64_t* places;   // [Bt][n]
   const int64_t* spans;    // [Bt][n][4]
   __device__ int drafts() const { return nd; }
+  __device__ int node_of(int row) const { return row >> (group >> 1); }   // 1, 2 or 4 of them
   __device__ float unit() const { return SCORED ? per_unit : SCORE; }
   __device__ float half_scale() const { return SCORED ? 0.5f * scale : HALF_SCORE; }
 };
@@ -415,7 +417,7 @@ __device__ __forceinline__ Active active_units(const Hull& h, int sealed, int to
 constexpr int Q_ROW = D * 2 + 16, Q_TILE = T_ROWS * Q_ROW;
 template <typename A>
 __device__ __forceinline__ uint4 fetch_rows(const A& a, int b, int kvh, int first) {
-  const int l = threadIdx.x & 63, r = min(first + (l >> 4), a.n * a.group - 1), node = r / a.group;
+  const int l = threadIdx.x & 63, r = min(first + (l >> 4), a.n * a.group - 1), node = a.node_of(r);
   return ld16_any(a.q + (((int64_t)b * a.n + node) * a.n_kv * a.group + kvh * a.group + (r - node * a.group)) * D + (l & 15) * 8);
 }
 __device__ __forceinline__ void keep_rows(uint8_t* at, int row, uint4 x) {
@@ -438,7 +440,7 @@ __device__ __forceinline__ void zero_undefined(Rows& w, f16x8 (&q)[N]) {
 template <typename A>
 __device__ __forceinline__ void start_rows(RowsOf<A>& s, const A& a, int tile, const uint8_t* at) {
   const int l = threadIdx.x & 63;
-  s.node = min(tile * T_ROWS + (l & 31), a.n * a.group - 1) / a.group;
+  s.node = a.node_of(min(tile * T_ROWS + (l & 31), a.n * a.group - 1));
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) s.q[ks] = *reinterpret_cast<const f16x8*>(at + (l & 31) * Q_ROW + ((l >> 5) * 8 + ks) * 16);
   s.m = -INFINITY;
@@ -889,13 +891,13 @@ __device__ __forceinline__ void join_sets(const A& a, const float* sets, int str
 // Row r of a KV group among the outputs.
 template <typename A>
 __device__ __forceinline__ int64_t row_out(const A& a, int head, int r) {
-  const int b = head / a.n_kv, kvh = head - b * a.n_kv, node = r / a.group;
+  const int b = head / a.n_kv, kvh = head - b * a.n_kv, node = a.node_of(r);
   return ((int64_t)b * a.n + node) * a.n_kv * a.group + kvh * a.group + (r - node * a.group);
 }
 template <typename A>
 __device__ __forceinline__ float out_offset(const A& a, int head, int r) {
   if constexpr (A::SCORED) {
-    const int b = head / a.n_kv, kvh = head - b * a.n_kv, node = r / a.group;
+    const int b = head / a.n_kv, kvh = head - b * a.n_kv, node = a.node_of(r);
     return row_offset(a, (int64_t)b * a.n + node, kvh * a.group + (r - node * a.group));
   }
   return 0.0f;
@@ -1099,7 +1101,7 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
   Spans mine;
   bool spans = false;
   if constexpr (A::PLACED) {
-    rows.node = min(tile * T_ROWS + n32, a.n * a.group - 1) / a.group;
+    rows.node = a.node_of(min(tile * T_ROWS + n32, a.n * a.group - 1));
     score_rows(rows, a, b, kvh, tile, (int)a.nb * BLK + a.trail, lds.span, mine);   // (every wave the same)
     spans = a.spans != nullptr;
     if (spans) {
@@ -1377,7 +1379,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
   Active active;
   bool spans = false;
   if constexpr (A::PLACED) {
-    rows.node = min((tile0 + wr) * T_ROWS + n32, a.n * a.group - 1) / a.group;
+    rows.node = a.node_of(min((tile0 + wr) * T_ROWS + n32, a.n * a.group - 1));
     Spans mine;
     score_rows(rows, a, b, kvh, tile0 + wr, (int)a.nb * BLK + a.trail, lds.span[w], mine);
     spans = a.spans != nullptr;
