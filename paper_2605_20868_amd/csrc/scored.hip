@@ -118,6 +118,13 @@ static void put_scores(SetArgs<SCORES>& a, const cqa_scoring& s, bool many) {
   a.cap = s.cap;
   a.cap_kind = s.cap == 0.0f ? CAP_NONE : (many && s.cap <= LOW_CAPS ? CAP_LOW : CAP_HIGH);
   a.gain = a.cap_kind == CAP_NONE ? 0.0f : (a.cap_kind == CAP_LOW ? 2.0f * LOG2E : 1.0f) * (a.scale / s.cap);
+  if (a.cap_kind == CAP_HIGH) {
+    const bool powers = a.gain >= 1e-4f && a.gain <= 1e4f;   // the seventh, by the smallest coefficient, is a normal number
+    a.series_end = SERIES_END / a.gain;
+    a.pre = powers ? 1.0f : a.gain;
+    double power = powers ? a.gain : 1.0;
+    for (int i = 0; i < 4; ++i, power *= powers ? (double)a.gain * a.gain : 1.0) a.series[i] = (float)(SERIES[i] * power);
+  }
   a.per_unit = LOG2E * (a.cap_kind == CAP_NONE ? a.scale : (a.cap_kind == CAP_LOW ? 2.0f * s.cap : s.cap));
   a.offset = a.cap_kind == CAP_LOW ? s.cap : 0.0f;
   a.slopes = s.slopes_dev;
@@ -170,7 +177,7 @@ static int32_t run(const Cache* shared, const Cache* c, int layer, const NodeCal
   const Pass own = put_pass(a, c, layer, call.n, drafts, (int)beginning);
   const Pass theirs = has_shared ? put_pass(b, shared, layer, call.n * (c->desc.batch / shared->desc.batch), 0, 0) : Pass{};
   if constexpr (SCORES != PLAIN) {
-    const bool many = (has_own && own.shape.rows > 32) || (has_shared && theirs.shape.rows > 32);
+    const bool many = (has_own && own.shape.rows >= 128) || (has_shared && theirs.shape.rows >= 128);
     put_scores(a, *call.scoring, many);
     put_scores(b, *call.scoring, many);
   }

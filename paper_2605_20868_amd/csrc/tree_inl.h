@@ -94,9 +94,10 @@ struct TreeArgs {
 //   What the softmax works on is the score in units of its own, `per_unit` exponents of 2 each, and less a constant of the row:
 //   CAP_NONE   q . k
 //   CAP_LOW    -1 / (1 + e^(2 x / cap)) = (tanh(x / cap) - 1) / 2, an exponential and a reciprocal: off by 2^-24 of a unit, 2 cap
-//   CAP_HIGH   tanh(x / cap), relatively exact, for some eight operations more
-// LOW where a pass reconstructs for many rows at once, which the scores' operations bound, and the cap is at most LOW_CAPS.  (8 heads, 131072 tokens, 64 nodes
-// of 4 heads: LOW 222 us, HIGH 287; one token: 66.5, 68.0.)
+//   CAP_HIGH   tanh(x / cap), relatively exact: a series up to 0.36, which is one operation more, beside 1 - 2 / (1 + e^(2 x / cap)) where a wave has larger ones
+// LOW where a pass reconstructs for 128 or 256 rows at once, which the scores' operations bound, and the cap is at most LOW_CAPS (us a call in a graph, LOW and
+// HIGH: 8 heads, 131072 tokens, 64 nodes of 4 heads 222, 287; 2 x 8 heads, 16000 tokens, 20 nodes of 4 50.5, 57.0; 64 rows, 8 heads, 32000 tokens 44, 42; one token,
+// 131072 tokens 66.5, 66.7).
 // and the bias counts from the distance `near` of the row's nearest attended token (the farthest, under a negative slope), so that the scores of a
 // row that attends far tokens only keep their bits.
 enum { CAP_NONE = 0, CAP_LOW, CAP_HIGH };
@@ -114,6 +115,8 @@ struct SetArgs : TreeArgs {
   int drafted;             // the sequences have drafted tokens, in this pass or another
   int cap_kind;
   float gain;              // x / cap by q . k: CAP_LOW in exponents of 2, twice
+  // CAP_HIGH: the series by powers of pre q . k, 1, 3, ...; it holds for q . k up to series_end.  pre is 1, or the gain, whose powers no coefficients hold
+  float series[4], series_end, pre;
   float per_unit, offset;  // offset: of the score, where the unit's zero is
   float cap, scale;
   const float* slopes;     // [Hq]
@@ -304,26 +307,41 @@ __device__ __forceinline__ float row_offset(const A& a, int64_t node, int q_head
   }
   return 0.0f;
 }
-// A lane's products with N tokens become scores.  far(r): |place - token| - near.
-// (A series of six coefficients where all of a wave's products are in its range, which is relatively exact at the small ones, is two operations a
-// score more than CAP_LOW: 8 heads, 131072 tokens, 64 nodes of 4 heads 293 us, 241.)
+// tanh(x) for |x| up to 0.36: x times a polynomial in x^2, within 4.4e-8 (weighted least squares, equal ripples), 1.5e-7 in FP32.
+constexpr float SERIES_END = 0.36f;
+constexpr float SERIES[4] = {0.99999994f, -0.33332261f, 0.13291534f, -0.048687924f};
+template <typename A>
+__device__ __forceinline__ float tanh_series(const A& a, float s) {
+  const float y = s * s;
+  return s * fmaf(y, fmaf(y, fmaf(y, a.series[3], a.series[2]), a.series[1]), a.series[0]);
+}
+// A lane's products with N tokens become scores.  far(r): |place - token| - near.  A row's numbers do not depend on the form that the others of its wave need.
 template <typename A>
 __device__ __forceinline__ float cap_low(const A& a, float s) { return __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s * a.gain)); }
-// low_done: CAP_LOW has been applied.
-template <int N, typename A, typename Rows, typename V, typename Far>
+// low_done: CAP_LOW has been applied.  NEAR: CAP_HIGH looks whether the series is enough (a kernel without registers for both forms does not).
+template <int N, bool NEAR = true, typename A, typename Rows, typename V, typename Far>
 __device__ __forceinline__ void score(const A& a, const Rows& w, V& s, Far far, bool low_done = false) {
   if (a.cap_kind == CAP_LOW) {
     if (!low_done)
 #pragma unroll
       for (int r = 0; r < N; ++r) s[r] = cap_low(a, s[r]);
   } else if (a.cap_kind == CAP_HIGH) {
+    float most = 0.0f;
 #pragma unroll
-    for (int r = 0; r < N; ++r) {
-      // (1 - 2 / (1 + e^2x) loses its relative accuracy near zero, where five terms of the series have it)
-      const float x = s[r] * a.gain, y = x * x;
-      const float low = x * fmaf(y, fmaf(y, fmaf(y, fmaf(y, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
-      const float high = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f / LN2))), 1.0f);
-      s[r] = fabsf(x) < 0.25f ? low : high;
+    for (int r = 0; r < N; ++r) most = fmaxf(most, fabsf(s[r]));
+    if (NEAR && a.pre == 1.0f && !__any(most > a.series_end)) {
+#pragma unroll
+      for (int r = 0; r < N; ++r) {
+        s[r] = tanh_series(a, s[r]);
+        if (r % 8 == 7) __builtin_amdgcn_sched_barrier(0);   // (all at once took 50 registers more than there are)
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < N; ++r) {
+        const float high = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[r] * a.gain * (2.0f / LN2))), 1.0f);
+        s[r] = fabsf(s[r]) <= a.series_end ? tanh_series(a, s[r] * a.pre) : high;
+        if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+      }
     }
   }
   if constexpr (A::PLACED)
@@ -630,7 +648,7 @@ __device__ __forceinline__ void attend32(const A& a, RowsOf<A>& w, uint32_t bits
   f32x16 s[1];
   uint32_t p[1][8];
   scores32(w, s[0], key);
-  if constexpr (A::SCORED) score<16>(a, w, s[0], [&](int r) { return (float)(abs(w.place - places[r]) - w.near); });
+  if constexpr (A::SCORED) score<16, false>(a, w, s[0], [&](int r) { return (float)(abs(w.place - places[r]) - w.near); });
   weigh32<1>(a, w, s, p, true, [&](int) { return bits; }, [&](int) { return 0.0f; });
   values32(w, p[0], value);
 }
@@ -1231,7 +1249,7 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
       partial = false;
       wave_sync();
     }
-    if constexpr (A::SCORED) score<16>(a, rows, x[0], RunFar<BLK>(rows, (pair * 2 + half) * BLK));
+    if constexpr (A::SCORED) score<16, !A::PLACED>(a, rows, x[0], RunFar<BLK>(rows, (pair * 2 + half) * BLK));
     weigh32<1>(
         a, rows, x, p, masked, [&](int) { return A::PLACED ? there : ((int64_t)u * 2 + half < a.nb ? 0xffffu : 0u); }, [&](int) { return eta; }, silent_of(rows));
     each<8>([&](auto i_) {
@@ -1658,7 +1676,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
           if (blk >= a.nb || rows.idle) there[mt] = 0u;
           open |= there[mt];
           rows.vmax = fmaxf(rows.vmax, there[mt] == 0u ? 0.0f : lds.nu[turn & 3][in]);
-          score<16>(a, rows, sc[mt], RunFar<BLK>(rows, blk * BLK), EARLY && mt == 0);
+          score<16, MT == 1>(a, rows, sc[mt], RunFar<BLK>(rows, blk * BLK), EARLY && mt == 0);
         }
         masked |= some;
         weigh32<MT>(
@@ -1666,7 +1684,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
       } else {
         if constexpr (A::SCORED)
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) score<16>(a, rows, sc[mt], [](int) { return 0.0f; }, EARLY && mt == 0);
+          for (int mt = 0; mt < MT; ++mt) score<16, MT == 1>(a, rows, sc[mt], [](int) { return 0.0f; }, EARLY && mt == 0);
         weigh32<MT>(
             a, rows, sc, p, (int64_t)(u + 1) * BLKS > a.nb, [&](int mt) { return (int64_t)u * BLKS + (wt * MT + mt) * 2 + half < a.nb ? 0xffffu : 0u; },
             [&](int mt) { return s_eta[turn & 3][(wt * MT + mt) * 2 + half]; });
