@@ -572,7 +572,10 @@ int32_t cqa_tree_workspace_bytes(const cqa_cache* c, int32_t n_draft, int64_t* b
  *   spans_dev   int64 [batch][n_nodes][4], or NULL: every cached token.  Node i attends the cached tokens j with s[0] <= j < s[1] or
  *               s[2] <= j < s[3], each once where the spans overlap; a span may be empty (to <= from) or reach beyond the cached tokens.  Sliding
  *               windows with the first tokens kept, left-padded batches and packed documents are such spans; what no node of a
- *               sequence attends between its two spans, or around them, is not read.
+ *               sequence attends between its two spans, or around them, is not read.  Cached keys and values that are not finite (padding that an
+ *               idle row computed) do not reach a node whose spans leave them out, but by its certificate where it attends others of the
+ *               same block of 16; a node that attends a trailing one, or a sealed one of a block whose steps or scales are not finite for
+ *               it, returns NaN and PRECOND
  * Slopes, places and spans are read on the device. */
 typedef struct cqa_scoring {
   float scale;

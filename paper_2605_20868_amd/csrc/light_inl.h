@@ -264,11 +264,18 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
       there = silent ? 0u : there;
     }
     open |= there;
+    float eta = value_error(an);
+    if constexpr (A::PLACED)
+      if (spans) {
+        uint32_t flawed[2];
+        mend_pair(km0, km1, vm, flawed);
+        if (there & (vb ? flawed[1] : flawed[0]) >> (g & 1) * 8) rows.sum = NAN;   // stays
+        eta = there == 0u ? 0.0f : eta;
+      }
     // metadata
     reinterpret_cast<uint4*>(wave + L_KM)[l] = km0;
     reinterpret_cast<uint4*>(wave + L_KM + L_KM_BLK)[l] = km1;
     *reinterpret_cast<uint4*>(wave + L_VM + (l >> 5) * L_VM_BLK + (l & 31) * 16) = paired(vm);
-    const float eta = value_error(an);
     rows.vmax = fmaxf(rows.vmax, A::PLACED && there == 0u ? 0.0f : an.y);
     load_meta(u + WAVES);
     wave_sync();

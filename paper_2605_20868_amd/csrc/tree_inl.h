@@ -442,6 +442,59 @@ __device__ __forceinline__ void keep_rows(uint8_t* at, int row, uint4 x) {
   const int l = threadIdx.x & 63;
   *reinterpret_cast<uint4*>(at + (row + (l >> 4)) * Q_ROW + (l & 15) * 16) = x;
 }
+// Metadata of sealed blocks some of whose originals were not finite (padding that nobody attends).  Where the spans leave such tokens out, a weight of zero must
+// not meet their numbers: they become zeros, and the rows that do attend them get a sum that is no number.
+// FLOATS: four steps or zero points, else the scales or offsets of eight tokens; whether all are finite.
+template <bool FLOATS>
+__device__ __forceinline__ bool sound(uint4 x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  if constexpr (FLOATS) {
+    float none = 0.0f;   // stays
+#pragma unroll
+    for (int i = 0; i < 4; ++i) none = fmaf(0.0f, __uint_as_float(w[i]), none);
+    return none == 0.0f;
+  }
+  const f16x2 zero = {(_Float16)0.0f, (_Float16)0.0f};
+  f16x2 none = zero;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) none = __builtin_elementwise_fma(zero, __builtin_bit_cast(f16x2, w[i]), none);
+  return (__builtin_bit_cast(uint32_t, none) & 0x7fff7fffu) == 0u;
+}
+__device__ __forceinline__ uint4 mended_floats(uint4 x) {
+  const auto keep = [](uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u ? 0u : w; };
+  return make_uint4(keep(x.x), keep(x.y), keep(x.z), keep(x.w));
+}
+// Of eight tokens' scales or offsets; flaws: a bit for each token whose number is not finite.
+__device__ __forceinline__ uint4 mended_halves(uint4 x, uint32_t& flaws) {
+  flaws = 0u;
+  const auto keep = [&](uint32_t w, int i) {
+    const uint32_t lo = (w & 0x7c00u) == 0x7c00u, hi = (w & 0x7c000000u) == 0x7c000000u;
+    flaws |= lo << i | hi << (i + 1);
+    return (lo ? 0u : w & 0xffffu) | (hi ? 0u : w & 0xffff0000u);
+  };
+  return make_uint4(keep(x.x, 0), keep(x.y, 2), keep(x.z, 4), keep(x.w, 6));
+}
+// The flawed ones of a block's 16 tokens; flaws: lane p of 32 (kind, octet, group) those of its octet.  Lanes 32 further: another block's.
+__device__ __forceinline__ uint32_t flawed_tokens(uint32_t flaws, int block) {
+  uint32_t bits = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t of = (uint32_t)(__ballot(flaws >> i & 1u) >> (32 * block));
+    bits |= (uint32_t)((of & 0x00ff00ffu) != 0u) << i | (uint32_t)((of & 0xff00ff00u) != 0u) << (8 + i);
+  }
+  return bits;
+}
+// A pair of blocks' metadata, of a wave; the flawed tokens of either block.
+__device__ __forceinline__ void mend_pair(uint4& km0, uint4& km1, uint4& vm, uint32_t (&flawed)[2]) {
+  flawed[0] = flawed[1] = 0u;
+  const bool k0 = sound<true>(km0), k1 = sound<true>(km1), v = sound<false>(vm);
+  if (__all(k0 & k1 & v)) return;
+  uint32_t flaws;
+  vm = mended_halves(vm, flaws);
+  km0 = mended_floats(km0), km1 = mended_floats(km1);
+  flawed[0] = __all(k0) ? flawed_tokens(flaws, 0) : 0xffffu;
+  flawed[1] = __all(k1) ? flawed_tokens(flaws, 1) : 0xffffu;
+}
 // A query or a slope that is not finite (a slope of more than 10^28 with it, for distances are numbers too): zeros, which nothing passes on; the row's
 // sum is no number at the end.
 template <typename Rows, int N>
@@ -1183,13 +1236,20 @@ __device__ __forceinline__ void attend_few(const A& a, int64_t head, int split, 
       if ((int64_t)pair * 2 + half >= a.nb || rows.idle) there = 0u;
       open |= there;
     }
+    float eta = value_error(an);
+    if constexpr (A::PLACED)
+      if (spans) {
+        uint32_t flawed[2];
+        mend_pair(km0, km1, vm, flawed);
+        if (there & (half ? flawed[1] : flawed[0])) rows.sum = NAN;   // stays
+        eta = there == 0u ? 0.0f : eta;
+      }
     // metadata: sigma and z by (block, kind, half of the channels), scales and offsets by block
     float* const skm = reinterpret_cast<float*>(wave + FEW_KM);
     float* const at = skm + half * FEW_KM_KIND + ((l >> 4) & 1) * FEW_KM_HALF + (l & 15) * 4;
     *reinterpret_cast<uint4*>(at) = km0;
     *reinterpret_cast<uint4*>(at + FEW_KM_BLK) = km1;
     *reinterpret_cast<uint4*>(wave + FEW_VM + half * FEW_VM_BLK + n32 * 16) = paired(vm);
-    const float eta = value_error(an);
     rows.vmax = fmaxf(rows.vmax, A::PLACED && there == 0u ? 0.0f : an.y);
     load_meta(u + step);
     wave_sync();
@@ -1369,6 +1429,7 @@ struct ManyLds {
   float* norm;                                  // [TOK]
   uint8_t* bad;                                 // [TOK]
   float (*nu)[ManyShape<WR>::BLKS];             // [4], PLACED
+  uint32_t (*flawed)[2][ManyShape<WR>::BLKS];   // [4], PLACED: by keys, by values
   int* place;                                   // [TOK], PLACED
   Spans (*span)[T_ROWS];                        // [8], PLACED
 };
@@ -1478,7 +1539,21 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
   const auto value_of = [&](const uint4* s_v, int blk, int oct, int ct) { return __builtin_bit_cast(f16x8, s_v[(blk * 2 + oct) * D + ct * 32 + n32]); };
   // The wave's part of a tile, keys and widths and eta, or values.  Metadata go through LDS (stage): 512 bytes of either kind, the
   // second one (zero points, offsets) 544 bytes behind the first.
-  const auto stage = [&](auto keys, int qd) {
+  const auto stage = [&](auto keys, int qd, int turn) {
+    if constexpr (A::PLACED)
+      if (spans) {
+        uint32_t flawed = 0u;
+        if (!__all(sound<keys.value>(raw[qd][2]))) {
+          if constexpr (keys.value) {
+            raw[qd][2] = mended_floats(raw[qd][2]);
+            flawed = 0xffffu;
+          } else {
+            raw[qd][2] = mended_halves(raw[qd][2], flawed);
+            flawed = flawed_tokens(flawed, 0);
+          }
+        }
+        if (l == 0) lds.flawed[turn & 3][keys.value ? 0 : 1][qd * 4 + wb] = flawed;
+      }
     if constexpr (keys.value)
       *reinterpret_cast<uint4*>(s_meta + (l * 4 + (l >> 4) * 4) * 4) = raw[qd][2];
     else if (half == 0)
@@ -1577,6 +1652,17 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
   constexpr int CAPS = 3, CAPS_FROM = PRODUCTS - 6;
   const auto key_mt = [](int k) constexpr { return EARLY ? k / 8 : k % MT; };
   const auto key_ks = [](int k) constexpr { return EARLY ? k % 8 : k / MT; };
+  // PLACED: rows that attend flawed tokens of the tile before, whose keys and values have both come
+  const auto look_back = [&](int u, int turn) {
+    if (!spans) return;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int in = (wt * MT + mt) * 2 + half;
+      const uint32_t flawed = lds.flawed[turn & 3][0][in] | lds.flawed[turn & 3][1][in];
+      if (__any(flawed != 0u))
+        if (tile_at(u) * BLKS + in < a.nb && (flawed & span_bits(lds.span[w][n32], (tile_at(u) * BLKS + in) * BLK))) rows.sum = NAN;   // stays
+    }
+  };
   const auto sealed_tiles = [&](auto keys) {
     for (int turn = 0; u < units; ++u, buf ^= 1, ++turn) {
       const bool last = u + 1 >= units, full = fresh == 32;
@@ -1611,7 +1697,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
         }
       };
       __builtin_amdgcn_s_setprio(1);
-      stage(keys, 0);
+      stage(keys, 0, keys.value ? turn + 1 : turn);
       each<AHEAD>(operand);
       begin(keys);
       __builtin_amdgcn_sched_barrier(0);
@@ -1625,7 +1711,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
             constexpr int P = (I - FROM) * EACH + k_.value, QD = P / PIECES, J = P % PIECES;
             if constexpr (P < PIECES * QUADS) {
               if constexpr (QD > 0 && J == 0) {
-                stage(keys, QD);
+                stage(keys, QD, keys.value ? turn + 1 : turn);
                 begin(keys);
               }
               reconstruct(keys, std::integral_constant<int, QD>{}, std::integral_constant<int, J>{}, keys.value ? buf ^ 1 : buf, ring1, slot, turn + 1);
@@ -1666,6 +1752,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
       __builtin_amdgcn_s_setprio(0);
       turn_over();
       if constexpr (A::PLACED) {
+        if (turn > 0) look_back(u - 1, turn - 1);
         const int tile = tile_at(u);
         uint32_t there[MT];
         bool masked = (int64_t)(tile + 1) * BLKS > a.nb;
@@ -1680,7 +1767,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
         }
         masked |= some;
         weigh32<MT>(
-            a, rows, sc, p, masked, [&](int mt) { return there[mt]; }, [&](int mt) { return s_eta[turn & 3][(wt * MT + mt) * 2 + half]; }, rows.idle);
+            a, rows, sc, p, masked, [&](int mt) { return there[mt]; }, [&](int mt) { return there[mt] == 0u ? 0.0f : s_eta[turn & 3][(wt * MT + mt) * 2 + half]; }, rows.idle);
       } else {
         if constexpr (A::SCORED)
 #pragma unroll
@@ -1697,7 +1784,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
     for (int i = tid; i < 16 * TOK; i += 512) (reinterpret_cast<uint4*>(s_main + S::TILE) + 16 * TOK)[i] = make_uint4(0u, 0u, 0u, 0u);
     if (w < 4) {
       each<QUADS>([&](auto qd) {
-        stage(std::true_type{}, qd.value);
+        stage(std::true_type{}, qd.value, 0);
         begin(std::true_type{});
         each<PIECES>([&](auto j) { reconstruct(std::true_type{}, qd, j, 0, 0, 0, 0); });
       });
@@ -1713,6 +1800,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
       sealed_tiles(std::false_type{});
     }
     add_values(buf ^ 1);
+    if constexpr (A::PLACED) look_back(units - 1, units - 1 - from);
   }
   if constexpr (A::PLACED) rows.dmax = rows.idle ? 0.0f : rows.dmax;
   rows.sealed = rows.sum;
@@ -1783,11 +1871,12 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(A a) {
   __shared__ __align__(16) uint8_t s_bad[S::TOK];
   if constexpr (A::PLACED) {
     __shared__ float s_nu[4][S::BLKS];
+    __shared__ uint32_t s_flawed[4][2][S::BLKS];
     __shared__ __align__(16) int s_place[S::TOK];
     __shared__ __align__(16) Spans s_span[8][T_ROWS];
-    attend_many<WR>(a, blockIdx.x, blockIdx.y, blockIdx.z, ManyLds<WR>{s_main, s_eta, s_norm, s_bad, s_nu, s_place, s_span});
+    attend_many<WR>(a, blockIdx.x, blockIdx.y, blockIdx.z, ManyLds<WR>{s_main, s_eta, s_norm, s_bad, s_nu, s_flawed, s_place, s_span});
   } else {
-    attend_many<WR>(a, blockIdx.x, blockIdx.y, blockIdx.z, ManyLds<WR>{s_main, s_eta, s_norm, s_bad, nullptr, nullptr, nullptr});
+    attend_many<WR>(a, blockIdx.x, blockIdx.y, blockIdx.z, ManyLds<WR>{s_main, s_eta, s_norm, s_bad, nullptr, nullptr, nullptr, nullptr});
   }
 }
 

@@ -302,6 +302,48 @@ def test_numbers_that_are_not_finite(n, beginning):
             assert (O[1, 0] == 0).all() and (flags[1, 0] == 0).all() and (cert["lse"][1, 0] == -np.inf).all()
 
 
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("n,hkv", [(1, 1), (1, 70), (6, 1), (16, 1), (30, 1), (64, 1), (90, 2)])
+def test_padding_that_is_not_finite(n, hkv, shared):
+    """Cached padding of NaN and infinities, sealed and trailing, before and between what is attended: to the rows that leave it out it is as any
+    other padding, bit for bit, and the rows that attend it are NaN with PRECOND.  (In a block with attended tokens it is NaN, and in its stead the
+    other padding repeats one of them, which leaves the block's steps and errors.)"""
+    print("padding", n, hkv, shared, flush=True)
+    rng = np.random.default_rng(n)
+    bt, tokens, pads = 2, 714, (37, 64)
+    x = make(rng, bt, hkv, 4, tokens, n, False, shared=1 if shared else 0, beginning=150)
+    clean = {k: None if v is None else v.copy() for k, v in x.items()}
+    for name in ("k", "v"):
+        clean[name][0, :, :37] = clean[name][0, :, 37:38]
+        x[name][0, :, :37] = np.nan
+        x[name][0, :, 704:] = np.nan                                              # trailing ones
+    x["k"][1, :, :48, 7::16] = np.inf
+    x["k"][1, :, 20:30] = -np.inf
+    x["v"][1, :, 30:64] = np.where(np.arange(128) % 3 == 0, np.inf, -np.inf)
+    x["v"][1, :, 336:352, 5] = np.inf                                             # a block between the spans
+    lead = 150 if shared else 0
+    spans = np.zeros((bt, n, 4), np.int64)
+    spans[0, :] = [lead + 37, lead + 300, lead + 300, lead + 704]
+    spans[1, :] = [lead + 64, lead + 336, lead + 352, lead + tokens]
+    score = dict(cap=6.0, slopes=slopes_of(4 * hkv, 1))
+    with Caches(clean, 4) as c:
+        good = call(c.shared, c.gc, x["q"], spans=spans, **score)
+        gc = GpuLayerCache(bt, 4 * hkv, hkv, tokens + 16, tier2=False)
+        gc.append(x["k"], x["v"])
+        got = call(c.shared, gc, x["q"], spans=spans, **score)
+        assert same(good, got) and np.isfinite(got[0]).all() and (got[2] == 0).all()
+        some = np.arange(0, n, 3)
+        rest = np.setdiff1d(np.arange(n), some)
+        for first, second in (([lead + 37, lead + 705, 0, 0], [lead + 300, lead + 337, 0, 0]), ([lead, lead + 17, 0, 0], [0, 0, lead + 47, lead + 49])):
+            wide = spans.copy()
+            wide[0, some], wide[1, some] = first, second
+            O, _, flags = call(c.shared, gc, x["q"], spans=wide, **score)
+            assert np.isnan(O[:, some]).all() and (flags[:, some] & 8 != 0).all()
+            # (the other rows' sums are in the order that this call's spans give them)
+            assert np.array_equal(O[:, rest], call(c.shared, c.gc, x["q"], spans=wide, **score)[0][:, rest]) and (flags[:, rest] == 0).all()
+        gc.close()
+
+
 @pytest.mark.parametrize("n,bt,hkv", [(1, 1, 1), (13, 1, 1), (27, 1, 1), (64, 1, 1), (64, 130, 2)])
 def test_spans_at_the_ends_of_blocks_tiles_and_turns(n, bt, hkv):
     """Spans of one token, of a tile, one short of and one beyond it, alike for all nodes and not."""
