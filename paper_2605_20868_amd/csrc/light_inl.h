@@ -4,6 +4,8 @@
 // rows, so that three waves share a SIMD instead of two.  What bounds it is the reconstruction on the vector ALU, which does not depend on the number of
 // rows, and the latency of its loads, which the third wave hides; the softmax of 32 rows, of which a single token's are four, is a quarter of the vector
 // operations, that of 16 an eighth.
+// 8 KV heads of 131072 tokens, one token of 4 query heads, capped: 63 us in a trace (a call 68) for 302 MB, 4.8 TB/s; vector ALU 55 % busy, waves wait 35 % of
+// their cycles; 60 us is the time of a copy of as many bytes.
 //
 //   S^T [32 tokens][16 rows] = K^ Q^T as two tiles of 16 tokens.  A lane (n, g), n = l & 15, g = l >> 4, gets four tokens of each tile for row n.  The tiles
 //     are tokens 0 - 3 and 4 - 7 of the pair's four octets, so that these eight are octet g: of one block, one dword of value codes, and packed
@@ -23,13 +25,13 @@ constexpr int L_SET_O = D * L_ROWS, L_SET = L_SET_O + 8 * L_ROWS;      // floats
 constexpr int L_KM_BLK = KM_BYTES + 32, L_VM_BLK = VM_BYTES + 32;      // bytes; padded: the addresses of a read lie in different banks
 constexpr int L_W_RUN = 16 * 16 + 16;                                  // widths [run of 8 channels][16 blocks]
 constexpr int L_KM = 0, L_VM = L_KM + 2 * L_KM_BLK, L_W = L_VM + 2 * L_VM_BLK, L_META_END = L_W + D / 8 * L_W_RUN;
-constexpr int L_EXACT = 64;                                            // trailing and drafted tokens of a turn
+constexpr int exact_of(int waves) { return waves < 4 ? 32 : 64; }      // trailing and drafted tokens of a turn
 constexpr int L_Q = L_ROWS * Q_ROW;
-static_assert(L_META_END <= L_SET * 4 && 2 * L_EXACT * D * 2 <= 4 * L_SET * 4 && L_VM % 16 == 0 && L_W % 16 == 0, "a wave's part of LDS, of four waves'");
+static_assert(L_META_END <= L_SET * 4 && 2 * exact_of(4) * D * 2 <= 4 * L_SET * 4 && 2 * exact_of(2) * D * 2 <= 2 * L_SET * 4 && L_VM % 16 == 0 && L_W % 16 == 0, "a wave's part of LDS, of four waves'");
 
 // Pairs by workgroup: a turn of the trailing and drafted tokens takes as long as two of the sealed ones.
 __host__ __device__ inline TileShares light_shares(int pairs, int others, int nsplit, int waves) {
-  return tile_shares(pairs, (others + L_EXACT - 1) / L_EXACT, nsplit, 2 * waves);
+  return tile_shares(pairs, (others + exact_of(waves) - 1) / exact_of(waves), nsplit, 2 * waves);
 }
 
 struct LightRows {
@@ -160,14 +162,21 @@ template <int WAVES, typename A>
 __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split, const LightLds& lds) {
   const int tid = threadIdx.x, l = tid & 63, n16 = l & 15, g = l >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  constexpr int L_EXACT = exact_of(WAVES);
   const int b = (int)(head / a.n_kv), kvh = (int)(head - (int64_t)b * a.n_kv);
   uint8_t* const wave = reinterpret_cast<uint8_t*>(lds.set[w]);
   std::conditional_t<A::SCORED, Scored<LightRows>, LightRows> rows;
   const int last_row = a.n * a.group - 1;
   rows.node = a.node_of(min(n16, last_row));
-  // rows 4 w .. 4 w + 3 of the queries by each of four waves: 16 lanes a row
-  const int q_row = min(4 * (w & 3) + g, last_row), q_node = a.node_of(q_row);
-  const uint4 q_in = ld16_any(a.q + (((int64_t)b * a.n + q_node) * a.n_kv * a.group + kvh * a.group + (q_row - q_node * a.group)) * D + n16 * 8);
+  // four rows of the queries at a time by each of four waves, or of two: 16 lanes a row
+  constexpr int Q_TURNS = WAVES < 4 ? 4 / WAVES : 1;
+  const auto q_row = [&](int i) { return 4 * ((w + i * WAVES) & 3) + g; };
+  uint4 q_in[Q_TURNS];
+#pragma unroll
+  for (int i = 0; i < Q_TURNS; ++i) {
+    const int row = min(q_row(i), last_row), node = a.node_of(row);
+    q_in[i] = ld16_any(a.q + (((int64_t)b * a.n + node) * a.n_kv * a.group + kvh * a.group + (row - node * a.group)) * D + n16 * 8);
+  }
 
   const uint8_t* const base = a.t1 + head * a.nq_cap * QUAD_BYTES;
   int units = (int)((a.nb + 1) >> 1);                       // pairs of sealed blocks
@@ -226,7 +235,8 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
   load_meta(u);
   load_keys(u);
   load_values(u);
-  *reinterpret_cast<uint4*>(lds.q + (4 * (w & 3) + g) * Q_ROW + n16 * 16) = q_in;   // (of each four waves the same)
+#pragma unroll
+  for (int i = 0; i < Q_TURNS; ++i) *reinterpret_cast<uint4*>(lds.q + q_row(i) * Q_ROW + n16 * 16) = q_in[i];   // (of each four waves the same)
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 4; ++i) rows.q[i] = *reinterpret_cast<const f16x8*>(lds.q + n16 * Q_ROW + (i >> 1) * 128 + g * 32 + (i & 1) * 16);
@@ -401,6 +411,7 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
 
 template <int WAVES, typename F>
 __device__ __forceinline__ void with_light_lds(F f) {
+  constexpr int L_EXACT = exact_of(WAVES);
   __shared__ __align__(16) float s_set[WAVES][L_SET];
   __shared__ __align__(16) uint8_t s_q[L_Q];
   __shared__ __align__(16) float s_norm[L_EXACT];

@@ -48,14 +48,21 @@ struct Shape {
 };
 static int light_splits(int n_cu, int64_t heads, int waves, int64_t sealed, int64_t others) {
   const int64_t most = std::max<int64_t>(1, 12 / waves * (int64_t)n_cu / heads), tiles = (sealed + 32 * waves - 1) / (32 * waves);
-  return (int)std::min(most, tiles <= 1 && others <= L_EXACT ? 1 : tiles + (others + L_EXACT - 1) / L_EXACT);
+  return (int)std::min(most, tiles <= 1 && others <= exact_of(waves) ? 1 : tiles + (others + exact_of(waves) - 1) / exact_of(waves));
 }
 // Up to 16 rows go by the light kernel: twelve waves a workgroup, one of which a compute unit holds, where these have three turns and more, for there are
-// fewer sets to join; else four waves (us a call in a graph with twelve and with four: 8 heads, 131072 tokens 64.1, 67.8; 4 x 8 heads, windows of 4096 in
-// 32768 23.6, 24.4; 8 heads, 8000 tokens 14.4, 12.6; 64 x 8 heads, 1029 tokens 44.3, 33.6; 200 x 4 heads, 263 tokens 47.4, 26.1).  More rows: tree_rows.
+// fewer sets to join; two where more heads are there than workgroups of four can be at a time, and short ones or no more than of two; else four
+// (us a call in a graph with twelve and with four: 8 heads, 131072 tokens 64.1, 67.8; 4 x 8 heads, windows of 4096 in 32768 23.6, 24.4; 8 heads, 8000 tokens
+// 14.4, 12.6; 64 x 8 heads, 1029 tokens 44.3, 33.6.  With four and with two: 512 heads, 263 tokens 15.1, 17.9; 640 19.7, 20.7; 800 25.4, 20.0; 3200 68.7, 59.8;
+// 800 heads, 40 tokens 17.7, 10.9; 1029 tokens 57.3, 50.1; 4101 tokens 232, 234; 1024 heads, 517 tokens 37.8, 32.3; 1600 heads, 1029 tokens 110.7, 122.4).
+// More rows: tree_rows.
+static int light_waves(int n_cu, int64_t heads, int64_t sealed) {
+  if (heads <= n_cu && (sealed + 383) / 384 >= 3 * (n_cu / heads)) return 12;
+  return heads > 3 * n_cu && sealed <= (heads <= 6 * n_cu ? 2048 : 512) ? 2 : 4;
+}
 static Shape shape_of(int n_cu, int64_t heads, int n_rows, int64_t sealed, int64_t others) {
   if (n_rows <= L_ROWS) {
-    const int waves = heads <= n_cu && (sealed + 383) / 384 >= 3 * (n_cu / heads) ? 12 : 4;
+    const int waves = light_waves(n_cu, heads, sealed);
     return {L_ROWS, waves, light_splits(n_cu, heads, waves, sealed, others)};
   }
   const int rows = tree_rows(n_cu, heads, n_rows, sealed, others);
@@ -67,6 +74,7 @@ static int64_t kv_groups(const Cache* c) { return (int64_t)c->desc.batch * c->de
 static int64_t set_floats(const Cache* c, int64_t nodes, int64_t others) {
   const int64_t heads = kv_groups(c);
   const int n_rows = row_count(c, nodes);
+  // (of two waves there is one set a head)
   if (n_rows <= L_ROWS) return heads * light_splits(c->n_cu, heads, 4, c->desc.max_tokens, others) * T_FLOATS;
   const auto most = [&](int rows) { return (int64_t)tree_splits(c->n_cu, heads, n_rows, rows, c->desc.max_tokens, others); };
   return heads * ((n_rows + 31) / 32) * std::max(most(32), most(n_rows <= 64 ? 64 : (n_rows <= 128 ? 128 : 256))) * T_FLOATS;
@@ -135,7 +143,9 @@ template <typename A>
 static int32_t launch_rows(const A& a, const Pass& x, hipStream_t st) {
   if (x.shape.rows != L_ROWS) return launch_pass(a, x.heads, x.shape.rows, x.others, st);
   const dim3 grid((uint32_t)x.heads, (uint32_t)a.nsplit);
-  if (x.shape.waves == 4)
+  if (x.shape.waves == 2)
+    tree_light_kernel<2><<<grid, 128, 0, st>>>(a);
+  else if (x.shape.waves == 4)
     tree_light_kernel<4><<<grid, 256, 0, st>>>(a);
   else
     tree_light_kernel<12><<<grid, 768, 0, st>>>(a);

@@ -91,15 +91,15 @@ struct TreeArgs {
 
 // Of a pass whose nodes may be several sequences' (a beginning that they share), that has drafted tokens or none, that may leave its sets to be
 // joined with another pass's; SCORES: with scores of the caller's.  x = scale q . k,  y = cap tanh(x / cap),  score = y - slope |p - j|.
-//   What the softmax works on is the score in units of its own, `per_unit` exponents of 2 each, and less a constant of the row:
+// The bias counts from the distance `near` of the row's nearest attended token (the farthest, under a negative slope), so that the scores of a row that
+// attends far tokens only keep their bits.  What the softmax works on is the score in units of its own, `per_unit` exponents of 2 each, and less a
+// constant of the row:
 //   CAP_NONE   q . k
 //   CAP_LOW    -1 / (1 + e^(2 x / cap)) = (tanh(x / cap) - 1) / 2, an exponential and a reciprocal: off by 2^-24 of a unit, 2 cap
 //   CAP_HIGH   tanh(x / cap), relatively exact: a series up to 0.36, which is one operation more, beside 1 - 2 / (1 + e^(2 x / cap)) where a wave has larger ones
 // LOW where a pass reconstructs for 128 or 256 rows at once, which the scores' operations bound, and the cap is at most LOW_CAPS (us a call in a graph, LOW and
 // HIGH: 8 heads, 131072 tokens, 64 nodes of 4 heads 222, 287; 2 x 8 heads, 16000 tokens, 20 nodes of 4 50.5, 57.0; 64 rows, 8 heads, 32000 tokens 44, 42; one token,
 // 131072 tokens 66.5, 66.7).
-// and the bias counts from the distance `near` of the row's nearest attended token (the farthest, under a negative slope), so that the scores of a
-// row that attends far tokens only keep their bits.
 enum { CAP_NONE = 0, CAP_LOW, CAP_HIGH };
 constexpr float LOW_CAPS = 256.0f;
 enum Scores { PLAIN = 0, SCALED, PLACED };   // q . k / sqrt(d) of every token; by scale and cap; by places and spans as well

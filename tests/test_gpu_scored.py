@@ -560,6 +560,34 @@ def test_more_sequences_than_compute_units_and_more_than_256_rows():
             gc.close()
 
 
+@pytest.mark.parametrize("tokens,bt,hkv,g,n,cap,bias,spans", [
+    (0, 200, 4, 4, 4, 0.0, 0, "all"), (37, 200, 4, 4, 1, 0.0, 0, "all"), (263, 200, 4, 2, 7, 30.0, 0, "all"), (130, 400, 2, 4, 3, 300.0, 1, "padded"),
+    (2053, 100, 8, 4, 1, 5.0, 1, "any"), (519, 400, 4, 1, 16, 0.0, -1, "sorted"), (33, 200, 4, 4, 4, 0.0, 0, "window")])
+@pytest.mark.parametrize("beginning", [0, 85])
+def test_more_short_sequences_than_the_device_holds(tokens, bt, hkv, g, n, cap, bias, spans, beginning):
+    """Workgroups of two waves: every kind of score, trailing and drafted tokens of several turns, groups of one row and of sixteen."""
+    print("short sequences", tokens, bt, hkv, g, n, beginning, flush=True)
+    rng = np.random.default_rng(tokens + beginning)
+    x = make(rng, 4, hkv, g, tokens, n, n > 1, "student", 2.0, 1 if beginning else 0, beginning)
+    seen = random_tree(rng, 4, n) if n > 1 else None
+    total = beginning + tokens
+    places = total - (0 if n > 1 else 1) + rng.integers(0, 9, (4, n))
+    at = make_spans(rng, spans, 4, n, total, places)
+    score = dict(cap=cap, slopes=slopes_of(hkv * g, bias), places=places if bias else None, spans=at)
+    tile = lambda y: None if y is None else np.tile(y, (bt // 4,) + (1,) * (y.ndim - 1))  # noqa: E731
+    with Caches(x, g) as c:
+        ref = scored.decode(c.shared_oc, c.oc, x["q"], x["kd"], x["vd"], seen, oracle.Tolerances(), **score)
+        gc = GpuLayerCache(bt, hkv * g, hkv, max(tokens, 1), tier2=False)
+        if tokens:
+            gc.append(tile(x["k"]), tile(x["v"]))
+        many = dict(score, places=tile(score["places"]), spans=tile(at))
+        mask = None if seen is None else drafts.mask_words(tile(seen))
+        O, cert, flags = call(c.shared, gc, tile(x["q"]), tile(x["kd"]), tile(x["vd"]), mask, **many)
+        assert_nodes(ref, O[:4], {f: y[:4] for f, y in cert.items()}, flags[:4], bt)
+        assert all(np.array_equal(O[i], O[i % 4]) and np.array_equal(flags[i], flags[i % 4]) for i in range(bt))
+        gc.close()
+
+
 @pytest.mark.parametrize("hkv,g,beginning,bt,n,cap", [(4, 4, 20016, 32, 1, 0.0), (4, 4, 20005, 16, 1, 40.0), (2, 4, 33003, 12, 6, 0.0), (8, 2, 5001, 160, 1, 20.0)])
 def test_many_sequences_behind_a_long_beginning(hkv, g, beginning, bt, n, cap):
     """33 and more rows of several sequences by a workgroup that reconstructs once for all."""
