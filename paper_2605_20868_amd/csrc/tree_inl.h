@@ -564,8 +564,19 @@ __device__ __forceinline__ void values32(TreeRows& w, const uint32_t (&p)[8], Va
           value(oct, ct), __builtin_bit_cast(f16x8, make_uint4(p[4 * oct], p[4 * oct + 1], p[4 * oct + 2], p[4 * oct + 3])), w.o[ct], 0, 0, 0);
 }
 // What weights relative to a largest score m are worth beside a largest one M >= m (-inf: there are none).
+// Under CAP_LOW the exponents are rounded with m (less_most), and here alike.
 template <typename A>
-__device__ __forceinline__ float set_weight(const A& a, float m, float M) { return m == M ? 1.0f : __builtin_amdgcn_exp2f((m - M) * a.unit()); }
+__device__ __forceinline__ bool low_cap(const A& a) {
+  if constexpr (A::SCORED) return a.cap_kind == CAP_LOW;
+  return false;
+}
+template <typename A>
+__device__ __forceinline__ float less_most(const A& a, float m) { return fmaf(-m, a.unit(), MOST); }
+template <typename A>
+__device__ __forceinline__ float set_weight(const A& a, float m, float M) {
+  if (m == M) return 1.0f;
+  return __builtin_amdgcn_exp2f(low_cap(a) ? less_most(a, M) - less_most(a, m) : (m - M) * a.unit());
+}
 // Scores of MT times 32 tokens to weights, 2^MOST for a row's largest score so far, the row's m.  The weights enter
 // the product with the values as FP16: those down to 2^-28 of the largest keep 11 bits, and a million lighter ones are together off by 2^-19
 // of it.  (With 1 for the largest, tokens of 2^-25 of it vanished, and all of the result with them where the heavy ones' values are zero.)
@@ -619,13 +630,8 @@ __device__ __forceinline__ void softmax32(const A& a, TreeRows& w, f32x16 (&s)[M
     w.evmax = fmaxf(w.evmax, e);
   }
 }
-template <typename A>
-__device__ __forceinline__ bool low_cap(const A& a) {
-  if constexpr (A::SCORED) return a.cap_kind == CAP_LOW;
-  return false;
-}
 // The same in passes of SetArgs, for MT times N scores of a lane.  Under CAP_LOW, whose scores are within 2 cap of each other, m is taken off in the
-// multiply-add that scales them: one rounding, 2^-18 of an exponent, that all weights by this m share (8 heads, 131072 tokens, 64 nodes of 4 heads 245, 229
+// multiply-add that scales them: one rounding, 2^-18 of an exponent, that all weights by this m share and that set_weight and lse know of (8 heads, 131072 tokens, 64 nodes of 4 heads 245, 229
 // us).  largest(x): over the lanes of a row; block(x): the sum over a block.
 // silent: a lane's row has no part in it (one that attends no cached token, among others whose tokens are not looked at one by one).
 template <int MT, int N, typename A, typename Rows, typename V, typename Bits, typename Eta, typename Largest, typename Block>
@@ -659,7 +665,7 @@ __device__ __forceinline__ void softmax_sets(const A& a, Rows& w, V (&s)[MT], ui
   const float m = w.m == -INFINITY ? 0.0f : w.m;   // nothing attended yet: every weight is exp2(-inf) = 0
   float most = MOST;
   if (low_cap(a))
-    most = fmaf(-m, a.unit(), MOST);
+    most = less_most(a, m);
   else
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
@@ -1001,7 +1007,11 @@ __device__ __forceinline__ Certificate certificate(const A& a, float M, float L,
   ct.v_max = VM;
   ct.alpha_tail_hat = sealed * inv;
   ct.lse = empty ? -INFINITY : fmaf(M, a.unit() * LN2, logf(L) - MOST * LN2);
-  if constexpr (A::SCORED) ct.lse = empty ? ct.lse : ct.lse + offset;
+  if constexpr (A::SCORED) {
+    if (low_cap(a)) ct.lse = fmaf(2.0f * a.cap, M, offset) + fmaf(-LN2, fmaf(M, a.unit(), less_most(a, M)), logf(L));   // (m's part and its rounding)
+    else ct.lse += offset;
+    if (empty) ct.lse = -INFINITY;
+  }
   ct.max_block_contrib = EM * inv;
   ct.reserved = 0.0f;
   float tail = 0.0f;
