@@ -236,9 +236,10 @@ __device__ __forceinline__ Spans spans_among(const SpansGiven& x, int first, int
   if (s.lo1 >= s.hi1) s.lo1 = s.hi1 = 0;
   return s;
 }
-// Whether a token of block k is in them.
+// Whether a token of block k is in them.  (No branches: the compiler makes one of each &&.)
 __device__ __forceinline__ bool some_of(const Spans& s, int k) {
-  return (k >= s.lo0 / BLK && k < (s.hi0 + BLK - 1) / BLK) || (k >= s.lo1 / BLK && k < (s.hi1 + BLK - 1) / BLK);
+  const auto in = [&](uint32_t lo, uint32_t hi) { return (uint32_t)k - lo / BLK < (hi + BLK - 1) / BLK - lo / BLK; };
+  return (uint32_t)in(s.lo0, s.hi0) | (uint32_t)in(s.lo1, s.hi1);
 }
 // The open ones of the 16 tokens from t on.
 __device__ __forceinline__ uint32_t span_bits(const Spans& s, int t) {
@@ -1440,6 +1441,7 @@ struct ManyLds {
   uint8_t* bad;                                 // [TOK]
   float (*nu)[ManyShape<WR>::BLKS];             // [4], PLACED
   uint32_t (*flawed)[2][ManyShape<WR>::BLKS];   // [4], PLACED: by keys, by values
+  uint32_t* flaws;                              // PLACED: 1 as soon as a token was flawed
   int* place;                                   // [TOK], PLACED
   Spans (*span)[T_ROWS];                        // [8], PLACED
 };
@@ -1537,6 +1539,8 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
   bool partial = false;      // PLACED: some row of the wave does not attend all of them
   uint32_t open = 0u;        // PLACED: tokens of sealed blocks that the lane's row has attended
   int buf = 0;
+  if constexpr (A::PLACED)
+    if (tid == 0) *lds.flaws = 0u;
   __syncthreads();
 
   const auto key_of = [&](const uint4* s_k, int unit, int ks) { return __builtin_bit_cast(f16x8, s_k[(half * 8 + ks) * TOK + unit * 32 + n32]); };
@@ -1562,7 +1566,10 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
             flawed = flawed_tokens(flawed, 0);
           }
         }
-        if (l == 0) lds.flawed[turn & 3][keys.value ? 0 : 1][qd * 4 + wb] = flawed;
+        if (l == 0) {
+          lds.flawed[turn & 3][keys.value ? 0 : 1][qd * 4 + wb] = flawed;
+          if (flawed != 0u) *lds.flaws = 1u;
+        }
       }
     if constexpr (keys.value)
       *reinterpret_cast<uint4*>(s_meta + (l * 4 + (l >> 4) * 4) * 4) = raw[qd][2];
@@ -1664,7 +1671,6 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
   const auto key_ks = [](int k) constexpr { return EARLY ? k % 8 : k / MT; };
   // PLACED: rows that attend flawed tokens of the tile before, whose keys and values have both come
   const auto look_back = [&](int u, int turn) {
-    if (!spans) return;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const int in = (wt * MT + mt) * 2 + half;
@@ -1762,7 +1768,15 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
       __builtin_amdgcn_s_setprio(0);
       turn_over();
       if constexpr (A::PLACED) {
-        if (turn > 0) look_back(u - 1, turn - 1);
+        // (what LDS holds is asked for at once: where each is used, a tile took 1000 cycles more; windows over 131072 tokens, 64 nodes of 4 heads 263, 251 us)
+        float eta[MT], block_nu[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          const int in = (wt * MT + mt) * 2 + half;
+          eta[mt] = s_eta[turn & 3][in];
+          block_nu[mt] = lds.nu[turn & 3][in];
+        }
+        const uint32_t flaws = *lds.flaws;
         const int tile = tile_at(u);
         uint32_t there[MT];
         bool masked = (int64_t)(tile + 1) * BLKS > a.nb;
@@ -1772,12 +1786,13 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
           there[mt] = some ? span_bits(lds.span[w][n32], blk * BLK) : 0xffffu;
           if (blk >= a.nb || rows.idle) there[mt] = 0u;
           open |= there[mt];
-          rows.vmax = fmaxf(rows.vmax, there[mt] == 0u ? 0.0f : lds.nu[turn & 3][in]);
+          rows.vmax = fmaxf(rows.vmax, there[mt] == 0u ? 0.0f : block_nu[mt]);
           score<16, MT == 1>(a, rows, sc[mt], RunFar<BLK>(rows, blk * BLK), EARLY && mt == 0);
         }
         masked |= some;
         weigh32<MT>(
-            a, rows, sc, p, masked, [&](int mt) { return there[mt]; }, [&](int mt) { return there[mt] == 0u ? 0.0f : s_eta[turn & 3][(wt * MT + mt) * 2 + half]; }, rows.idle);
+            a, rows, sc, p, masked, [&](int mt) { return there[mt]; }, [&](int mt) { return there[mt] == 0u ? 0.0f : eta[mt]; }, rows.idle);
+        if (turn > 0 && __builtin_amdgcn_readfirstlane(flaws) != 0u) look_back(u - 1, turn - 1);
       } else {
         if constexpr (A::SCORED)
 #pragma unroll
@@ -1810,7 +1825,8 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
       sealed_tiles(std::false_type{});
     }
     add_values(buf ^ 1);
-    if constexpr (A::PLACED) look_back(units - 1, units - 1 - from);
+    if constexpr (A::PLACED)
+      if (*lds.flaws != 0u) look_back(units - 1, units - 1 - from);
   }
   if constexpr (A::PLACED) rows.dmax = rows.idle ? 0.0f : rows.dmax;
   rows.sealed = rows.sum;
@@ -1882,11 +1898,12 @@ __global__ __launch_bounds__(512, 2) void tree_many_kernel(A a) {
   if constexpr (A::PLACED) {
     __shared__ float s_nu[4][S::BLKS];
     __shared__ uint32_t s_flawed[4][2][S::BLKS];
+    __shared__ uint32_t s_flaws;
     __shared__ __align__(16) int s_place[S::TOK];
     __shared__ __align__(16) Spans s_span[8][T_ROWS];
-    attend_many<WR>(a, blockIdx.x, blockIdx.y, blockIdx.z, ManyLds<WR>{s_main, s_eta, s_norm, s_bad, s_nu, s_flawed, s_place, s_span});
+    attend_many<WR>(a, blockIdx.x, blockIdx.y, blockIdx.z, ManyLds<WR>{s_main, s_eta, s_norm, s_bad, s_nu, s_flawed, &s_flaws, s_place, s_span});
   } else {
-    attend_many<WR>(a, blockIdx.x, blockIdx.y, blockIdx.z, ManyLds<WR>{s_main, s_eta, s_norm, s_bad, nullptr, nullptr, nullptr, nullptr});
+    attend_many<WR>(a, blockIdx.x, blockIdx.y, blockIdx.z, ManyLds<WR>{s_main, s_eta, s_norm, s_bad, nullptr, nullptr, nullptr, nullptr, nullptr});
   }
 }
 
