@@ -565,9 +565,11 @@ __device__ __forceinline__ void values32(TreeRows& w, const uint32_t (&p)[8], Va
           value(oct, ct), __builtin_bit_cast(f16x8, make_uint4(p[4 * oct], p[4 * oct + 1], p[4 * oct + 2], p[4 * oct + 3])), w.o[ct], 0, 0, 0);
 }
 // What weights relative to a largest score m are worth beside a largest one M >= m (-inf: there are none).
-// Under CAP_LOW the exponents are rounded with m (less_most), and here alike.
+// Under CAP_LOW without a bias, whose scores are within 2 cap of each other, the exponents are rounded with m (less_most), and here alike.  (With a bias
+// that rounding may be more than FP16's range: those of far tokens alone are as large as the caller's slopes.)
 template <typename A>
-__device__ __forceinline__ bool low_cap(const A& a) {
+__device__ __forceinline__ bool rounds_most(const A& a) {
+  if constexpr (A::PLACED) return a.cap_kind == CAP_LOW && a.slopes == nullptr;
   if constexpr (A::SCORED) return a.cap_kind == CAP_LOW;
   return false;
 }
@@ -576,7 +578,7 @@ __device__ __forceinline__ float less_most(const A& a, float m) { return fmaf(-m
 template <typename A>
 __device__ __forceinline__ float set_weight(const A& a, float m, float M) {
   if (m == M) return 1.0f;
-  return __builtin_amdgcn_exp2f(low_cap(a) ? less_most(a, M) - less_most(a, m) : (m - M) * a.unit());
+  return __builtin_amdgcn_exp2f(rounds_most(a) ? less_most(a, M) - less_most(a, m) : (m - M) * a.unit());
 }
 // Scores of MT times 32 tokens to weights, 2^MOST for a row's largest score so far, the row's m.  The weights enter
 // the product with the values as FP16: those down to 2^-28 of the largest keep 11 bits, and a million lighter ones are together off by 2^-19
@@ -631,7 +633,7 @@ __device__ __forceinline__ void softmax32(const A& a, TreeRows& w, f32x16 (&s)[M
     w.evmax = fmaxf(w.evmax, e);
   }
 }
-// The same in passes of SetArgs, for MT times N scores of a lane.  Under CAP_LOW, whose scores are within 2 cap of each other, m is taken off in the
+// The same in passes of SetArgs, for MT times N scores of a lane.  Under CAP_LOW without a bias m is taken off in the
 // multiply-add that scales them: one rounding, 2^-18 of an exponent, that all weights by this m share and that set_weight and lse know of (8 heads, 131072 tokens, 64 nodes of 4 heads 245, 229
 // us).  largest(x): over the lanes of a row; block(x): the sum over a block.
 // silent: a lane's row has no part in it (one that attends no cached token, among others whose tokens are not looked at one by one).
@@ -665,7 +667,7 @@ __device__ __forceinline__ void softmax_sets(const A& a, Rows& w, V (&s)[MT], ui
   }
   const float m = w.m == -INFINITY ? 0.0f : w.m;   // nothing attended yet: every weight is exp2(-inf) = 0
   float most = MOST;
-  if (low_cap(a))
+  if (rounds_most(a))
     most = less_most(a, m);
   else
 #pragma unroll
@@ -1009,7 +1011,7 @@ __device__ __forceinline__ Certificate certificate(const A& a, float M, float L,
   ct.alpha_tail_hat = sealed * inv;
   ct.lse = empty ? -INFINITY : fmaf(M, a.unit() * LN2, logf(L) - MOST * LN2);
   if constexpr (A::SCORED) {
-    if (low_cap(a)) ct.lse = fmaf(2.0f * a.cap, M, offset) + fmaf(-LN2, fmaf(M, a.unit(), less_most(a, M)), logf(L));   // (m's part and its rounding)
+    if (rounds_most(a)) ct.lse = fmaf(2.0f * a.cap, M, offset) + fmaf(-LN2, fmaf(M, a.unit(), less_most(a, M)), logf(L));   // (m's part and its rounding)
     else ct.lse += offset;
     if (empty) ct.lse = -INFINITY;
   }

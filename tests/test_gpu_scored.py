@@ -344,6 +344,39 @@ def test_padding_that_is_not_finite(n, hkv, shared):
         gc.close()
 
 
+@pytest.mark.parametrize("steep", [30.0, 1e5, 1e20, -1e5])
+@pytest.mark.parametrize("n,cap,beginning", [(1, 5.0, 0), (20, 30.0, 0), (64, 30.0, 0), (64, 1e4, 0), (32, 30.0, 700), (64, 30.0, 700)])
+def test_steep_biases(n, cap, beginning, steep):
+    """Tokens whose weights are nothing beside the nearest ones', in workgroups that see no others: their scores are far beyond what a rounding of
+    the largest leaves."""
+    print("steep", n, cap, beginning, steep, flush=True)
+    rng = np.random.default_rng(n)
+    x = make(rng, 1, 1, 4, 1500, n, n > 1, shared=1 if beginning else 0, beginning=beginning)
+    seen = random_tree(rng, 1, n) if n > 1 else None
+    compare(x, 4, seen, (n, steep), cap=cap, slopes=np.array([steep, steep / 3, 0.01, 0.0], np.float32))
+
+
+@pytest.mark.parametrize("steep", [30.0, 1e5, 1e20, -1e5])
+@pytest.mark.parametrize("n,cap,tokens", [(64, 30.0, 1290), (32, 200.0, 2500)])
+def test_steep_biases_of_many_rows(n, cap, tokens, steep):
+    """The same in the workgroups that reconstruct for 128 and 256 rows."""
+    print("steep, many rows", n, cap, steep, flush=True)
+    rng = np.random.default_rng(n)
+    bt, g = 130, 4
+    x = make(rng, 1, 2, g, tokens, n, True)
+    seen = random_tree(rng, 1, n)
+    score = dict(cap=cap, slopes=np.array([steep, steep / 3, 0.01, 0.0, -0.01, steep / 7, 0.5, steep], np.float32))
+    with Caches(x, g) as c:
+        ref = scored.decode(None, c.oc, x["q"], x["kd"], x["vd"], seen, oracle.Tolerances(), **score)
+        gc = GpuLayerCache(bt, 2 * g, 2, tokens, tier2=False)
+        many = [np.tile(x[i], (bt, 1, 1, 1)) for i in ("k", "v", "q", "kd", "vd")]
+        gc.append(*many[:2])
+        O, cert, flags = call(None, gc, *many[2:], drafts.mask_words(np.tile(seen, (bt, 1, 1))), **score)
+        assert_nodes(ref, O[:1], {f: y[:1] for f, y in cert.items()}, flags[:1], (n, steep))
+        assert all(np.array_equal(O[i], O[0]) for i in range(bt))
+        gc.close()
+
+
 @pytest.mark.parametrize("n,bt,hkv", [(1, 1, 1), (13, 1, 1), (27, 1, 1), (64, 1, 1), (64, 130, 2)])
 def test_spans_at_the_ends_of_blocks_tiles_and_turns(n, bt, hkv):
     """Spans of one token, of a tile, one short of and one beyond it, alike for all nodes and not."""
