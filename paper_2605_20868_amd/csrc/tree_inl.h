@@ -1747,11 +1747,13 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
         __builtin_amdgcn_sched_barrier(0);
       });
       if (full || last) {
-        // (up to the last block that has come: on the last tile, other waves write the first record's widths behind it meanwhile)
-        const int blk = min(n32, fresh - 1);
+        // (up to the last block that there is.  Behind it a tile holds zeros, or, where a quad of it is behind the last one, the head's first record, whose
+        // widths bound no row that has not attended it; on the last tile, other waves write that record's widths further behind meanwhile.)
+        const int behind = (int)((int64_t)(tile_at(u) + 1) * BLKS - a.nb), end = fresh - 1 - max(behind, 0);
+        const int blk = min(n32, end);
         const auto width = [&](int ks) { return *reinterpret_cast<const f16x8*>(width_at(ring, half * 8 + ks, blk)); };
         const auto block_of = [&](int slot) {
-          slot = min(slot, fresh - 1);
+          slot = min(slot, end);
           return tile_at(ring_from + slot / BLKS) * BLKS + slot % BLKS;
         };
         if (wt == 0) {

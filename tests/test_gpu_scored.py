@@ -455,6 +455,56 @@ def some_nodes(c, x, seen, places, some, **score):
     return [[full[j][b][0] for j in range(len(some))] for b in range(x["q"].shape[0])]
 
 
+@pytest.mark.parametrize("n,blocks", [(13, 68), (13, 76), (13, 67), (13, 69), (13, 72), (27, 69), (27, 71), (64, 68), (64, 70)])
+@pytest.mark.parametrize("beginnings", [False, True])
+def test_a_bound_is_over_blocks_that_are_there(n, blocks, beginnings):
+    """A tile of 64 and more rows ends behind the last sealed block: what it holds there is no block of the row's, also where the row attends the trailing
+    tokens, whose places these would be.  The first block's keys, far wider than all others, are left out by most rows."""
+    print("blocks that are there", n, blocks, beginnings, flush=True)
+    rng = np.random.default_rng(100 * blocks + n)
+    bt = 256 if n * 4 <= 64 else 160
+    tokens, own = 16 * blocks + 5, 21
+    x = make(rng, 4, 1, 4, own if beginnings else tokens, n, False, shared=4 if beginnings else 0, beginning=tokens)
+    x["sk" if beginnings else "k"][:, :, :16] *= np.float16(256.0)
+    spans = np.zeros((4, n, 4), np.int64)
+    spans[0] = [40, tokens, 0, 0]                                  # padded
+    spans[1] = [16 * blocks, tokens, 0, 0]                         # trailing tokens only: no sealed one bounds anything
+    spans[2] = [tokens - 150, tokens, 0, 0]                        # a window
+    spans[2, n // 2] = [0, 3, 16 * blocks + 2, tokens]             # ... with the first tokens
+    spans[3] = [0, 0, 16 * blocks - 1, 16 * blocks + 1]
+    spans[3, 0] = 0                                                # nothing
+    some = np.unique([0, n // 2, n - 1])
+    with Caches(x, 4) as c:
+        ref = scored.decode(c.shared_oc, c.oc, x["q"][:, some], None, None, None, oracle.Tolerances(), spans=spans[:, some])
+        wide = {k: again(v, bt) for k, v in x.items()}
+        with Caches(wide, 4) as w:
+            O, cert, flags = call(w.shared, w.gc, wide["q"], spans=again(spans, bt))
+    assert (cert["delta_h"][1] == 0).all()
+    for y in (O, flags, *cert.values()):
+        assert all(np.array_equal(y[i], y[i % 4]) for i in range(bt))
+    O, cert, flags = O[:4, some], {f: y[:4, some] for f, y in cert.items()}, flags[:4, some]
+    wide_rows(ref[2][1], x["q"][2, n // 2], x["sk" if beginnings else "k"][2, 0, :3], {f: y[2, 1] for f, y in cert.items()}, flags[2, 1])
+    for field in cert:
+        cert[field][2, 1] = [r.get(field, 0.0) for r in ref[2][1]]
+    O[2, 1], flags[2, 1] = [r["O"] for r in ref[2][1]], [r["flags"] for r in ref[2][1]]
+    assert_nodes(ref, O, cert, flags, (n, blocks))
+
+
+def wide_rows(ref, q, k, cert, flags):
+    """The certificate of a node's heads that attend keys of some 256 times the ordinary size, whose scores the bar of 1e-4 for FP32's arithmetic does not
+    cover.  A score is a sum of 128 products, exact in FP32 each: it is off by 128 2^-24 of the sum of their sizes s at most, so that a weight beside
+    another's is off by the factor e^(2 128 2^-24 s), and a mass by as much.  Delta, a sum of 128 numbers of one sign, is relatively off by 128 2^-24, and
+    E_key, which has e^(mass_exp Delta) and e^(2 Delta), by that of (mass_exp + 2) Delta."""
+    for h, r in enumerate(ref):
+        size = float((np.abs(k.astype(np.float64)) @ np.abs(q[h].astype(np.float64))).max()) / math.sqrt(128.0)
+        weight = math.expm1(2 * 128 * 2.0 ** -24 * size)
+        bound = 128 * 2.0 ** -24 * (oracle.Tolerances().mass_exp + 2) * r["delta_h"]
+        for field, tol in (("delta_h", 0.0), ("v_max", 0.0), ("E_val", weight), ("alpha_tail_hat", weight), ("max_block_contrib", weight), ("E_key", weight + math.expm1(bound))):
+            assert abs(float(cert[field][h]) - r[field]) <= (1e-4 + tol) * abs(r[field]) + 1e-9, (field, h, float(cert[field][h]), r[field])
+        assert abs(float(cert["lse"][h]) - r["lse"]) <= 1e-4 * max(1.0, abs(r["lse"])) + 128 * 2.0 ** -24 * size
+        assert int(flags[h]) == r["flags"]
+
+
 def test_the_plain_scores_are_the_tree_calls():
     """No scoring, a scoring of nothing, and a span of everything."""
     print("plain", flush=True)
