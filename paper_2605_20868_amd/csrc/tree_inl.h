@@ -496,11 +496,12 @@ __device__ __forceinline__ void mend_pair(uint4& km0, uint4& km1, uint4& vm, uin
   flawed[0] = __all(k0) ? flawed_tokens(flaws, 0) : 0xffffu;
   flawed[1] = __all(k1) ? flawed_tokens(flaws, 1) : 0xffffu;
 }
-// A query or a slope that is not finite (a slope of more than 10^28 with it, for distances are numbers too): zeros, which nothing passes on; the row's
-// sum is no number at the end.
-template <typename Rows, int N>
-__device__ __forceinline__ void zero_undefined(Rows& w, f16x8 (&q)[N]) {
-  const bool steep = !(fabsf(w.slope) <= 1e28f);
+// A query or a slope that is not finite (a slope of more than 10^28 times the cap, or the scale, with it, for distances are numbers too): zeros, which nothing
+// passes on; the row's sum is no number at the end.
+template <typename A, typename Rows, int N>
+__device__ __forceinline__ void zero_undefined(const A& a, Rows& w, f16x8 (&q)[N]) {
+  bool steep = false;
+  if constexpr (A::PLACED) steep = !(fabsf(w.slope) <= (a.cap_kind == CAP_LOW ? 0.5f * 1e28f : 1e28f));   // (CAP_LOW's unit is two caps)
   w.undefined |= steep;
   w.slope = steep ? 0.0f : w.slope;
 #pragma unroll
@@ -529,7 +530,7 @@ __device__ __forceinline__ void start_rows(RowsOf<A>& s, const A& a, int tile, c
       bad |= !(finite2(x.x) & finite2(x.y) & finite2(x.z) & finite2(x.w));
     }
     s.undefined = max_x32(bad ? 1.0f : 0.0f) != 0.0f;
-    zero_undefined(s, s.q);
+    zero_undefined(a, s, s.q);
   }
 }
 // The bias and the spans of a wave's rows, of sequence or beginning b; sealed and trailing tokens: count.  The spans go to LDS, a row's 16 bytes.

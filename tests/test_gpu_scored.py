@@ -377,6 +377,32 @@ def test_steep_biases_of_many_rows(n, cap, tokens, steep):
         gc.close()
 
 
+# up to 16, 32, 64, 128 and 256 rows a workgroup; the last with the tokens as a beginning's
+@pytest.mark.parametrize("n,bt,tokens,beginning", [(1, 2, 300, 0), (3, 2, 300, 700), (8, 2, 300, 0), (13, 160, 1290, 0), (32, 130, 1300, 0), (64, 130, 1290, 0), (64, 130, 40, 1290)])
+@pytest.mark.parametrize("cap,scale", [(30.0, 0.0), (200.0, 0.0), (1e4, 0.0), (0.0, 0.0), (0.0, 4.0)])
+def test_a_bias_is_too_steep_from_the_same_slope_on(n, bt, tokens, beginning, cap, scale):
+    """10^28 cap, or 10^28 scale without one, whichever kernel a row's number and the cache's length choose."""
+    print("too steep", n, bt, tokens, beginning, cap, scale, flush=True)
+    rng = np.random.default_rng(n + tokens)
+    g, hkv = 4, 2
+    x = make(rng, 1, hkv, g, tokens, n, True, shared=1 if beginning else 0, beginning=beginning)
+    seen = random_tree(rng, 1, n)
+    unit = cap or scale or 1.0 / math.sqrt(128.0)
+    slopes = (np.array([0.9e28, 1.1e28, -1.1e28, 1.9e28, 0.01, -1.9e28, 2.1e28, -0.9e28]) * unit).astype(np.float32)
+    undefined = np.abs(slopes) > 1e28 * unit
+    score = dict(cap=cap, scale=scale, slopes=slopes)
+    with Caches(x, g) as c:
+        ref = scored.decode(c.shared_oc, c.oc, x["q"], x["kd"], x["vd"], seen, oracle.Tolerances(), **score)
+        wide = {k: again(v, bt) for k, v in x.items()}
+        with Caches(wide, g) as w:
+            O, cert, flags = call(w.shared, w.gc, wide["q"], wide["kd"], wide["vd"], drafts.mask_words(again(seen, bt)), **score)
+    for y in (O, flags, *cert.values()):
+        assert all(np.array_equal(y[i], y[0], equal_nan=True) for i in range(bt))
+    assert np.isnan(O[0][:, undefined]).all() and (flags[0][:, undefined] & 8 != 0).all()
+    fine = np.flatnonzero(~undefined)
+    assert_nodes([[[heads[h] for h in fine] for heads in ref[0]]], O[:1][:, :, fine], {f: y[:1][:, :, fine] for f, y in cert.items()}, flags[:1][:, :, fine], (n, cap))
+
+
 @pytest.mark.parametrize("n,bt,hkv", [(1, 1, 1), (13, 1, 1), (27, 1, 1), (64, 1, 1), (64, 130, 2)])
 def test_spans_at_the_ends_of_blocks_tiles_and_turns(n, bt, hkv):
     """Spans of one token, of a tile, one short of and one beyond it, alike for all nodes and not."""
