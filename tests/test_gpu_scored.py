@@ -720,6 +720,20 @@ def test_many_sequences_behind_a_long_beginning(hkv, g, beginning, bt, n, cap):
         assert all(np.array_equal(y[i], y[i % 4]) for i in range(bt))
 
 
+def test_joining_as_many_sets_as_two_caches_can_leave():
+    """One KV head: three workgroups a compute unit in either pass, 1536 sets of a row, whose weights take more of LDS than 64 KB beside what is joined."""
+    print("scored most sets", flush=True)
+    t = _torch()
+    rng = np.random.default_rng(61)
+    tokens, beginning = 98437, 98506
+    x = make(rng, 1, 1, 4, tokens, 1, False, "student", 2.0, 1, beginning)
+    with Caches(x, 4) as c:
+        sets = 3 * t.cuda.get_device_properties(0).multi_processor_count
+        assert min(tokens, beginning) // 128 >= sets
+        for score in (dict(), dict(cap=30.0, slopes=np.array([0.001, 0.0, 1e-5, -1e-6], np.float32))):
+            assert_nodes(scored.decode(c.shared_oc, c.oc, x["q"], None, None, None, oracle.Tolerances(), **score), *call(c.shared, c.gc, x["q"], **score), "sets")
+
+
 def test_nothing_at_all_is_attended():
     """Empty caches and no drafted tokens, and an empty mask."""
     print("scored empty", flush=True)
