@@ -563,7 +563,8 @@ int32_t cqa_tree_workspace_bytes(const cqa_cache* c, int32_t n_draft, int64_t* b
  * its index (of a shared beginning's: from its first; the sequence's own: behind the beginning's last); a drafted token's is that of its
  * node.
  *   scale       0: 1 / sqrt(128); otherwise 2^-40 .. 2^40
- *   cap         0: none; otherwise 2^-20 .. 2^60
+ *   cap         0: none; otherwise 2^-20 .. 2^60.  tanh is within 2^-21 of itself, and for caps up to 128, where a launch takes 65 and more rows of a KV
+ *               group together, within 2^-25 besides
  *   slopes_dev  float [n_q_heads], or NULL: no bias.  Negative slopes are allowed; one that is no finite number, or beyond 10^28 scale (10^28
  *               cap, with a cap), makes its head's rows NaN with PRECOND, as such queries do
  *   places_dev  int64 [batch][n_nodes], or NULL: node i of drafted ones is at the number of cached tokens + i; without drafted tokens

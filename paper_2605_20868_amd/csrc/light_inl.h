@@ -254,7 +254,7 @@ __device__ __forceinline__ void attend_light(const A& a, int64_t head, int split
       bad |= !(finite2(x.x) & finite2(x.y) & finite2(x.z) & finite2(x.w));
     }
     rows.undefined = max_over_groups(bad ? 1.0f : 0.0f) != 0.0f;
-    zero_undefined(a, rows, rows.q);
+    zero_undefined(rows, rows.q);
   }
 
   uint32_t open = 0u;     // what the lane's row has attended

@@ -119,13 +119,15 @@ static Pass put_pass(SetArgs<SCORES>& a, const Cache* c, int layer, int nodes, i
   x.floats = x.heads * a.row_tiles * a.nsplit * T_FLOATS;
   return x;
 }
+// low: the pass takes its caps as CAP_LOW; any_low: this or the call's other pass
 template <Scores SCORES>
-static void put_scores(SetArgs<SCORES>& a, const cqa_scoring& s, bool many) {
+static void put_scores(SetArgs<SCORES>& a, const cqa_scoring& s, bool low, bool any_low) {
   constexpr float LOG2E = 1.4426950408889634f;
   a.scale = s.scale != 0.0f ? s.scale : PLAIN_SCALE;
   a.cap = s.cap;
-  a.cap_kind = s.cap == 0.0f ? CAP_NONE : (many && s.cap <= LOW_CAPS ? CAP_LOW : CAP_HIGH);
-  a.gain = a.cap_kind == CAP_NONE ? 0.0f : (a.cap_kind == CAP_LOW ? 2.0f * LOG2E : 1.0f) * (a.scale / s.cap);
+  a.cap_kind = s.cap == 0.0f ? CAP_NONE : (low ? CAP_LOW : CAP_HIGH);
+  a.rounded = any_low && s.slopes_dev == nullptr;
+  a.gain = a.cap_kind == CAP_NONE ? 0.0f : (low ? 2.0f * LOG2E : 1.0f) * (a.scale / s.cap);
   if (a.cap_kind == CAP_HIGH) {
     const bool powers = a.gain >= 1e-4f && a.gain <= 1e4f;   // the seventh, by the smallest coefficient, is a normal number
     a.series_end = SERIES_END / a.gain;
@@ -133,8 +135,7 @@ static void put_scores(SetArgs<SCORES>& a, const cqa_scoring& s, bool many) {
     double power = powers ? a.gain : 1.0;
     for (int i = 0; i < 4; ++i, power *= powers ? (double)a.gain * a.gain : 1.0) a.series[i] = (float)(SERIES[i] * power);
   }
-  a.per_unit = LOG2E * (a.cap_kind == CAP_NONE ? a.scale : (a.cap_kind == CAP_LOW ? 2.0f * s.cap : s.cap));
-  a.offset = a.cap_kind == CAP_LOW ? s.cap : 0.0f;
+  a.per_unit = LOG2E * (a.cap_kind == CAP_NONE ? a.scale : s.cap);
   a.slopes = s.slopes_dev;
   a.places = s.places_dev;
   a.spans = s.spans_dev;
@@ -187,9 +188,10 @@ static int32_t run(const Cache* shared, const Cache* c, int layer, const NodeCal
   const Pass own = put_pass(a, c, layer, call.n, drafts, (int)beginning);
   const Pass theirs = has_shared ? put_pass(b, shared, layer, call.n * (c->desc.batch / shared->desc.batch), 0, 0) : Pass{};
   if constexpr (SCORES != PLAIN) {
-    const bool many = (has_own && own.shape.rows >= 128) || (has_shared && theirs.shape.rows >= 128);
-    put_scores(a, *call.scoring, many);
-    put_scores(b, *call.scoring, many);
+    const bool may = call.scoring->cap != 0.0f && call.scoring->cap <= LOW_CAPS;
+    const bool low = may && has_own && own.shape.rows >= 128, their_low = may && has_shared && theirs.shape.rows >= 128;
+    put_scores(a, *call.scoring, low, low || their_low);
+    put_scores(b, *call.scoring, their_low, low || their_low);
   }
   if (!has_shared) return launch_alone(a, own, c->n_cu, st);
   if (!has_own) return launch_alone(b, theirs, c->n_cu, st);

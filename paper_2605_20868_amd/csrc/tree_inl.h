@@ -92,16 +92,17 @@ struct TreeArgs {
 // Of a pass whose nodes may be several sequences' (a beginning that they share), that has drafted tokens or none, that may leave its sets to be
 // joined with another pass's; SCORES: with scores of the caller's.  x = scale q . k,  y = cap tanh(x / cap),  score = y - slope |p - j|.
 // The bias counts from the distance `near` of the row's nearest attended token (the farthest, under a negative slope), so that the scores of a row that
-// attends far tokens only keep their bits.  What the softmax works on is the score in units of its own, `per_unit` exponents of 2 each, and less a
-// constant of the row:
+// attends far tokens only keep their bits.  What the softmax works on is the score in units of its own, `per_unit` exponents of 2 each:
 //   CAP_NONE   q . k
-//   CAP_LOW    -1 / (1 + e^(2 x / cap)) = (tanh(x / cap) - 1) / 2, an exponential and a reciprocal: off by 2^-24 of a unit, 2 cap
-//   CAP_HIGH   tanh(x / cap), relatively exact: a series up to 0.36, which is one operation more, beside 1 - 2 / (1 + e^(2 x / cap)) where a wave has larger ones
+//   CAP_LOW    tanh(x / cap) = (1 - E) / (1 + E) with x's sign, E = e^(-2 |x| / cap): within 2^-21 of itself but for E's own rounding, 2^-25 of a unit
+//   CAP_HIGH   tanh(x / cap) within 2^-21 of itself: a series up to 0.36, beside 1 - 2 / (1 + e^(2 x / cap)) where a wave has larger ones
 // LOW where a pass reconstructs for 128 or 256 rows at once, which the scores' operations bound, and the cap is at most LOW_CAPS (us a call in a graph, LOW and
-// HIGH: 8 heads, 131072 tokens, 64 nodes of 4 heads 222, 287; 2 x 8 heads, 16000 tokens, 20 nodes of 4 50.5, 57.0; 64 rows, 8 heads, 32000 tokens 44, 42; one token,
-// 131072 tokens 66.5, 66.7).
+// HIGH: 8 heads, 131072 tokens, 64 nodes of 4 heads 257, 316; 2 x 8 heads, 16000 tokens, 20 nodes of 4 49.6, 54.7).  Up to that cap E's rounding is no more than what FP32 products
+// of ordinary queries and keys leave (max_block_contrib against 64 bits, the most sensitive, LOW and the plain form in FP32: 2 x 4 sequences behind 16399 tokens, cap 50 4.7e-7,
+// 9.1e-7, cap 128 8.5e-7, 9.0e-7, cap 250 1.5e-6, 9.1e-7; -1 / (1 + e^(2 x / cap)), three operations fewer, 1.5e-6, 4.0e-6 and 8.1e-6, and 232 us where LOW took 242).
+// Both forms have one unit, so that a call's two passes may take different ones.
 enum { CAP_NONE = 0, CAP_LOW, CAP_HIGH };
-constexpr float LOW_CAPS = 256.0f;
+constexpr float LOW_CAPS = 128.0f;
 enum Scores { PLAIN = 0, SCALED, PLACED };   // q . k / sqrt(d) of every token; by scale and cap; by places and spans as well
 template <Scores SCORES>
 struct SetArgs : TreeArgs {
@@ -114,10 +115,11 @@ struct SetArgs : TreeArgs {
   int cached;              // cached tokens of all passes: spans and places count through them
   int drafted;             // the sequences have drafted tokens, in this pass or another
   int cap_kind;
+  int rounded;             // the exponents are rounded with m (less_most): of all passes alike
   float gain;              // x / cap by q . k: CAP_LOW in exponents of 2, twice
   // CAP_HIGH: the series by powers of pre q . k, 1, 3, ...; it holds for q . k up to series_end.  pre is 1, or the gain, whose powers no coefficients hold
   float series[4], series_end, pre;
-  float per_unit, offset;  // offset: of the score, where the unit's zero is
+  float per_unit;
   float cap, scale;
   const float* slopes;     // [Hq]
   const int64_t* places;   // [Bt][n]
@@ -301,10 +303,10 @@ __device__ __forceinline__ RowBias row_bias(const A& a, int64_t node, int q_head
 template <typename A>
 __device__ __forceinline__ float row_offset(const A& a, int64_t node, int q_head) {
   if constexpr (A::SCORED) {
-    if constexpr (!A::PLACED) return a.offset;
-    if (a.slopes == nullptr) return a.offset;
+    if constexpr (!A::PLACED) return 0.0f;
+    if (a.slopes == nullptr) return 0.0f;
     const RowBias x = row_bias(a, node, q_head, spans_given(a, node));
-    return fmaf(-x.slope, (float)x.near, a.offset);
+    return -x.slope * (float)x.near;
   }
   return 0.0f;
 }
@@ -318,11 +320,15 @@ __device__ __forceinline__ float tanh_series(const A& a, float s) {
 }
 // A lane's products with N tokens become scores.  far(r): |place - token| - near.  A row's numbers do not depend on the form that the others of its wave need.
 template <typename A>
-__device__ __forceinline__ float cap_low(const A& a, float s) { return __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s * a.gain)); }
-// low_done: CAP_LOW has been applied.  NEAR: CAP_HIGH looks whether the series is enough (a kernel without registers for both forms does not).
-template <int N, bool NEAR = true, typename A, typename Rows, typename V, typename Far>
+__device__ __forceinline__ float cap_low(const A& a, float s) {
+  const float e = __builtin_amdgcn_exp2f(-fabsf(s * a.gain));
+  return copysignf((1.0f - e) * __builtin_amdgcn_rcpf(1.0f + e), s);
+}
+// low_done: CAP_LOW has been applied.  NEAR: CAP_HIGH looks whether the series is enough (a kernel without registers for both forms does not).  LOW: the kernel
+// is one that takes caps as CAP_LOW.
+template <int N, bool NEAR = true, bool LOW = false, typename A, typename Rows, typename V, typename Far>
 __device__ __forceinline__ void score(const A& a, const Rows& w, V& s, Far far, bool low_done = false) {
-  if (a.cap_kind == CAP_LOW) {
+  if (LOW && a.cap_kind == CAP_LOW) {
     if (!low_done)
 #pragma unroll
       for (int r = 0; r < N; ++r) s[r] = cap_low(a, s[r]);
@@ -498,10 +504,9 @@ __device__ __forceinline__ void mend_pair(uint4& km0, uint4& km1, uint4& vm, uin
 }
 // A query or a slope that is not finite (a slope of more than 10^28 times the cap, or the scale, with it, for distances are numbers too): zeros, which nothing
 // passes on; the row's sum is no number at the end.
-template <typename A, typename Rows, int N>
-__device__ __forceinline__ void zero_undefined(const A& a, Rows& w, f16x8 (&q)[N]) {
-  bool steep = false;
-  if constexpr (A::PLACED) steep = !(fabsf(w.slope) <= (a.cap_kind == CAP_LOW ? 0.5f * 1e28f : 1e28f));   // (CAP_LOW's unit is two caps)
+template <typename Rows, int N>
+__device__ __forceinline__ void zero_undefined(Rows& w, f16x8 (&q)[N]) {
+  const bool steep = !(fabsf(w.slope) <= 1e28f);
   w.undefined |= steep;
   w.slope = steep ? 0.0f : w.slope;
 #pragma unroll
@@ -530,7 +535,7 @@ __device__ __forceinline__ void start_rows(RowsOf<A>& s, const A& a, int tile, c
       bad |= !(finite2(x.x) & finite2(x.y) & finite2(x.z) & finite2(x.w));
     }
     s.undefined = max_x32(bad ? 1.0f : 0.0f) != 0.0f;
-    zero_undefined(a, s, s.q);
+    zero_undefined(s, s.q);
   }
 }
 // The bias and the spans of a wave's rows, of sequence or beginning b; sealed and trailing tokens: count.  The spans go to LDS, a row's 16 bytes.
@@ -566,12 +571,11 @@ __device__ __forceinline__ void values32(TreeRows& w, const uint32_t (&p)[8], Va
           value(oct, ct), __builtin_bit_cast(f16x8, make_uint4(p[4 * oct], p[4 * oct + 1], p[4 * oct + 2], p[4 * oct + 3])), w.o[ct], 0, 0, 0);
 }
 // What weights relative to a largest score m are worth beside a largest one M >= m (-inf: there are none).
-// Under CAP_LOW without a bias, whose scores are within 2 cap of each other, the exponents are rounded with m (less_most), and here alike.  (With a bias
-// that rounding may be more than FP16's range: those of far tokens alone are as large as the caller's slopes.)
+// Where a pass takes its caps as CAP_LOW and there is no bias, scores are within 2 LOW_CAPS of each other, and the exponents are rounded with m (less_most), here alike, and in
+// the other pass of the call, whose sets meet these.  (With a bias that rounding may be more than FP16's range: those of far tokens alone are as large as the caller's slopes.)
 template <typename A>
 __device__ __forceinline__ bool rounds_most(const A& a) {
-  if constexpr (A::PLACED) return a.cap_kind == CAP_LOW && a.slopes == nullptr;
-  if constexpr (A::SCORED) return a.cap_kind == CAP_LOW;
+  if constexpr (A::SCORED) return a.rounded != 0;
   return false;
 }
 template <typename A>
@@ -634,8 +638,8 @@ __device__ __forceinline__ void softmax32(const A& a, TreeRows& w, f32x16 (&s)[M
     w.evmax = fmaxf(w.evmax, e);
   }
 }
-// The same in passes of SetArgs, for MT times N scores of a lane.  Under CAP_LOW without a bias m is taken off in the
-// multiply-add that scales them: one rounding, 2^-18 of an exponent, that all weights by this m share and that set_weight and lse know of (8 heads, 131072 tokens, 64 nodes of 4 heads 245, 229
+// The same in passes of SetArgs, for MT times N scores of a lane.  Where exponents are rounded with m it is taken off in the
+// multiply-add that scales them: one rounding, 2^-17 of an exponent at most, that all weights by this m share and that set_weight and lse know of (8 heads, 131072 tokens, 64 nodes of 4 heads 245, 229
 // us).  largest(x): over the lanes of a row; block(x): the sum over a block.
 // silent: a lane's row has no part in it (one that attends no cached token, among others whose tokens are not looked at one by one).
 template <int MT, int N, typename A, typename Rows, typename V, typename Bits, typename Eta, typename Largest, typename Block>
@@ -706,12 +710,12 @@ __device__ __forceinline__ bool silent_of(const Rows& w) {
   return false;
 }
 // All of it, of exact tokens.
-template <typename A, typename Key, typename Value>
+template <bool LOW = false, typename A, typename Key, typename Value>
 __device__ __forceinline__ void attend32(const A& a, RowsOf<A>& w, uint32_t bits, const int* places, Key key, Value value) {
   f32x16 s[1];
   uint32_t p[1][8];
   scores32(w, s[0], key);
-  if constexpr (A::SCORED) score<16, false>(a, w, s[0], [&](int r) { return (float)(abs(w.place - places[r]) - w.near); });
+  if constexpr (A::SCORED) score<16, false, LOW>(a, w, s[0], [&](int r) { return (float)(abs(w.place - places[r]) - w.near); });
   weigh32<1>(a, w, s, p, true, [&](int) { return bits; }, [&](int) { return 0.0f; });
   values32(w, p[0], value);
 }
@@ -1012,7 +1016,7 @@ __device__ __forceinline__ Certificate certificate(const A& a, float M, float L,
   ct.alpha_tail_hat = sealed * inv;
   ct.lse = empty ? -INFINITY : fmaf(M, a.unit() * LN2, logf(L) - MOST * LN2);
   if constexpr (A::SCORED) {
-    if (rounds_most(a)) ct.lse = fmaf(2.0f * a.cap, M, offset) + fmaf(-LN2, fmaf(M, a.unit(), less_most(a, M)), logf(L));   // (m's part and its rounding)
+    if (rounds_most(a)) ct.lse = fmaf(a.cap, M, offset) + fmaf(-LN2, fmaf(M, a.unit(), less_most(a, M)), logf(L));   // (m's part and its rounding)
     else ct.lse += offset;
     if (empty) ct.lse = -INFINITY;
   }
@@ -1667,7 +1671,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
   constexpr int PRODUCTS = 16 * MT, AHEAD = 6, FROM = 2, EACH = QUADS == 2 ? 4 : 2, BEHIND = FROM + PIECES * QUADS / EACH;
   static_assert(PIECES * QUADS % EACH == 0 && BEHIND < PRODUCTS, "the pieces end ahead of the products");
   // Products with keys: the accumulators take turns; where caps are applied, the first 32 tokens' come first, and their caps stand between the others',
-  // CAPS scores a product (8 heads, 131072 tokens, 64 nodes of 4 heads 237 us, behind the products 242).
+  // CAPS scores a product (8 heads, 131072 tokens, 64 nodes of 4 heads 257 us, behind the products 263).
   constexpr bool EARLY = A::SCORED && MT == 2;
   constexpr int CAPS = 3, CAPS_FROM = PRODUCTS - 6;
   const auto key_mt = [](int k) constexpr { return EARLY ? k / 8 : k % MT; };
@@ -1792,7 +1796,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
           if (blk >= a.nb || rows.idle) there[mt] = 0u;
           open |= there[mt];
           rows.vmax = fmaxf(rows.vmax, there[mt] == 0u ? 0.0f : block_nu[mt]);
-          score<16, MT == 1>(a, rows, sc[mt], RunFar<BLK>(rows, blk * BLK), EARLY && mt == 0);
+          score<16, MT == 1, WR >= 4>(a, rows, sc[mt], RunFar<BLK>(rows, blk * BLK), EARLY && mt == 0);
         }
         masked |= some;
         weigh32<MT>(
@@ -1801,7 +1805,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
       } else {
         if constexpr (A::SCORED)
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) score<16, MT == 1>(a, rows, sc[mt], [](int) { return 0.0f; }, EARLY && mt == 0);
+          for (int mt = 0; mt < MT; ++mt) score<16, MT == 1, WR >= 4>(a, rows, sc[mt], [](int) { return 0.0f; }, EARLY && mt == 0);
         weigh32<MT>(
             a, rows, sc, p, (int64_t)(u + 1) * BLKS > a.nb, [&](int mt) { return (int64_t)u * BLKS + (wt * MT + mt) * 2 + half < a.nb ? 0xffffu : 0u; },
             [&](int mt) { return s_eta[turn & 3][(wt * MT + mt) * 2 + half]; });
@@ -1860,7 +1864,7 @@ __device__ __forceinline__ void attend_many(const A& a, int64_t head, int split,
       const int unit = wt * MT + mt, blk = unit * 2 + half;
       open |= bits[mt];
       open_exact(rows, bits[mt], s_norm + blk * BLK, s_bad + blk * BLK);
-      attend32(
+      attend32<(WR >= 4)>(
           a, rows, bits[mt], A::PLACED ? lds.place + blk * BLK : nullptr, [&](int ks) { return key_of(s_k, unit, ks); }, [&](int oct, int ct) { return value_of(s_v, blk, oct, ct); });
     }
   }

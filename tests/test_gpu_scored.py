@@ -218,6 +218,44 @@ def test_the_ends_of_caps_and_scales(n, tokens, cap, scale):
     compare(x, 4, None, (cap, scale), cap=cap, scale=scale)
 
 
+# up to 16, 32, 64, 128 and 256 rows a workgroup; the last with the tokens as a beginning's
+@pytest.mark.parametrize("n,bt,tokens,beginning", [(1, 1, 1300, 0), (8, 1, 1300, 0), (13, 256, 1300, 0), (27, 160, 1300, 0), (64, 160, 1300, 0), (64, 160, 40, 1300), (13, 160, 40, 1300)])
+@pytest.mark.parametrize("cap", [30.0, 64.0, 250.0])
+def test_a_cap_keeps_the_bits_of_small_scores(n, bt, tokens, beginning, cap):
+    """Rows that attend two tokens each, whose q . k are whole numbers, so that the cap is what rounds.  A score is off by cap (2^-25 + |tanh| 2^-21), caps
+    beyond 128 by the second alone (include/cqa.h): scale / cap, its product with q . k, 1 - E, 1 + E and the quotient by some 8 2^-24 of the tanh, E by half of 2^-24.  Two weights beside each other are off by twice that; their exponents of 2, of 14 at most, by half a step, 2^-21 ln 2, each, the exponentials by 2^-23 each; sum, quotient, the
+    block's error and the product by 2^-24 each: 1.2e-6.  lse, besides its score's part, by a step of ln(2^15) = 10.4, 2^-20, and of the numbers taken off it, as large: 2e-6."""
+    print("bits of caps", n, bt, tokens, beginning, cap, flush=True)
+    rng = np.random.default_rng(n + beginning)
+    g, scale = 4, 2.0 ** -4
+    x = make(rng, 1, 1, g, tokens, n, False, shared=1 if beginning else 0, beginning=beginning)
+    for name in ("k", "sk"):
+        if name in x:
+            x[name] = np.where(rng.random(x[name].shape) < 0.5, -1.0, 1.0).astype(np.float16)
+    x["q"] = rng.integers(-2, 3, x["q"].shape).astype(np.float16)
+    total = beginning + tokens
+    keys = np.concatenate([x[name][0, 0] for name in ("sk", "k") if name in x]).astype(np.float64)
+    with Caches(x, g) as c, Caches({k: again(v, bt) for k, v in x.items()}, g) as w:
+        for turn in range(4):
+            spans = np.zeros((1, n, 4), np.int64)
+            spans[..., 0] = rng.integers(0, total // 2 - 16, (1, n))
+            spans[..., 2] = rng.integers(total // 2, total // 16 * 16 if not beginning else total - 16, (1, n))
+            spans[..., 1], spans[..., 3] = spans[..., 0] + 1, spans[..., 2] + 1
+            ref = scored.decode(c.shared_oc, c.oc, x["q"], None, None, None, oracle.Tolerances(), scale=scale, cap=cap, spans=spans)[0]
+            O, cert, flags = call(w.shared, w.gc, again(x["q"], bt), scale=scale, cap=cap, spans=again(spans, bt))
+            for i in range(n):
+                pair = keys[[spans[0, i, 0], spans[0, i, 2]]]
+                for h in range(g):
+                    r = ref[i][h]
+                    most = float(np.tanh(np.abs(pair @ x["q"][0, i, h].astype(np.float64)) * scale / cap).max())
+                    off = cap * ((2.0 ** -25 if cap <= 128 else 0.0) + most * 2.0 ** -21)
+                    for field in ("alpha_tail_hat", "max_block_contrib", "E_val"):
+                        tol = 2 * off + 1.2e-6
+                        assert abs(cert[field][0, i, h] - r[field]) <= tol * r[field], (field, turn, i, h, cert[field][0, i, h] / r[field] - 1, tol)
+                    assert abs(cert["lse"][0, i, h] - r["lse"]) <= off + 2e-6, (turn, i, h, cert["lse"][0, i, h] - r["lse"], off)
+            assert (flags == 0).all() and all(np.array_equal(O[i], O[0]) for i in range(bt))
+
+
 @pytest.mark.parametrize("n", [1, 20, 64])
 @pytest.mark.parametrize("far", [0, 1000, 10 ** 6, 2 ** 29, 2 ** 33, -(2 ** 29), -(2 ** 40)])
 def test_rows_that_attend_only_far_tokens_keep_their_weights(n, far):
